@@ -43,7 +43,8 @@ enum {
   QCFG_EARCH = 7,      /* device is not sm_100                                      */
   QCFG_ECUDA = 8,      /* a CUDA runtime/driver call failed; see qcfg_last_error    */
   QCFG_ETIMEOUT = 9,   /* a bounded device-side wait gave up                        */
-  QCFG_ESTATE = 11     /* call order (e.g. evaluation before calibration)           */
+  QCFG_ESTATE = 11,    /* call order (e.g. evaluation before calibration)           */
+  QCFG_EPAGE = 12      /* cache: a number out of range, pages used up, a number twice */
 };
 enum { QCFG_PER_TENSOR = 0, QCFG_PER_ROW = 1 };
 enum { QCFG_ACT_NONE = 0, QCFG_ACT_RELU = 1, QCFG_ACT_GELU_TANH = 2 };
@@ -74,7 +75,7 @@ int qcfg_create(qcfg_ctx** out, int device);
 int qcfg_destroy(qcfg_ctx* ctx);
 
 /* Synchronises `stream`, then returns and clears the device error word:
- * QCFG_OK, QCFG_ETIMEOUT, QCFG_ENONFINITE or QCFG_ECUDA.                                  */
+ * QCFG_OK, QCFG_ETIMEOUT, QCFG_ENONFINITE, QCFG_EPAGE or QCFG_ECUDA.                      */
 int qcfg_sync_status(qcfg_ctx* ctx, void* stream);
 /* Self-test of the failure path of the kernels' bounded waits (every device-side wait, on a
  * barrier or on a counter in shared or global memory, gives up after a time limit instead of
@@ -239,6 +240,133 @@ int qcfg_gemm_i8_requant(qcfg_ctx* ctx, const int8_t* qx_dev, int64_t ldx, const
 int qcfg_gemm_bf16(qcfg_ctx* ctx, const void* x_bf16_dev, int64_t ldx, const void* w_bf16_dev,
                    int64_t ldw, int64_t m, int64_t n, int64_t k, int act, float* y_dev,
                    void* stream);
+
+/* ---- serving at 8 bits ------------------------------------------------------------------
+ * What a model needs once its configuration has been found: linear layers whose activations get a
+ * scale for each token when they come (Eq. 1 applied row by row, in the call), and a key/value
+ * cache held in 8 bits with the attention that reads it.  (The paper stops at the configuration;
+ * codes and scales follow its Eq. 1 with b = 8 like everything above.)
+ *   - These calls set the context's device for their duration: any device may be current.
+ *   - They allocate nothing and wait for nothing, so they can be captured into CUDA graphs.  Working
+ *     memory is the caller's; calls that may overlap need different ones.
+ *   - Numbers of sequences, pages and rows that lie in device memory are checked on the device: one
+ *     outside its range leaves out the work it stands for and surfaces as QCFG_EPAGE from
+ *     qcfg_sync_status.                                                                       */
+
+/* Element types of the caller's activations.                                                 */
+enum { QCFG_FP32 = 0, QCFG_BF16 = 1, QCFG_FP16 = 2 };
+
+/* Codes of Eq. 1 with one scale for each row (token): absmax[r] = max_c |x[r][c]|, scale and
+ * inverse from it like qcfg_scales_from_absmax, codes like qcfg_quantize (a zero always gets code
+ * 0).  x_dev is [rows x cols] of `dtype` with leading dimension ld (elements), aligned to its
+ * elements; q_dev like qcfg_quantize's; scale_dev receives `rows` floats.  bits in 2..8.  A row
+ * with a NaN or Inf has its finite elements quantized by their own maximum and 0 for the others,
+ * and surfaces as QCFG_ENONFINITE.                                                            */
+int qcfg_quantize_tokens(qcfg_ctx* ctx, const void* x_dev, int dtype, int64_t rows, int64_t cols, int64_t ld, int bits,
+                         int8_t* q_dev, int64_t ldq, float* scale_dev, void* stream);
+
+/* qcfg_gemm_i8 with a scale for each token: y[m][n] = act(float(acc[m][n]) * (scale_x[m] *
+ * scale_w[n]) + bias[n]), rounded once to `dtype`; bias_dev may be NULL.  y_dev is [m x ldy]
+ * elements, aligned to them, ldy >= n; columns n..ldy-1 are left untouched.                    */
+int qcfg_gemm_i8_token(qcfg_ctx* ctx, const int8_t* qx_dev, int64_t ldx, const int8_t* qw_dev, int64_t ldw, int64_t m, int64_t n,
+                       int64_t k, const float* scale_x_dev, const float* scale_w_dev, const float* bias_dev, int act,
+                       void* y_dev, int dtype, int64_t ldy, void* stream);
+
+/* A linear layer on activations as they come: qcfg_quantize_tokens and qcfg_gemm_i8_token, in one
+ * kernel for a few tokens.  work_dev: qcfg_linear_i8_work(m, k) bytes on a 256-byte boundary (0 bytes: may be NULL). */
+int64_t qcfg_linear_i8_work(int64_t m, int64_t k);
+int qcfg_linear_i8(qcfg_ctx* ctx, const void* x_dev, int x_dtype, int64_t ldx, int bits, const int8_t* qw_dev, int64_t ldw,
+                   int64_t m, int64_t n, int64_t k, const float* scale_w_dev, const float* bias_dev, int act, void* y_dev,
+                   int y_dtype, int64_t ldy, void* work_dev, int64_t work_bytes, void* stream);
+
+/* Pages and the sequences that hold them; one pool serves the caches of all layers.  Device memory
+ * of the caller, filled with -1 / 0 / 0 at first and then kept by the calls below.  A sequence of
+ * len tokens holds ceil(len / page_tokens) pages, in order.                                    */
+typedef struct qcfg_kv_pool {
+  int32_t* table_dev;    /* [max_seqs][max_pages] page numbers, -1 behind the last             */
+  int32_t* len_dev;      /* [max_seqs] tokens                                                  */
+  int32_t* refs_dev;     /* [n_pages] sequences that hold the page, 0 = free                   */
+  int32_t n_pages;
+  int32_t page_tokens;   /* 16, 32, 64 or 128                                                  */
+  int32_t max_seqs, max_pages;
+} qcfg_kv_pool;
+/* One layer's keys and values: int8 codes on the 8-bit grid of Eq. 1, one maximum for each page and
+ * head from which the scales follow as in qcfg_scales_from_absmax.  16-byte aligned.           */
+typedef struct qcfg_kv_cache {
+  int8_t *k_dev, *v_dev;                /* [n_pages][kv_heads][page_tokens][head_dim]          */
+  float *k_absmax_dev, *v_absmax_dev;   /* [n_pages][kv_heads]                                 */
+  int32_t kv_heads;
+  int32_t head_dim;                     /* a multiple of 16, 16 .. 256                         */
+} qcfg_kv_cache;
+/* Which sequences a call is about and which rows of its tensors are theirs.  Entry i stands for
+ * sequence seqs_dev[i] (a row of the table; -1: an entry without one, for padded batches) and rows
+ * starts_dev[i] .. starts_dev[i+1]-1 of n_rows; starts_dev == NULL: one row each.  Rows behind the last
+ * entry's belong to nobody: they are neither read nor written.                                 */
+typedef struct qcfg_kv_batch {
+  const int32_t* seqs_dev;     /* [n]                                                          */
+  const int32_t* starts_dev;   /* [n+1], ascending, or NULL                                    */
+  int32_t n;
+  int64_t n_rows;
+} qcfg_kv_batch;
+
+/* Makes every sequence of the batch longer by its rows: pages are taken where the last one is full,
+ * lowest free numbers first, in the order of the entries, and len grows.  All or nothing: with too
+ * few free pages, a row of the table too short or a sequence listed twice nothing changes
+ * (QCFG_EPAGE from qcfg_sync_status).  At most 8192 entries (QCFG_ESHAPE).                       */
+int qcfg_kv_extend(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_batch* batch, void* stream);
+/* Gives back every page of the n sequences (a page held by others too stays theirs); their length is 0 then.
+ * Entries of -1 and empty sequences are passed over.                                           */
+int qcfg_kv_free(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const int32_t* seqs_dev, int32_t n, void* stream);
+/* Makes the empty sequence children_dev[i] a copy of parents_dev[i] (as it was before the call): full
+ * pages are shared, a last page in part gets a page of its own, the lowest free ones in the order of
+ * the entries.  src_dev[i] / dst_dev[i] receive the pages qcfg_kv_copy_pages has to copy in
+ * every layer's cache, -1 where there is none.  Entries with a child of -1 are passed over.  All or
+ * nothing like qcfg_kv_extend (a child that holds tokens or is listed twice, too few pages).  At most 8192 entries. */
+int qcfg_kv_fork(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const int32_t* parents_dev, const int32_t* children_dev, int32_t n,
+                 int32_t* src_dev, int32_t* dst_dev, void* stream);
+/* Moves the pages in use into the lowest numbers: with u pages in use, those at u and above go to the
+ * free ones below, both in ascending order; table and refs follow.  map_dev (2 * n_pages integers,
+ * the second half is working space) receives the new number of every page in use, -1 for free
+ * ones: qcfg_kv_copy_pages(cache, NULL, map, n_pages) moves the contents in every layer's cache.  */
+int qcfg_kv_compact(qcfg_ctx* ctx, const qcfg_kv_pool* pool, int32_t* map_dev, void* stream);
+/* Copies page src_dev[i] to page dst_dev[i], codes and maxima (src_dev == NULL: page i).  Entries with
+ * a -1 or equal numbers are passed over.  No page may be both read and written, none written twice. */
+int qcfg_kv_copy_pages(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const int32_t* src_dev,
+                       const int32_t* dst_dev, int32_t n, void* stream);
+
+/* Writes the keys and values of the last rows-of-the-entry tokens of every sequence of the batch
+ * (qcfg_kv_extend has made room for them).  A page's maximum is that of all tokens written to it:
+ * where new ones raise it, the codes before them become round_half_even(code * (old / new))
+ * (one fp32 division, one product); a page that begins with a new token forgets what it held.
+ * NaN and Inf are held as 0, do not count for the maximum and surface as QCFG_ENONFINITE.  k_dev, v_dev: [n_rows] rows of
+ * `dtype`, row and head strides in elements, 16-byte aligned pointers and strides (QCFG_EALIGN).
+ * Pages that several sequences hold are not written, nor is a sequence listed twice (QCFG_EPAGE from
+ * qcfg_sync_status).                                                                           */
+int qcfg_kv_append(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch, const void* k_dev,
+                   const void* v_dev, int dtype, int64_t row_stride, int64_t head_stride, void* stream);
+/* Values of cached tokens: row r of entry i is the token first_dev[i] + r of its sequence, code * scale, rounded once to
+ * `dtype`; tokens the sequence does not have give zeros.  k_dev, v_dev: dense [n_rows][kv_heads][head_dim],
+ * 16-byte aligned, either may be NULL.                                                         */
+int qcfg_kv_read(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch,
+                 const int32_t* first_dev, void* k_dev, void* v_dev, int dtype, void* stream);
+
+/* Attention over the cache.  The rows of entry i are the queries of the last tokens of its sequence: with
+ * `rows` rows and len tokens row r stands at position p = len - rows + r.  It sees the tokens 0 .. p
+ * (causal), with window > 0 only the last `window` of these, or all len tokens (causal == 0; window
+ * must be 0).  out = softmax(sm_scale * q k^T) v over what it sees; a row that sees nothing (p < 0, an
+ * empty sequence, an entry without one) gives zeros.  q_dev, out_dev: [n_rows] rows of
+ * `dtype` with q_heads heads of head_dim elements, strides in elements, 16-byte aligned pointers and
+ * strides (QCFG_EALIGN); head h reads cache head h / (q_heads / kv_heads).  out_dev must not
+ * overlap q_dev.  Sums, maxima and accumulators are fp32.
+ * max_rows, max_len: the longest entry's rows and the longest sequence's tokens as far as the caller
+ * knows them (0: unknown).  They only choose how the work is spread; the results hold for any value.
+ * work_dev: qcfg_kv_attention_work bytes on a 256-byte boundary, for the parts of rows whose context is
+ * split; its contents need not be set.                                                          */
+int64_t qcfg_kv_attention_work(qcfg_ctx* ctx, const qcfg_kv_cache* cache, int32_t n, int64_t n_rows, int32_t q_heads);
+int qcfg_kv_attention(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch, const void* q_dev,
+                      int64_t q_row_stride, int64_t q_head_stride, int32_t q_heads, void* out_dev, int64_t out_row_stride,
+                      int64_t out_head_stride, int dtype, int32_t max_rows, int32_t max_len, float sm_scale, int causal,
+                      int32_t window, void* work_dev, int64_t work_bytes, void* stream);
 
 /* ---- model-level steps ---------------------------------------------------------------- */
 

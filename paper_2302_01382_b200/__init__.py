@@ -6,6 +6,7 @@ use; if it is missing and cannot be built the call fails loudly -- there is no f
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import List, Optional, Sequence
@@ -20,13 +21,16 @@ ACT_NONE, ACT_RELU, ACT_GELU_TANH = 0, 1, 2
 SEARCH_BISECTION, SEARCH_GREEDY = 0, 1
 FORMS = ("conv_gather", "conv_im2col", "conv_slab", "conv_streamed", "shortcut", "rows", "narrow_fp32")
 STATUS_NAMES = {0: "OK", 1: "EINVAL", 2: "EBITS", 3: "ESHAPE", 4: "EALIGN", 5: "ENOMEM", 6: "ENONFINITE", 7: "EARCH",
-                8: "ECUDA", 9: "ETIMEOUT", 11: "ESTATE"}
+                8: "ECUDA", 9: "ETIMEOUT", 11: "ESTATE", 12: "EPAGE"}
 EINVAL, EBITS, ESHAPE, EALIGN, ENOMEM, ENONFINITE, EARCH, ECUDA, ETIMEOUT = range(1, 10)
-ESTATE = 11
+ESTATE, EPAGE = 11, 12
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 EXPORTS = ["qcfg_create", "qcfg_destroy", "qcfg_sync_status", "qcfg_selftest_wait_timeout", "qcfg_last_error", "qcfg_launch_count",
            "qcfg_set_fusion", "qcfg_set_pair_tiles", "qcfg_set_grouping", "qcfg_set_prefix_reuse", "qcfg_set_implicit_conv", "qcfg_set_gemm_chains", "qcfg_profile_enable", "qcfg_profile_read", "qcfg_calibrate", "qcfg_scales_from_absmax", "qcfg_quantize",
-           "qcfg_quant_error_sweep", "qcfg_quant_error_sweep_static", "qcfg_gemm_i8", "qcfg_gemm_i8_requant", "qcfg_gemm_bf16", "qcfg_model_create",
+           "qcfg_quant_error_sweep", "qcfg_quant_error_sweep_static", "qcfg_gemm_i8", "qcfg_gemm_i8_requant", "qcfg_gemm_bf16",
+           "qcfg_quantize_tokens", "qcfg_gemm_i8_token", "qcfg_linear_i8_work", "qcfg_linear_i8", "qcfg_kv_extend", "qcfg_kv_free", "qcfg_kv_fork",
+           "qcfg_kv_compact", "qcfg_kv_copy_pages", "qcfg_kv_append", "qcfg_kv_read", "qcfg_kv_attention_work", "qcfg_kv_attention", "qcfg_model_create",
            "qcfg_model_destroy", "qcfg_calibrate_model", "qcfg_model_act_absmax",
            "qcfg_model_weight_absmax", "qcfg_eval_config", "qcfg_latency_table", "qcfg_config_cost", "qcfg_noise_sensitivity", "qcfg_search", "qcfg_adjust_scales", "qcfg_scale_gradients", "qcfg_model_scales",
            "qcfg_model_reset_scales", "qcfg_debug_dump", "qcfg_debug_launch_forms"]
@@ -47,6 +51,20 @@ class LayerStruct(C.Structure):
                 ("residual_from", C.c_int32)]
 
 
+class PoolStruct(C.Structure):
+    _fields_ = [("table_dev", C.c_void_p), ("len_dev", C.c_void_p), ("refs_dev", C.c_void_p), ("n_pages", C.c_int32),
+                ("page_tokens", C.c_int32), ("max_seqs", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class CacheStruct(C.Structure):
+    _fields_ = [("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("k_absmax_dev", C.c_void_p), ("v_absmax_dev", C.c_void_p),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class BatchStruct(C.Structure):
+    _fields_ = [("seqs_dev", C.c_void_p), ("starts_dev", C.c_void_p), ("n", C.c_int32), ("n_rows", C.c_int64)]
+
+
 _lib = None
 
 
@@ -59,6 +77,7 @@ def load_library() -> C.CDLL:
         build_library()
     lib = C.CDLL(LIB)
     vp, i64, i32, ci, f32 = C.c_void_p, C.c_int64, C.c_int32, C.c_int, C.c_float
+    pool, cache, batch = C.POINTER(PoolStruct), C.POINTER(CacheStruct), C.POINTER(BatchStruct)
     sig = {
         "qcfg_create": [C.POINTER(vp), ci],
         "qcfg_destroy": [vp],
@@ -80,6 +99,17 @@ def load_library() -> C.CDLL:
         "qcfg_gemm_i8": [vp, vp, i64, vp, i64, i64, i64, i64, f32, vp, ci, vp, vp, vp],
         "qcfg_gemm_i8_requant": [vp, vp, i64, vp, i64, i64, i64, i64, f32, vp, ci, f32, ci, vp, i64, vp],
         "qcfg_gemm_bf16": [vp, vp, i64, vp, i64, i64, i64, i64, ci, vp, vp],
+        "qcfg_quantize_tokens": [vp, vp, ci, i64, i64, i64, ci, vp, i64, vp, vp],
+        "qcfg_gemm_i8_token": [vp, vp, i64, vp, i64, i64, i64, i64, vp, vp, vp, ci, vp, ci, i64, vp],
+        "qcfg_linear_i8": [vp, vp, ci, i64, ci, vp, i64, i64, i64, i64, vp, vp, ci, vp, ci, i64, vp, i64, vp],
+        "qcfg_kv_extend": [vp, pool, batch, vp],
+        "qcfg_kv_free": [vp, pool, vp, i32, vp],
+        "qcfg_kv_fork": [vp, pool, vp, vp, i32, vp, vp, vp],
+        "qcfg_kv_compact": [vp, pool, vp, vp],
+        "qcfg_kv_copy_pages": [vp, pool, cache, vp, vp, i32, vp],
+        "qcfg_kv_append": [vp, pool, cache, batch, vp, vp, ci, i64, i64, vp],
+        "qcfg_kv_read": [vp, pool, cache, batch, vp, vp, vp, ci, vp],
+        "qcfg_kv_attention": [vp, pool, cache, batch, vp, i64, i64, i32, vp, i64, i64, ci, i32, i32, f32, ci, i32, vp, i64, vp],
         "qcfg_model_create": [vp, C.POINTER(LayerStruct), i32, C.POINTER(vp)],
         "qcfg_model_destroy": [vp],
         "qcfg_calibrate_model": [vp, vp, vp, i64, vp],
@@ -108,6 +138,10 @@ def load_library() -> C.CDLL:
     lib.qcfg_last_error.restype = C.c_char_p
     lib.qcfg_launch_count.argtypes = [vp]
     lib.qcfg_launch_count.restype = i64
+    lib.qcfg_linear_i8_work.argtypes = [i64, i64]
+    lib.qcfg_linear_i8_work.restype = i64
+    lib.qcfg_kv_attention_work.argtypes = [vp, cache, i32, i64, i32]
+    lib.qcfg_kv_attention_work.restype = i64
     _lib = lib
     return lib
 
@@ -289,6 +323,244 @@ class Context:
         self._check(self.lib.qcfg_gemm_bf16(self.h, _ptr(x), x.stride(0), _ptr(w), w.stride(0), m, n, k, act, _ptr(y), _stream(stream)))
         return y
 
+    # ---- linear layers with a scale for each token
+    def _on_device(self, *tensors):
+        for t in tensors:
+            if t is not None and (t.device.type != "cuda" or t.device.index != self.device):
+                raise QcfgError(EINVAL, f"tensor on {t.device}, the context is on cuda:{self.device}")
+
+    def quantize_tokens(self, x: torch.Tensor, bits: int = 8, ldq: Optional[int] = None, stream=None):
+        """Codes of the rows of x (fp32, bf16 or fp16), each with its own scale.  Returns (codes [rows x ldq], scales)."""
+        self._on_device(x)
+        _rows_of(x)
+        rows, cols = x.shape
+        if ldq is None:
+            ldq = (cols + 15) // 16 * 16
+        with _stream_scope(stream):
+            q = torch.empty((rows, ldq), dtype=torch.int8, device=x.device)
+            scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+        self._check(self.lib.qcfg_quantize_tokens(self.h, _ptr(x), _dtype(x.dtype), rows, cols, _ld(x), bits, _ptr(q), ldq, _ptr(scale),
+                                                  self._here(stream)))
+        return q, scale
+
+    def gemm_i8_token(self, qx: torch.Tensor, qw: torch.Tensor, k: int, scale_x: torch.Tensor, scale_w: torch.Tensor,
+                      bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, dtype: torch.dtype = torch.float32,
+                      out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """act(float(qx qw^T) * (scale_x[m] * scale_w[n]) + bias[n]) as `dtype`."""
+        self._on_device(qx, qw, scale_x, scale_w, bias, out)
+        for t in (qx, qw):
+            _rows_of(t, torch.int8)
+        m, n = qx.shape[0], qw.shape[0]
+        if k > qx.shape[1] or k > qw.shape[1]:
+            raise QcfgError(ESHAPE, "k is larger than the operands' rows")
+        _vector(scale_x, m)
+        _vector(scale_w, n)
+        _vector(bias, n)
+        out = _output(out, (m, n), dtype, qx.device, stream)
+        self._check(self.lib.qcfg_gemm_i8_token(self.h, _ptr(qx), _ld(qx), _ptr(qw), _ld(qw), m, n, k, _ptr(scale_x), _ptr(scale_w),
+                                                _ptr(bias), act, _ptr(out), _dtype(out.dtype), _ld(out), self._here(stream)))
+        return out
+
+    def linear_i8(self, x: torch.Tensor, qw: torch.Tensor, scale_w: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                  act: int = ACT_NONE, bits: int = 8, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+        """A linear layer on x (fp32, bf16 or fp16, quantized row by row) with the weight codes qw [n x ld] that
+        quantize(w, inv, PER_ROW, bits) gives and their scales.  `dtype` of the result: that of x unless given."""
+        self._on_device(x, qw, scale_w, bias, out)
+        _rows_of(x)
+        _rows_of(qw, torch.int8)
+        (m, k), n = x.shape, qw.shape[0]
+        if k > qw.shape[1]:
+            raise QcfgError(ESHAPE, "x has more columns than the weight codes")
+        _vector(scale_w, n)
+        _vector(bias, n)
+        out = _output(out, (m, n), dtype or x.dtype, x.device, stream)
+        work, size = _work(self.lib.qcfg_linear_i8_work(m, k), x.device, stream)
+        self._check(self.lib.qcfg_linear_i8(self.h, _ptr(x), _dtype(x.dtype), _ld(x), bits, _ptr(qw), _ld(qw), m, n, k, _ptr(scale_w),
+                                            _ptr(bias), act, _ptr(out), _dtype(out.dtype), _ld(out), _ptr(work), size, self._here(stream)))
+        return out
+
+    def _here(self, stream) -> C.c_void_p:
+        """The stream's handle; without one the current stream of the context's device."""
+        return C.c_void_p((stream if stream is not None else torch.cuda.current_stream(self.device)).cuda_stream)
+
+
+def _rows_of(x: torch.Tensor, dtype: Optional[torch.dtype] = None):
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise QcfgError(ESHAPE, "a matrix with adjacent columns is needed")
+    if dtype is not None and x.dtype != dtype:
+        raise QcfgError(EINVAL, f"{dtype} is needed, got {x.dtype}")
+
+
+def _ld(x: torch.Tensor) -> int:
+    return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], x.stride(0))
+
+
+def _vector(x: Optional[torch.Tensor], n: int):
+    if x is not None and (x.dtype != torch.float32 or x.numel() != n or not x.is_contiguous()):
+        raise QcfgError(ESHAPE, f"{n} adjacent fp32 values are needed")
+
+
+def _dtype(t: torch.dtype) -> int:
+    if t not in DTYPES:
+        raise QcfgError(EINVAL, f"fp32, bf16 or fp16 is needed, got {t}")
+    return DTYPES[t]
+
+
+def _stream_scope(stream):
+    """Memory allocated inside belongs to the stream that will use it (None: the current one)."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def _output(out, shape, dtype, device, stream):
+    if out is None:
+        _dtype(dtype)
+        with _stream_scope(stream):
+            return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(shape) or out.stride(-1) != 1:
+        raise QcfgError(ESHAPE, f"out must be {tuple(shape)} with adjacent columns")
+    return out
+
+
+def _work(size: int, device, stream):
+    if size == 0:
+        return None, 0
+    with _stream_scope(stream):
+        return torch.empty(size, dtype=torch.uint8, device=device), size
+
+
+def _int32(x: Optional[torch.Tensor], n: Optional[int] = None):
+    if x is not None and (x.dtype != torch.int32 or not x.is_contiguous() or (n is not None and x.numel() != n)):
+        raise QcfgError(EINVAL, "adjacent int32 values are needed" + ("" if n is None else f", {n} of them"))
+
+
+class KvPool:
+    """Pages and the sequences that hold them (qcfg_kv_pool).  table [max_seqs, max_pages], lens [max_seqs] and refs [n_pages]
+    are int32 tensors on the context's device, made here unless given."""
+
+    def __init__(self, ctx: Context, n_pages: int, page_tokens: int, max_seqs: int, max_pages: int, table: Optional[torch.Tensor] = None,
+                 lens: Optional[torch.Tensor] = None, refs: Optional[torch.Tensor] = None):
+        dev = torch.device("cuda", ctx.device)
+        self.ctx = ctx
+        self.table = torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=dev) if table is None else table
+        self.lens = torch.zeros(max_seqs, dtype=torch.int32, device=dev) if lens is None else lens
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=dev) if refs is None else refs
+        ctx._on_device(self.table, self.lens, self.refs)
+        for t, n in ((self.table, max_seqs * max_pages), (self.lens, max_seqs), (self.refs, n_pages)):
+            _int32(t, n)
+        self.n_pages, self.page_tokens, self.max_seqs, self.max_pages = n_pages, page_tokens, max_seqs, max_pages
+        self._c = PoolStruct(self.table.data_ptr(), self.lens.data_ptr(), self.refs.data_ptr(), n_pages, page_tokens, max_seqs, max_pages)
+
+    def _batch(self, seqs: torch.Tensor, starts: Optional[torch.Tensor], rows: int) -> BatchStruct:
+        n = seqs.numel()
+        _int32(seqs)
+        _int32(starts, n + 1)
+        self.ctx._on_device(seqs, starts)
+        return BatchStruct(seqs.data_ptr(), None if starts is None else starts.data_ptr(), n, rows)
+
+    def extend(self, seqs: torch.Tensor, starts: Optional[torch.Tensor] = None, rows: Optional[int] = None, stream=None):
+        """Every sequence of `seqs` gets room for its rows (starts[i+1] - starts[i]; one each without starts)."""
+        b = self._batch(seqs, starts, 0x7fffffff - 4096 if rows is None else rows)
+        self.ctx._check(self.ctx.lib.qcfg_kv_extend(self.ctx.h, C.byref(self._c), C.byref(b), self.ctx._here(stream)))
+
+    def free(self, seqs: torch.Tensor, stream=None):
+        _int32(seqs)
+        self.ctx._on_device(seqs)
+        self.ctx._check(self.ctx.lib.qcfg_kv_free(self.ctx.h, C.byref(self._c), _ptr(seqs), seqs.numel(), self.ctx._here(stream)))
+
+    def fork(self, parents: torch.Tensor, children: torch.Tensor, stream=None):
+        """Returns (src, dst): the pages that copy_pages has to copy in every layer's cache."""
+        _int32(parents)
+        _int32(children, parents.numel())
+        self.ctx._on_device(parents, children)
+        with _stream_scope(stream):
+            src, dst = torch.empty_like(parents), torch.empty_like(parents)
+        self.ctx._check(self.ctx.lib.qcfg_kv_fork(self.ctx.h, C.byref(self._c), _ptr(parents), _ptr(children), parents.numel(), _ptr(src),
+                                                  _ptr(dst), self.ctx._here(stream)))
+        return src, dst
+
+    def compact(self, stream=None) -> torch.Tensor:
+        """Returns the new number of every page in use, -1 for free ones: copy_pages(None, that) moves the contents."""
+        with _stream_scope(stream):
+            where = torch.empty(2 * self.n_pages, dtype=torch.int32, device=self.refs.device)
+        self.ctx._check(self.ctx.lib.qcfg_kv_compact(self.ctx.h, C.byref(self._c), _ptr(where), self.ctx._here(stream)))
+        return where[:self.n_pages]
+
+
+class KvCache:
+    """One layer's keys and values in int8 (qcfg_kv_cache): codes [n_pages, kv_heads, page_tokens, head_dim] and maxima
+    [n_pages, kv_heads], made here unless given."""
+
+    def __init__(self, pool: KvPool, kv_heads: int, head_dim: int, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                 k_absmax: Optional[torch.Tensor] = None, v_absmax: Optional[torch.Tensor] = None):
+        dev = torch.device("cuda", pool.ctx.device)
+        self.pool, self.ctx, self.kv_heads, self.head_dim = pool, pool.ctx, kv_heads, head_dim
+        shape = (pool.n_pages, kv_heads, pool.page_tokens, head_dim)
+        self.k, self.v = (torch.zeros(shape, dtype=torch.int8, device=dev) if t is None else t for t in (k, v))
+        self.k_absmax, self.v_absmax = (torch.zeros(shape[:2], dtype=torch.float32, device=dev) if t is None else t for t in (k_absmax, v_absmax))
+        self.ctx._on_device(self.k, self.v, self.k_absmax, self.v_absmax)
+        for t, want, dt in ((self.k, shape, torch.int8), (self.v, shape, torch.int8), (self.k_absmax, shape[:2], torch.float32),
+                            (self.v_absmax, shape[:2], torch.float32)):
+            if tuple(t.shape) != want or t.dtype != dt or not t.is_contiguous():
+                raise QcfgError(ESHAPE, f"a dense {dt} tensor of {want} is needed")
+        self._c = CacheStruct(self.k.data_ptr(), self.v.data_ptr(), self.k_absmax.data_ptr(), self.v_absmax.data_ptr(), kv_heads, head_dim)
+
+    def _heads_of(self, x: torch.Tensor, heads: Optional[int]):
+        if x.dim() != 3 or x.shape[2] != self.head_dim or x.stride(2) != 1 or (heads is not None and x.shape[1] != heads):
+            raise QcfgError(ESHAPE, f"[rows, {heads or 'heads'}, {self.head_dim}] with adjacent elements is needed")
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, seqs: torch.Tensor, starts: Optional[torch.Tensor] = None, stream=None):
+        """Writes the last tokens of every sequence of the batch (KvPool.extend has made room for them)."""
+        self.ctx._on_device(k, v)
+        self._heads_of(k, self.kv_heads)
+        self._heads_of(v, self.kv_heads)
+        if k.shape != v.shape or k.dtype != v.dtype or k.stride()[:2] != v.stride()[:2]:
+            raise QcfgError(ESHAPE, "keys and values must agree in shape, type and strides")
+        b = self.pool._batch(seqs, starts, k.shape[0])
+        self.ctx._check(self.ctx.lib.qcfg_kv_append(self.ctx.h, C.byref(self.pool._c), C.byref(self._c), C.byref(b), _ptr(k), _ptr(v),
+                                                    _dtype(k.dtype), k.stride(0), k.stride(1), self.ctx._here(stream)))
+
+    def read(self, seqs: torch.Tensor, first: torch.Tensor, starts: Optional[torch.Tensor], rows: int, dtype: torch.dtype = torch.float32,
+             stream=None):
+        """Values of the tokens first[i] .. of every sequence, as many as its rows: (k, v), each [rows, kv_heads, head_dim].
+        Rows behind the last sequence's are left as they are (unset)."""
+        b = self.pool._batch(seqs, starts, rows)
+        _int32(first, seqs.numel())
+        self.ctx._on_device(first)
+        shape = (rows, self.kv_heads, self.head_dim)
+        k, v = (_output(None, shape, dtype, self.k.device, stream) for _ in range(2))
+        self.ctx._check(self.ctx.lib.qcfg_kv_read(self.ctx.h, C.byref(self.pool._c), C.byref(self._c), C.byref(b), _ptr(first), _ptr(k), _ptr(v),
+                                                  _dtype(dtype), self.ctx._here(stream)))
+        return k, v
+
+    def copy_pages(self, src: Optional[torch.Tensor], dst: torch.Tensor, stream=None):
+        """Page src[i] (i itself without src) to page dst[i]; entries of -1 are passed over."""
+        _int32(dst)
+        _int32(src, dst.numel())
+        self.ctx._on_device(src, dst)
+        self.ctx._check(self.ctx.lib.qcfg_kv_copy_pages(self.ctx.h, C.byref(self.pool._c), C.byref(self._c), _ptr(src), _ptr(dst), dst.numel(),
+                                                        self.ctx._here(stream)))
+
+    def attention(self, q: torch.Tensor, seqs: torch.Tensor, starts: Optional[torch.Tensor] = None, sm_scale: Optional[float] = None,
+                  causal: bool = True, window: int = 0, max_new: int = 0, max_len: int = 0, out: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+        """softmax(sm_scale * q k^T) v of the last tokens of every sequence: q [rows, q_heads, head_dim], out like q.
+        sm_scale: 1 / sqrt(head_dim) unless given; max_new, max_len: the longest entry and sequence, where known."""
+        self.ctx._on_device(q, out)
+        self._heads_of(q, None)
+        if out is None:
+            out = _output(None, q.shape, q.dtype, q.device, stream)
+        self._heads_of(out, q.shape[1])
+        if out.dtype != q.dtype or out.shape != q.shape:
+            raise QcfgError(ESHAPE, "out must be like q")
+        b = self.pool._batch(seqs, starts, q.shape[0])
+        lib, h = self.ctx.lib, self.ctx.h
+        work, size = _work(lib.qcfg_kv_attention_work(h, C.byref(self._c), b.n, b.n_rows, q.shape[1]), q.device, stream)
+        self.ctx._check(lib.qcfg_kv_attention(h, C.byref(self.pool._c), C.byref(self._c), C.byref(b), _ptr(q), q.stride(0), q.stride(1), q.shape[1],
+                                              _ptr(out), out.stride(0), out.stride(1), _dtype(q.dtype), max_new, max_len,
+                                              self.head_dim ** -0.5 if sm_scale is None else float(sm_scale), int(causal), window, _ptr(work), size,
+                                              self.ctx._here(stream)))
+        return out
 
 class Model:
     """Owns one qcfg_model built from a list of layer descriptions and device weights."""

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "serve.cuh"
 
 namespace qcfg {
 
@@ -770,6 +771,71 @@ using namespace qcfg;
 struct qcfg_ctx { Ctx c; };
 struct qcfg_model { Model m; };
 
+namespace {
+
+// Makes the context's device current for a call and puts the caller's back.
+struct DeviceScope {
+  int back = -1;
+  bool ok = true;
+  explicit DeviceScope(Ctx* c) {
+    int cur = -1;
+    ok = cudaGetDevice(&cur) == cudaSuccess;
+    if (ok && cur != device_of(c)) {
+      ok = cudaSetDevice(device_of(c)) == cudaSuccess;
+      if (ok) back = cur;
+    }
+    if (!ok) (void)cudaGetLastError();
+  }
+  ~DeviceScope() { if (back >= 0) (void)cudaSetDevice(back); }
+};
+
+bool dtype_ok(int t) { return t >= QCFG_FP32 && t <= QCFG_FP16; }
+int dtype_size(int t) { return t == QCFG_FP32 ? 4 : 2; }
+
+int check_pool(Ctx* c, const char* who, const qcfg_kv_pool* p) {
+  if (!p || !p->table_dev || !p->len_dev || !p->refs_dev) return set_error(c, QCFG_EINVAL, "%s: null pool", who);
+  if (p->page_tokens != 16 && p->page_tokens != 32 && p->page_tokens != 64 && p->page_tokens != 128)
+    return set_error(c, QCFG_ESHAPE, "%s: page_tokens must be 16, 32, 64 or 128, got %d", who, p->page_tokens);
+  if (p->n_pages < 1 || p->max_seqs < 1 || p->max_pages < 1 || (int64_t)p->max_pages * p->page_tokens > 0x7fffffff - 256)
+    return set_error(c, QCFG_ESHAPE, "%s: bad pool sizes", who);
+  if ((uintptr_t)p->table_dev % 4 || (uintptr_t)p->len_dev % 4 || (uintptr_t)p->refs_dev % 4)
+    return set_error(c, QCFG_EALIGN, "%s: pool arrays must be 4-byte aligned", who);
+  return QCFG_OK;
+}
+int check_cache(Ctx* c, const char* who, const qcfg_kv_cache* k) {
+  if (!k || !k->k_dev || !k->v_dev || !k->k_absmax_dev || !k->v_absmax_dev) return set_error(c, QCFG_EINVAL, "%s: null cache", who);
+  if (k->kv_heads < 1 || k->kv_heads > 4096 || k->head_dim < 16 || k->head_dim > 256 || k->head_dim % 16)
+    return set_error(c, QCFG_ESHAPE, "%s: kv_heads must be 1..4096 and head_dim a multiple of 16 up to 256", who);
+  if ((uintptr_t)k->k_dev % 16 || (uintptr_t)k->v_dev % 16 || (uintptr_t)k->k_absmax_dev % 4 || (uintptr_t)k->v_absmax_dev % 4)
+    return set_error(c, QCFG_EALIGN, "%s: cache must be 16-byte aligned", who);
+  return QCFG_OK;
+}
+int check_batch(Ctx* c, const char* who, const qcfg_kv_batch* b) {
+  if (!b || (b->n > 0 && !b->seqs_dev) || b->n < 0 || b->n_rows < 0) return set_error(c, QCFG_EINVAL, "%s: null batch or negative count", who);
+  if (b->n_rows > 0x7fffffff - 4096 || b->n > (1 << 20)) return set_error(c, QCFG_ESHAPE, "%s: batch too large", who);
+  if (!b->starts_dev && b->n_rows < b->n) return set_error(c, QCFG_ESHAPE, "%s: fewer rows than entries", who);
+  if ((uintptr_t)b->seqs_dev % 4 || (uintptr_t)b->starts_dev % 4) return set_error(c, QCFG_EALIGN, "%s: batch arrays must be 4-byte aligned", who);
+  return QCFG_OK;
+}
+PoolView view(const qcfg_kv_pool* p) { return {p->table_dev, p->len_dev, p->refs_dev, p->n_pages, p->page_tokens, p->max_seqs, p->max_pages}; }
+CacheView view(const qcfg_kv_cache* k) { return {k->k_dev, k->v_dev, k->k_absmax_dev, k->v_absmax_dev, k->kv_heads, k->head_dim}; }
+BatchView view(const qcfg_kv_batch* b) { return {b->seqs_dev, b->starts_dev, b->n, b->n_rows}; }
+
+int check_token_gemm(Ctx* c, const char* who, const void* qw, int64_t ldw, int64_t m, int64_t n, int64_t k, const float* sw, const float* bias, int act,
+                     const void* y, int dtype, int64_t ldy) {
+  if (!qw || !sw || (m > 0 && !y)) return set_error(c, QCFG_EINVAL, "%s: null pointer", who);
+  if (act < QCFG_ACT_NONE || act > QCFG_ACT_GELU_TANH) return set_error(c, QCFG_EINVAL, "%s: bad activation", who);
+  if (!dtype_ok(dtype)) return set_error(c, QCFG_EINVAL, "%s: bad element type", who);
+  if (m < 0 || n <= 0 || k <= 0 || m > 0x7fffffff || n > 0x7fffffff || k > 131072)
+    return set_error(c, QCFG_ESHAPE, "%s: n and k must be positive, k at most 131072 (int32 sums)", who);
+  if (ldw < k || ldy < n) return set_error(c, QCFG_ESHAPE, "%s: leading dimension too small", who);
+  if ((uintptr_t)qw % 16 || ldw % 16) return set_error(c, QCFG_EALIGN, "%s: weight codes need 16-byte aligned pointers and rows", who);
+  if ((uintptr_t)y % dtype_size(dtype) || (uintptr_t)sw % 4 || (uintptr_t)bias % 4) return set_error(c, QCFG_EALIGN, "%s: pointer not aligned to its elements", who);
+  return QCFG_OK;
+}
+
+}  // namespace
+
 extern "C" {
 
 int qcfg_create(qcfg_ctx** out, int device) {
@@ -825,6 +891,7 @@ int qcfg_sync_status(qcfg_ctx* ctx, void* stream) {
     gemm_chain_reset(c);
     if (w & ERR_TIMEOUT) return set_error(c, QCFG_ETIMEOUT, "a bounded device-side wait gave up");
     if (w & ERR_NONFINITE) return set_error(c, QCFG_ENONFINITE, "non-finite value found on the device");
+    if (w & ERR_PAGE) return set_error(c, QCFG_EPAGE, "cache: a number out of range, too few free pages, or a sequence listed twice");
   }
   return QCFG_OK;
 }
@@ -1028,6 +1095,200 @@ int qcfg_gemm_bf16(qcfg_ctx* ctx, const void* x_bf16_dev, int64_t ldx, const voi
   g.a = x_bf16_dev; g.lda = ldx; g.b = w_bf16_dev; g.ldb = ldw; g.m = m; g.n = n; g.k = k;
   g.is_bf16 = 1; g.act = act; g.y = y_dev; g.ldy = n;
   return launch_gemm(c, g, (cudaStream_t)stream);
+}
+
+// ---- serving at 8 bits ----------------------------------------------------------------------
+
+int qcfg_quantize_tokens(qcfg_ctx* ctx, const void* x_dev, int dtype, int64_t rows, int64_t cols, int64_t ld, int bits, int8_t* q_dev,
+                         int64_t ldq, float* scale_dev, void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  if (rows < 0 || cols <= 0 || (rows > 0 && (!x_dev || !q_dev || !scale_dev))) return set_error(c, QCFG_EINVAL, "quantize_tokens: null pointer or bad size");
+  if (!dtype_ok(dtype)) return set_error(c, QCFG_EINVAL, "quantize_tokens: bad element type");
+  if (!bits_int(bits)) return set_error(c, QCFG_EBITS, "quantize_tokens: bits must be 2..8, got %d", bits);
+  if (ld < cols || ldq < cols || rows > 0x7fffffff) return set_error(c, QCFG_ESHAPE, "quantize_tokens: leading dimension below cols or too many rows");
+  if (ldq % 16 || (uintptr_t)q_dev % 16 || (uintptr_t)x_dev % dtype_size(dtype) || (uintptr_t)scale_dev % 4)
+    return set_error(c, QCFG_EALIGN, "quantize_tokens: q_dev must be 16-byte aligned with ldq a multiple of 16, x_dev aligned to its elements");
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "quantize_tokens: device not available");
+  return launch_quantize_tokens(c, x_dev, dtype, rows, cols, ld, bits, q_dev, ldq, scale_dev, (cudaStream_t)stream);
+}
+
+int qcfg_gemm_i8_token(qcfg_ctx* ctx, const int8_t* qx_dev, int64_t ldx, const int8_t* qw_dev, int64_t ldw, int64_t m, int64_t n, int64_t k,
+                       const float* scale_x_dev, const float* scale_w_dev, const float* bias_dev, int act, void* y_dev, int dtype,
+                       int64_t ldy, void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_token_gemm(c, "gemm_i8_token", qw_dev, ldw, m, n, k, scale_w_dev, bias_dev, act, y_dev, dtype, ldy);
+  if (rc) return rc;
+  if (m > 0 && (!qx_dev || !scale_x_dev)) return set_error(c, QCFG_EINVAL, "gemm_i8_token: null pointer");
+  if (ldx < k) return set_error(c, QCFG_ESHAPE, "gemm_i8_token: leading dimension too small");
+  if ((uintptr_t)qx_dev % 16 || ldx % 16 || (uintptr_t)scale_x_dev % 4) return set_error(c, QCFG_EALIGN, "gemm_i8_token: codes need 16-byte aligned pointers and rows");
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "gemm_i8_token: device not available");
+  if (m == 0) return QCFG_OK;
+  const TokenGemm t{qx_dev, ldx, qw_dev, ldw, m, n, k, scale_x_dev, scale_w_dev, bias_dev, act, y_dev, dtype, ldy};
+  return launch_gemm_token(c, t, (cudaStream_t)stream);
+}
+
+int64_t qcfg_linear_i8_work(int64_t m, int64_t k) { return m <= 0 || k <= 0 ? 0 : linear_work(m, k); }
+
+int qcfg_linear_i8(qcfg_ctx* ctx, const void* x_dev, int x_dtype, int64_t ldx, int bits, const int8_t* qw_dev, int64_t ldw, int64_t m, int64_t n,
+                   int64_t k, const float* scale_w_dev, const float* bias_dev, int act, void* y_dev, int y_dtype, int64_t ldy, void* work_dev,
+                   int64_t work_bytes, void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_token_gemm(c, "linear_i8", qw_dev, ldw, m, n, k, scale_w_dev, bias_dev, act, y_dev, y_dtype, ldy);
+  if (rc) return rc;
+  if (m > 0 && !x_dev) return set_error(c, QCFG_EINVAL, "linear_i8: null pointer");
+  if (!dtype_ok(x_dtype)) return set_error(c, QCFG_EINVAL, "linear_i8: bad element type");
+  if (!bits_int(bits)) return set_error(c, QCFG_EBITS, "linear_i8: bits must be 2..8, got %d", bits);
+  if (ldx < k) return set_error(c, QCFG_ESHAPE, "linear_i8: leading dimension too small");
+  if ((uintptr_t)x_dev % dtype_size(x_dtype)) return set_error(c, QCFG_EALIGN, "linear_i8: x_dev must be aligned to its elements");
+  const int64_t need = qcfg_linear_i8_work(m, k);
+  if (need > 0 && (!work_dev || work_bytes < need)) return set_error(c, QCFG_EINVAL, "linear_i8: %lld bytes of working memory needed", (long long)need);
+  if (need > 0 && (uintptr_t)work_dev % 256) return set_error(c, QCFG_EALIGN, "linear_i8: working memory must be 256-byte aligned");
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "linear_i8: device not available");
+  if (m == 0) return QCFG_OK;
+  const TokenGemm t{nullptr, 0, qw_dev, ldw, m, n, k, nullptr, scale_w_dev, bias_dev, act, y_dev, y_dtype, ldy};
+  return launch_linear(c, x_dev, x_dtype, ldx, bits, t, work_dev, (cudaStream_t)stream);
+}
+
+int qcfg_kv_extend(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_batch* batch, void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_pool(c, "kv_extend", pool);
+  if (!rc) rc = check_batch(c, "kv_extend", batch);
+  if (rc) return rc;
+  if (batch->n > kPlanMost) return set_error(c, QCFG_ESHAPE, "kv_extend: at most %d entries", kPlanMost);
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "kv_extend: device not available");
+  return launch_kv_extend(c, view(pool), view(batch), (cudaStream_t)stream);
+}
+
+int qcfg_kv_free(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const int32_t* seqs_dev, int32_t n, void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_pool(c, "kv_free", pool);
+  if (rc) return rc;
+  if (n < 0 || (n > 0 && !seqs_dev)) return set_error(c, QCFG_EINVAL, "kv_free: null pointer or negative count");
+  if ((uintptr_t)seqs_dev % 4) return set_error(c, QCFG_EALIGN, "kv_free: seqs_dev must be 4-byte aligned");
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "kv_free: device not available");
+  return launch_kv_free(c, view(pool), seqs_dev, n, (cudaStream_t)stream);
+}
+
+int qcfg_kv_fork(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const int32_t* parents_dev, const int32_t* children_dev, int32_t n, int32_t* src_dev,
+                 int32_t* dst_dev, void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_pool(c, "kv_fork", pool);
+  if (rc) return rc;
+  if (n < 0 || (n > 0 && (!parents_dev || !children_dev || !src_dev || !dst_dev))) return set_error(c, QCFG_EINVAL, "kv_fork: null pointer or negative count");
+  if (n > kPlanMost) return set_error(c, QCFG_ESHAPE, "kv_fork: at most %d entries", kPlanMost);
+  if ((uintptr_t)parents_dev % 4 || (uintptr_t)children_dev % 4 || (uintptr_t)src_dev % 4 || (uintptr_t)dst_dev % 4)
+    return set_error(c, QCFG_EALIGN, "kv_fork: arrays must be 4-byte aligned");
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "kv_fork: device not available");
+  return launch_kv_fork(c, view(pool), parents_dev, children_dev, n, src_dev, dst_dev, (cudaStream_t)stream);
+}
+
+int qcfg_kv_compact(qcfg_ctx* ctx, const qcfg_kv_pool* pool, int32_t* map_dev, void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_pool(c, "kv_compact", pool);
+  if (rc) return rc;
+  if (!map_dev) return set_error(c, QCFG_EINVAL, "kv_compact: null pointer");
+  if ((uintptr_t)map_dev % 4) return set_error(c, QCFG_EALIGN, "kv_compact: map_dev must be 4-byte aligned");
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "kv_compact: device not available");
+  return launch_kv_compact(c, view(pool), map_dev, (cudaStream_t)stream);
+}
+
+int qcfg_kv_copy_pages(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const int32_t* src_dev, const int32_t* dst_dev, int32_t n,
+                       void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_pool(c, "kv_copy_pages", pool);
+  if (!rc) rc = check_cache(c, "kv_copy_pages", cache);
+  if (rc) return rc;
+  if (n < 0 || (n > 0 && !dst_dev)) return set_error(c, QCFG_EINVAL, "kv_copy_pages: null pointer or negative count");
+  if (!src_dev && n > pool->n_pages) return set_error(c, QCFG_ESHAPE, "kv_copy_pages: more entries than pages");
+  if ((uintptr_t)src_dev % 4 || (uintptr_t)dst_dev % 4) return set_error(c, QCFG_EALIGN, "kv_copy_pages: arrays must be 4-byte aligned");
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "kv_copy_pages: device not available");
+  return launch_kv_copy(c, view(pool), view(cache), src_dev, dst_dev, n, (cudaStream_t)stream);
+}
+
+int qcfg_kv_append(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch, const void* k_dev,
+                   const void* v_dev, int dtype, int64_t row_stride, int64_t head_stride, void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_pool(c, "kv_append", pool);
+  if (!rc) rc = check_cache(c, "kv_append", cache);
+  if (!rc) rc = check_batch(c, "kv_append", batch);
+  if (rc) return rc;
+  if (!dtype_ok(dtype)) return set_error(c, QCFG_EINVAL, "kv_append: bad element type");
+  if (batch->n_rows > 0 && batch->n > 0 && (!k_dev || !v_dev)) return set_error(c, QCFG_EINVAL, "kv_append: null pointer");
+  const int64_t es = dtype_size(dtype);
+  if ((uintptr_t)k_dev % 16 || (uintptr_t)v_dev % 16 || (row_stride * es) % 16 || (head_stride * es) % 16)
+    return set_error(c, QCFG_EALIGN, "kv_append: pointers and strides must be multiples of 16 bytes");
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "kv_append: device not available");
+  return launch_kv_append(c, view(pool), view(cache), view(batch), k_dev, v_dev, dtype, row_stride, head_stride, (cudaStream_t)stream);
+}
+
+int qcfg_kv_read(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch, const int32_t* first_dev, void* k_dev,
+                 void* v_dev, int dtype, void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_pool(c, "kv_read", pool);
+  if (!rc) rc = check_cache(c, "kv_read", cache);
+  if (!rc) rc = check_batch(c, "kv_read", batch);
+  if (rc) return rc;
+  if (!dtype_ok(dtype)) return set_error(c, QCFG_EINVAL, "kv_read: bad element type");
+  if (batch->n > 0 && !first_dev) return set_error(c, QCFG_EINVAL, "kv_read: null pointer");
+  if ((uintptr_t)k_dev % 16 || (uintptr_t)v_dev % 16 || (uintptr_t)first_dev % 4) return set_error(c, QCFG_EALIGN, "kv_read: outputs must be 16-byte aligned");
+  if (!k_dev && !v_dev) return QCFG_OK;
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "kv_read: device not available");
+  return launch_kv_read(c, view(pool), view(cache), view(batch), first_dev, k_dev, v_dev, dtype, (cudaStream_t)stream);
+}
+
+int64_t qcfg_kv_attention_work(qcfg_ctx* ctx, const qcfg_kv_cache* cache, int32_t n, int64_t n_rows, int32_t q_heads) {
+  if (!ctx || !cache || n <= 0 || n_rows <= 0 || q_heads <= 0) return 0;
+  return kv_attention_work(&ctx->c, view(cache), n, n_rows, q_heads);
+}
+
+int qcfg_kv_attention(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch, const void* q_dev,
+                      int64_t q_row_stride, int64_t q_head_stride, int32_t q_heads, void* out_dev, int64_t out_row_stride, int64_t out_head_stride,
+                      int dtype, int32_t max_rows, int32_t max_len, float sm_scale, int causal, int32_t window, void* work_dev, int64_t work_bytes,
+                      void* stream) {
+  if (!ctx) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  int rc = check_pool(c, "kv_attention", pool);
+  if (!rc) rc = check_cache(c, "kv_attention", cache);
+  if (!rc) rc = check_batch(c, "kv_attention", batch);
+  if (rc) return rc;
+  if (!dtype_ok(dtype)) return set_error(c, QCFG_EINVAL, "kv_attention: bad element type");
+  if (batch->n_rows > 0 && batch->n > 0 && (!q_dev || !out_dev)) return set_error(c, QCFG_EINVAL, "kv_attention: null pointer");
+  if (q_heads < 1 || q_heads % cache->kv_heads) return set_error(c, QCFG_ESHAPE, "kv_attention: q_heads must be a multiple of kv_heads");
+  if (q_heads > 65535) return set_error(c, QCFG_ESHAPE, "kv_attention: too many heads");
+  if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return set_error(c, QCFG_EINVAL, "kv_attention: sm_scale must be positive and finite");
+  if (window < 0 || (window > 0 && !causal)) return set_error(c, QCFG_EINVAL, "kv_attention: a window needs causal attention");
+  if (max_rows < 0 || max_len < 0) return set_error(c, QCFG_EINVAL, "kv_attention: negative hint");
+  const int64_t es = dtype_size(dtype);
+  if ((uintptr_t)q_dev % 16 || (uintptr_t)out_dev % 16 || (q_row_stride * es) % 16 || (q_head_stride * es) % 16 || (out_row_stride * es) % 16 ||
+      (out_head_stride * es) % 16)
+    return set_error(c, QCFG_EALIGN, "kv_attention: pointers and strides must be multiples of 16 bytes");
+  const int64_t need = qcfg_kv_attention_work(ctx, cache, batch->n, batch->n_rows, q_heads);
+  if (need > 0 && (!work_dev || work_bytes < need)) return set_error(c, QCFG_EINVAL, "kv_attention: %lld bytes of working memory needed", (long long)need);
+  if (need > 0 && (uintptr_t)work_dev % 256) return set_error(c, QCFG_EALIGN, "kv_attention: working memory must be 256-byte aligned");
+  DeviceScope dev(c);
+  if (!dev.ok) return set_error(c, QCFG_ECUDA, "kv_attention: device not available");
+  return launch_kv_attention(c, view(pool), view(cache), view(batch), q_dev, q_row_stride, q_head_stride, q_heads, out_dev, out_row_stride,
+                             out_head_stride, dtype, max_rows, max_len, sm_scale, causal ? 1 : 0, window, work_dev, (cudaStream_t)stream);
 }
 
 int qcfg_model_create(qcfg_ctx* ctx, const qcfg_layer* layers, int32_t n_layers, qcfg_model** out) {

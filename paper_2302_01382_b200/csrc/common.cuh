@@ -10,7 +10,7 @@
 namespace qcfg {
 
 // Device error word bits (ORed into the context's error word by kernels).
-enum : unsigned { ERR_TIMEOUT = 1u, ERR_NONFINITE = 2u };
+enum : unsigned { ERR_TIMEOUT = 1u, ERR_NONFINITE = 2u, ERR_PAGE = 4u };
 
 struct Ctx;  // defined in api.cu
 

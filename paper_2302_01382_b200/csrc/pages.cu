@@ -1,0 +1,521 @@
+// The paged 8-bit key/value cache: sequences take, share, give back and move pages (integers only, on the device, so that a
+// captured step can run them), and keys and values are written to pages and read back.
+//
+// A page of a head is quantized with one maximum (Eq. 1 at b = 8 over page_tokens x head_dim values).
+#include <cooperative_groups.h>
+
+#include "serve.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace qcfg {
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanCluster = 8;          // CTAs of the calls that walk whole tables
+constexpr unsigned kMark = 0x80000000u;  // a length whose sequence a running call has claimed
+
+__device__ __forceinline__ int pages_for(int64_t tokens, int page) { return (int)((tokens + page - 1) / page); }
+
+// Hands the lowest free pages out: page of rank r (0 .. total-1) goes to take(r, page).  One block.  False: fewer than `total`
+// are free, nothing has been taken.  Two walks over the counts, each ending as soon as it has seen enough.
+template <typename Take>
+__device__ bool take_pages(const PoolView& p, int total, int* buf, Take take) {
+  if (total == 0) return true;
+  for (int pass = 0; pass < 2; ++pass) {
+    int seen = 0;
+    for (int p0 = 0; p0 < p.n_pages && seen < total; p0 += 4 * kPlanThreads) {
+      const int at = p0 + 4 * threadIdx.x;
+      unsigned free = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (at + j < p.n_pages && p.refs[at + j] == 0) free |= 1u << j;
+      int sum;
+      int rank = seen + block_scan(__popc(free), buf, sum);
+      if (pass)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if ((free >> j & 1u) && rank < total) take(rank++, at + j);
+      seen += sum;
+    }
+    if (seen < total) return false;
+    __syncthreads();
+  }
+  return true;
+}
+
+// Exclusive prefix sums of need[0..n) in place, returns the total.  One block.
+__device__ int scan_needs(int* need, int n, int* buf) {
+  int base = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    int sum;
+    const int before = block_scan(i < n ? need[i] : 0, buf, sum);
+    if (i < n) need[i] = base + before;
+    base += sum;
+  }
+  __syncthreads();
+  return base;
+}
+// The last i with first[i] <= r (first ascends; entries without pages share a value with the next)
+__device__ __forceinline__ int owner_of(const int* first, int n, int r) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= r) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Sequences get longer.  One block: a decoding step asks for a page now and then, and most calls end before the walk.
+__global__ void __launch_bounds__(kPlanThreads) kv_extend_kernel(PoolView p, BatchView b, unsigned* err) {
+  pdl_entry();
+  extern __shared__ int sh[];
+  int* need = sh;                  // [n] pages wanted, then their prefix sums
+  int* grown = sh + b.n;           // [n] new length; -1: not claimed by this entry
+  __shared__ int buf[33], bad;
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < b.n; i += kPlanThreads) {
+    int64_t lo, hi;
+    entry_rows(b, i, lo, hi);
+    const int s = b.seqs[i];
+    need[i] = 0;
+    grown[i] = -1;
+    if (s >= p.max_seqs) bad = 1;
+    if (s < 0 || s >= p.max_seqs) continue;
+    const int old = (int)atomicOr(reinterpret_cast<unsigned*>(p.len) + s, kMark);
+    if (old < 0) { bad = 1; continue; }
+    const int64_t len = old + (hi - lo);
+    if (len > (int64_t)p.max_pages * p.page) bad = 1;
+    else need[i] = pages_for(len, p.page) - pages_for(old, p.page);
+    grown[i] = len > 0x7fffffff ? old : (int)len;
+  }
+  __syncthreads();
+  const int total = scan_needs(need, b.n, buf);
+  bool ok = bad == 0;
+  if (ok)
+    ok = take_pages(p, total, buf, [&](int rank, int page) {
+      const int i = owner_of(need, b.n, rank), s = b.seqs[i];
+      const int old = (int)((unsigned)p.len[s] & ~kMark);
+      p.table[(int64_t)s * p.max_pages + pages_for(old, p.page) + rank - need[i]] = page;
+      p.refs[page] = 1;
+    });
+  __syncthreads();
+  for (int i = threadIdx.x; i < b.n; i += kPlanThreads) {
+    if (grown[i] < 0) continue;
+    int* len = p.len + b.seqs[i];
+    *len = ok ? grown[i] : (int)((unsigned)*len & ~kMark);
+  }
+  if (!ok && threadIdx.x == 0) atomicOr(err, ERR_PAGE);
+}
+
+// Gives pages back: a table entry counts for the block that takes it out, so a sequence listed twice loses its pages once.
+__global__ void __launch_bounds__(128) kv_free_kernel(PoolView p, const int32_t* seqs, unsigned* err) {
+  pdl_entry();
+  const int s = seqs[blockIdx.x];
+  if (s >= p.max_seqs && threadIdx.x == 0) atomicOr(err, ERR_PAGE);
+  if (s < 0 || s >= p.max_seqs) return;
+  int* row = p.table + (int64_t)s * p.max_pages;
+  for (int j = threadIdx.x; j < p.max_pages; j += 128) {
+    if (row[j] == -1) continue;
+    const int page = atomicExch(row + j, -1);
+    if (page >= 0 && page < p.n_pages) atomicSub(p.refs + page, 1);
+    else if (page != -1) atomicOr(err, ERR_PAGE);
+  }
+  if (threadIdx.x == 0) p.len[s] = 0;
+}
+
+// One cluster: its first block checks the forks and takes their pages, then all blocks copy the table rows, a warp each.
+__global__ void __cluster_dims__(kPlanCluster, 1, 1) __launch_bounds__(kPlanThreads)
+kv_fork_kernel(PoolView p, const int32_t* parents, const int32_t* children, int n, int32_t* src, int32_t* dst, unsigned* err) {
+  pdl_entry();
+  extern __shared__ int sh[];
+  int* need = sh;                  // [n]
+  int* length = sh + n;            // [n] the parent's length; -1: nothing to do
+  __shared__ int buf[33], bad;
+  cg::cluster_group cluster = cg::this_cluster();
+  if (cluster.block_rank() == 0) {
+    if (threadIdx.x == 0) bad = 0;
+    __syncthreads();
+    for (int f = threadIdx.x; f < n; f += kPlanThreads) {
+      const int from = parents[f], to = children[f];
+      need[f] = 0;
+      length[f] = -1;
+      src[f] = -1;
+      dst[f] = -1;
+      if (to >= p.max_seqs || (to >= 0 && (from < 0 || from >= p.max_seqs))) { bad = 1; continue; }
+      if (to < 0) continue;
+      // a child holds nothing and no other entry has claimed it
+      if (atomicCAS(reinterpret_cast<unsigned*>(p.len) + to, 0u, kMark) != 0u) { bad = 1; continue; }
+      const int len = (int)((unsigned)p.len[from] & ~kMark);
+      if (len > (int64_t)p.max_pages * p.page) { bad = 1; length[f] = 0; continue; }
+      length[f] = len;
+      need[f] = len % p.page != 0;
+    }
+    __syncthreads();
+    const int total = scan_needs(need, n, buf);
+    bool ok = bad == 0;
+    if (ok)
+      ok = take_pages(p, total, buf, [&](int rank, int page) {
+        const int f = owner_of(need, n, rank), full = length[f] / p.page;
+        src[f] = p.table[(int64_t)parents[f] * p.max_pages + full];
+        dst[f] = page;
+        p.table[(int64_t)children[f] * p.max_pages + full] = page;
+        p.refs[page] = 1;
+      });
+    if (threadIdx.x == 0) {
+      bad = !ok;
+      if (!ok) atomicOr(err, ERR_PAGE);
+    }
+  }
+  cluster.sync();
+  const int failed = *cluster.map_shared_rank(&bad, 0);
+  const int* lengths = cluster.map_shared_rank(length, 0);
+  const int lane = threadIdx.x & 31;
+  // claims were made on lengths of 0; a failed entry that claimed nothing has length -1 and is not touched
+  for (int f = cluster.block_rank() * (kPlanThreads / 32) + (threadIdx.x >> 5); f < n; f += kPlanCluster * (kPlanThreads / 32)) {
+    const int len = lengths[f];
+    if (len < 0) continue;
+    const int32_t* from = p.table + (int64_t)parents[f] * p.max_pages;
+    int32_t* to = p.table + (int64_t)children[f] * p.max_pages;
+    if (!failed)
+      for (int j = lane; j < len / p.page; j += 32) {
+        const int page = from[j];
+        to[j] = page;
+        if (page >= 0 && page < p.n_pages) atomicAdd(p.refs + page, 1);
+        else atomicOr(err, ERR_PAGE);
+      }
+    if (lane == 0) p.len[children[f]] = failed ? 0 : len;
+  }
+  cluster.sync();                  // the first block's shared memory has been read
+}
+
+// Live pages move down.  One cluster; block r walks the slice [r * slice, ...) of the counts.
+__global__ void __cluster_dims__(kPlanCluster, 1, 1) __launch_bounds__(kPlanThreads)
+kv_compact_kernel(PoolView p, int32_t* map, unsigned* err) {
+  pdl_entry();
+  int32_t* hole_list = map + p.n_pages;
+  __shared__ int buf[33], live_here, counts[2];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = cluster.block_rank();
+  const int slice = (p.n_pages + kPlanCluster - 1) / kPlanCluster;
+  const int lo = min(rank * slice, p.n_pages), hi = min(lo + slice, p.n_pages);
+  int sum = 0, total;
+  for (int i = lo + threadIdx.x; i < hi; i += kPlanThreads) sum += p.refs[i] > 0;
+  block_scan(sum, buf, total);
+  if (threadIdx.x == 0) live_here = total;
+  cluster.sync();
+  int live = 0;
+  for (int r = 0; r < kPlanCluster; ++r) live += *cluster.map_shared_rank(&live_here, r);
+  // holes below `live` and movers at or above it, per slice and before this one
+  int holes = 0, movers = 0, n_holes, n_movers;
+  for (int i = lo + threadIdx.x; i < hi; i += kPlanThreads) {
+    const bool used = p.refs[i] > 0;
+    holes += !used && i < live;
+    movers += used && i >= live;
+  }
+  block_scan(holes, buf, n_holes);
+  block_scan(movers, buf, n_movers);
+  if (threadIdx.x == 0) { counts[0] = n_holes; counts[1] = n_movers; }
+  cluster.sync();
+  int hole_at = 0, mover_at = 0;
+  for (int r = 0; r < rank; ++r) {
+    const int* c = cluster.map_shared_rank(counts, r);
+    hole_at += c[0];
+    mover_at += c[1];
+  }
+  // the holes in order
+  for (int i0 = lo; i0 < hi; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    const bool hole = i < hi && i < live && p.refs[i] <= 0;
+    const int r = hole_at + block_scan(hole, buf, total);
+    if (hole) hole_list[r] = i;
+    if (i < hi && i < live) map[i] = hole ? -1 : i;
+    hole_at += total;
+  }
+  cluster.sync();
+  // movers take them in order, and counts follow (nobody reads a count below `live` any more)
+  for (int i0 = lo; i0 < hi; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    const int refs = i < hi && i >= live ? p.refs[i] : 0;
+    const int r = mover_at + block_scan(refs > 0, buf, total);
+    if (refs > 0) {
+      const int to = hole_list[r];
+      map[i] = to;
+      p.refs[to] = refs;
+      p.refs[i] = 0;
+    } else if (i < hi && i >= live) {
+      map[i] = -1;
+    }
+    mover_at += total;
+  }
+  cluster.sync();
+  // table rows, a warp each
+  const int lane = threadIdx.x & 31;
+  for (int s = rank * (kPlanThreads / 32) + (threadIdx.x >> 5); s < p.max_seqs; s += kPlanCluster * (kPlanThreads / 32)) {
+    int32_t* row = p.table + (int64_t)s * p.max_pages;
+    const int pages = min(pages_for(max(p.len[s], 0), p.page), p.max_pages);
+    for (int j = lane; j < pages; j += 32) {
+      const int page = row[j];
+      if (page < live) {
+        if (page < 0) atomicOr(err, ERR_PAGE);
+        continue;
+      }
+      if (page >= p.n_pages) { atomicOr(err, ERR_PAGE); continue; }
+      row[j] = map[page];
+    }
+  }
+}
+
+// Page copies: a block moves up to 16 KB of one page's codes, the first block of a page its maxima too.
+constexpr int kCopyThreads = 256;
+constexpr int kCopyBytes = 16384;
+__global__ void __launch_bounds__(kCopyThreads) kv_copy_kernel(CacheView c, int n_pages, int64_t page_bytes, const int32_t* src,
+                                                               const int32_t* dst, unsigned* err) {
+  pdl_entry();
+  const int i = blockIdx.x;
+  const int to = dst[i], from = src ? src[i] : i;
+  if (to < 0 || from < 0 || to == from) return;
+  if (to >= n_pages || from >= n_pages) {
+    if (threadIdx.x == 0) atomicOr(err, ERR_PAGE);
+    return;
+  }
+  const int64_t at = (int64_t)blockIdx.y * kCopyBytes;
+  const int64_t end = min(at + kCopyBytes, page_bytes);
+  int8_t* base = blockIdx.z ? c.v : c.k;
+  const uint4* s = reinterpret_cast<const uint4*>(base + from * page_bytes);
+  uint4* d = reinterpret_cast<uint4*>(base + to * page_bytes);
+  uint4 v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t o = at / 16 + threadIdx.x + j * kCopyThreads;
+    if (o * 16 < end) v[j] = s[o];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t o = at / 16 + threadIdx.x + j * kCopyThreads;
+    if (o * 16 < end) d[o] = v[j];
+  }
+  if (blockIdx.y == 0) {
+    float* a = blockIdx.z ? c.v_absmax : c.k_absmax;
+    for (int h = threadIdx.x; h < c.heads; h += kCopyThreads) a[(int64_t)to * c.heads + h] = a[(int64_t)from * c.heads + h];
+  }
+}
+
+// New keys or values of one page and head.
+constexpr int kAppendThreads = 128;
+template <typename T>
+__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(PoolView p, CacheView c, BatchView b, const T* k, const T* v,
+                                                                   int64_t row_stride, int64_t head_stride, unsigned* err) {
+  pdl_entry();
+  constexpr int V = Vec<T>::N;
+  int64_t first;
+  const int i = entry_of_item(b, blockIdx.x, p.page, b.starts ? 2 : 0, first);
+  if (i < 0 || i >= b.n) return;
+  int64_t lo, hi;
+  entry_rows(b, i, lo, hi);
+  const int s = entry_seq(b, p, i, err);
+  if (s < 0 || hi == lo) return;
+  const int len = seq_len(p, s);
+  const int64_t old = len - (hi - lo);             // tokens before this call
+  if (old < 0) {
+    if (threadIdx.x == 0) atomicOr(err, ERR_PAGE);
+    return;
+  }
+  const int64_t j = old / p.page + (blockIdx.x - first);
+  if (j * p.page >= len) return;
+  int twice = 0;
+  for (int e = threadIdx.x; e < b.n; e += kAppendThreads) twice |= e != i && b.seqs[e] == s;
+  const int number = p.table[(int64_t)s * p.max_pages + j];
+  const bool valid = number >= 0 && number < p.n_pages && p.refs[number] == 1;
+  if (__syncthreads_or(twice || !valid)) {
+    if (threadIdx.x == 0) atomicOr(err, ERR_PAGE);
+    return;
+  }
+  const int h = blockIdx.y;
+  const T* x = blockIdx.z ? v : k;
+  int8_t* codes = (blockIdx.z ? c.v : c.k) + ((int64_t)number * c.heads + h) * p.page * c.dim;
+  float* absmax = (blockIdx.z ? c.v_absmax : c.k_absmax) + (int64_t)number * c.heads + h;
+  const int t0 = (int)(max(old, j * p.page) - j * p.page);           // new tokens of the page: [t0, t1)
+  const int t1 = (int)(min((int64_t)len, (j + 1) * p.page) - j * p.page);
+  x += (lo + j * p.page + t0 - old) * row_stride + h * head_stride;
+  const int per_row = c.dim / V, n_vec = (t1 - t0) * per_row;
+  unsigned top = 0, odd = 0;
+  for (int e = threadIdx.x; e < n_vec; e += kAppendThreads) {
+    const int t = e / per_row, d = (e - t * per_row) * V;
+    float f[V];
+    load_vec<T>(x + t * row_stride + d, f);
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      const unsigned a = abs_bits(f[q]);
+      if (a < 0x7f800000u) top = a > top ? a : top; else odd = 1;
+    }
+  }
+  __shared__ unsigned tops[kAppendThreads / 32];
+  top = warp_max_u(top);
+  if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+  const float held = t0 > 0 ? *absmax : 0.0f;
+  if (__syncthreads_or(odd) && threadIdx.x == 0) atomicOr(err, ERR_NONFINITE);
+#pragma unroll
+  for (int w = 0; w < kAppendThreads / 32; ++w) top = tops[w] > top ? tops[w] : top;
+  const float fresh = __uint_as_float(top), now = held > fresh ? held : fresh;
+  const float inv = inv_scale_of(now);
+  for (int e = threadIdx.x; e < n_vec; e += kAppendThreads) {
+    const int t = e / per_row, d = (e - t * per_row) * V;
+    float f[V];
+    load_vec<T>(x + t * row_stride + d, f);
+    union { uint32_t w[V / 4]; int8_t b[V]; } q;
+#pragma unroll
+    for (int g = 0; g < V; ++g) q.b[g] = (int8_t)(finite_bits(f[g]) ? code_of(f[g], inv) : 0);
+    uint32_t* to = reinterpret_cast<uint32_t*>(codes + (t0 + t) * c.dim + d);
+#pragma unroll
+    for (int g = 0; g < V / 4; ++g) to[g] = q.w[g];
+  }
+  if (t0 > 0 && now > held && held > 0.0f) {       // the earlier codes on the new grid
+    const float ratio = __fdiv_rn(held, now);
+    for (int e = threadIdx.x; e < t0 * c.dim / 4; e += kAppendThreads) {
+      char4* at = reinterpret_cast<char4*>(codes) + e;
+      const char4 q = *at;
+      *at = make_char4((signed char)__float2int_rn(q.x * ratio), (signed char)__float2int_rn(q.y * ratio),
+                       (signed char)__float2int_rn(q.z * ratio), (signed char)__float2int_rn(q.w * ratio));
+    }
+  }
+  if (threadIdx.x == 0) *absmax = now;
+}
+
+// Values of cached tokens, a warp for each row.
+constexpr int kReadWarps = 8;
+template <typename T>
+__global__ void __launch_bounds__(32 * kReadWarps) kv_read_kernel(PoolView p, CacheView c, BatchView b, const int32_t* first_tok, T* k,
+                                                                  T* v, unsigned* err) {
+  pdl_entry();
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * kReadWarps + (threadIdx.x >> 5);
+  if (row >= b.rows) return;
+  int i = (int)row;
+  if (b.starts) {
+    int count = 0;
+    for (int e = lane; e < b.n; e += 32) count += b.starts[e] <= row;
+    i = __reduce_add_sync(0xffffffffu, count) - 1;
+  }
+  if (i < 0 || i >= b.n) return;
+  int64_t lo, hi;
+  entry_rows(b, i, lo, hi);
+  if (row >= hi) return;
+  const int s = entry_seq(b, p, i, err);
+  int number = -1;
+  int64_t pos = 0;
+  if (s >= 0) {
+    pos = first_tok[i] + (row - lo);
+    if (pos >= 0 && pos < seq_len(p, s)) {
+      number = p.table[(int64_t)s * p.max_pages + pos / p.page];
+      if (number < 0 || number >= p.n_pages) {
+        if (lane == 0) atomicOr(err, ERR_PAGE);
+        number = -1;
+      }
+    }
+  }
+  const int per_head = c.dim / 4, n_vec = c.heads * per_head;
+  for (int e = lane; e < n_vec; e += 32) {
+    const int h = e / per_head, d = (e - h * per_head) * 4;
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      T* out = z ? v : k;
+      if (!out) continue;
+      union { T t[4]; uint4 w4; uint2 w2; } o;
+      char4 q = make_char4(0, 0, 0, 0);
+      float scale = 0.0f;
+      if (number >= 0) {
+        const int64_t at = (int64_t)number * c.heads + h;
+        q = *reinterpret_cast<const char4*>((z ? c.v : c.k) + (at * p.page + pos % p.page) * c.dim + d);
+        scale = scale_of((z ? c.v_absmax : c.k_absmax)[at]);
+      }
+      o.t[0] = from_float<T>(q.x * scale);
+      o.t[1] = from_float<T>(q.y * scale);
+      o.t[2] = from_float<T>(q.z * scale);
+      o.t[3] = from_float<T>(q.w * scale);
+      T* to = out + (row * c.heads + h) * c.dim + d;
+      if (sizeof(T) == 4) *reinterpret_cast<uint4*>(to) = o.w4;
+      else *reinterpret_cast<uint2*>(to) = o.w2;
+    }
+  }
+}
+
+}  // namespace
+
+int launch_kv_extend(Ctx* ctx, const PoolView& p, const BatchView& b, cudaStream_t st) {
+  if (b.n == 0) return QCFG_OK;
+  const size_t smem = (size_t)b.n * 8;
+  if (smem > 40000) {
+    const cudaError_t e = cudaFuncSetAttribute(kv_extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPlanMost * 8);
+    if (e != cudaSuccess) return check_cuda(ctx, e, "kv_extend");
+  }
+  launch_pdl(kv_extend_kernel, dim3(1), dim3(kPlanThreads), smem, st, p, b, err_word(ctx));
+  count_launch(ctx);
+  return check_cuda(ctx, cudaGetLastError(), "kv_extend");
+}
+int launch_kv_free(Ctx* ctx, const PoolView& p, const int32_t* seqs, int n, cudaStream_t st) {
+  if (n == 0) return QCFG_OK;
+  launch_pdl(kv_free_kernel, dim3(n), dim3(128), 0, st, p, seqs, err_word(ctx));
+  count_launch(ctx);
+  return check_cuda(ctx, cudaGetLastError(), "kv_free");
+}
+int launch_kv_fork(Ctx* ctx, const PoolView& p, const int32_t* parents, const int32_t* children, int n, int32_t* src, int32_t* dst, cudaStream_t st) {
+  if (n == 0) return QCFG_OK;
+  const size_t smem = (size_t)n * 8;
+  if (smem > 40000) {
+    const cudaError_t e = cudaFuncSetAttribute(kv_fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPlanMost * 8);
+    if (e != cudaSuccess) return check_cuda(ctx, e, "kv_fork");
+  }
+  launch_pdl(kv_fork_kernel, dim3(kPlanCluster), dim3(kPlanThreads), smem, st, p, parents, children, n, src, dst, err_word(ctx));
+  count_launch(ctx);
+  return check_cuda(ctx, cudaGetLastError(), "kv_fork");
+}
+int launch_kv_compact(Ctx* ctx, const PoolView& p, int32_t* map, cudaStream_t st) {
+  if (p.n_pages == 0) return QCFG_OK;
+  launch_pdl(kv_compact_kernel, dim3(kPlanCluster), dim3(kPlanThreads), 0, st, p, map, err_word(ctx));
+  count_launch(ctx);
+  return check_cuda(ctx, cudaGetLastError(), "kv_compact");
+}
+int launch_kv_copy(Ctx* ctx, const PoolView& p, const CacheView& c, const int32_t* src, const int32_t* dst, int n, cudaStream_t st) {
+  if (n == 0) return QCFG_OK;
+  const int64_t bytes = (int64_t)c.heads * p.page * c.dim;
+  const dim3 grid(n, (unsigned)((bytes + kCopyBytes - 1) / kCopyBytes), 2);
+  launch_pdl(kv_copy_kernel, grid, dim3(kCopyThreads), 0, st, c, p.n_pages, bytes, src, dst, err_word(ctx));
+  count_launch(ctx);
+  return check_cuda(ctx, cudaGetLastError(), "kv_copy_pages");
+}
+template <typename T>
+static void append_as(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const void* k, const void* v, int64_t row_stride,
+                      int64_t head_stride, cudaStream_t st) {
+  const int64_t items = b.starts ? b.rows / p.page + 2 * (int64_t)b.n : b.n;
+  launch_pdl(kv_append_kernel<T>, dim3((unsigned)items, c.heads, 2), dim3(kAppendThreads), 0, st, p, c, b, (const T*)k, (const T*)v, row_stride,
+             head_stride, err_word(ctx));
+}
+int launch_kv_append(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const void* k, const void* v, int dtype,
+                     int64_t row_stride, int64_t head_stride, cudaStream_t st) {
+  if (b.n == 0 || b.rows == 0) return QCFG_OK;
+  if (dtype == QCFG_FP32) append_as<float>(ctx, p, c, b, k, v, row_stride, head_stride, st);
+  else if (dtype == QCFG_BF16) append_as<__nv_bfloat16>(ctx, p, c, b, k, v, row_stride, head_stride, st);
+  else append_as<__half>(ctx, p, c, b, k, v, row_stride, head_stride, st);
+  count_launch(ctx);
+  return check_cuda(ctx, cudaGetLastError(), "kv_append");
+}
+template <typename T>
+static void read_as(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const int32_t* first, void* k, void* v, cudaStream_t st) {
+  launch_pdl(kv_read_kernel<T>, dim3((unsigned)((b.rows + kReadWarps - 1) / kReadWarps)), dim3(32 * kReadWarps), 0, st, p, c, b, first, (T*)k, (T*)v,
+             err_word(ctx));
+}
+int launch_kv_read(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const int32_t* first, void* k, void* v, int dtype,
+                   cudaStream_t st) {
+  if (b.n == 0 || b.rows == 0) return QCFG_OK;
+  if (dtype == QCFG_FP32) read_as<float>(ctx, p, c, b, first, k, v, st);
+  else if (dtype == QCFG_BF16) read_as<__nv_bfloat16>(ctx, p, c, b, first, k, v, st);
+  else read_as<__half>(ctx, p, c, b, first, k, v, st);
+  count_launch(ctx);
+  return check_cuda(ctx, cudaGetLastError(), "kv_read");
+}
+
+}  // namespace qcfg
