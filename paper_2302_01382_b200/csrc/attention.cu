@@ -33,30 +33,39 @@ __device__ __forceinline__ void seen_range(const AttnArgs& a, int64_t pos, int l
   lo = a.window > 0 && pos + 1 > a.window ? (int)(pos + 1) - a.window : 0;
 }
 
-// ---- few rows: warps stream the cache -----------------------------------------------------------
+// ---- warps stream the cache ------------------------------------------------------------------------
 //
-// Work is counted in units of 64 tokens of one (entry, cache head, tile of 16 rows); a row is a (query token, head of the
-// group).  All units of a call form one sequence that the resident blocks share evenly, so a ragged batch, a single long context and many
-// short ones load the GPU alike.  A block works through its units segment by segment (a segment: units of one tile); a tile cut
-// between blocks leaves its parts in `work`, and a second kernel joins them in a fixed order.
+// Work is counted in units of 64 tokens of one (entry, cache head, tile of rows); a row is a (query token, head of the group).
+// All units of a call form one sequence that the resident blocks share evenly, so a ragged batch, a single long context and many
+// short ones load the GPU alike; a tile counts kSetup units more for what it costs to begin.  A block works through its units
+// segment by segment (a segment: units of one tile); a tile cut between blocks leaves its parts in `work`, and a second
+// kernel joins them in a fixed order.
 // Within a segment each of the four warps takes every fourth run of 32 tokens, with its own ring of stages (cp.async) and its own
 // running maximum: nothing is synchronised until the segment ends.
+//
+// The products are taken the other way round, scores^T = K q^T and out^T += V^T weights^T: then the tokens and the elements fill the 16 rows
+// of an MMA and the query rows its 8 columns, so that a group of up to 8 heads leaves no half of a product unused, and the
+// conversions of codes (1.25 and 1.5 instructions each, what bounds this kernel next to HBM) are shared by all NR column tiles.
+// In the A operand an element of K is (token, dimension), of V^T (dimension, token); the sums run over dimensions and
+// tokens in any order, so both are read 16 bytes at a time as they lie in memory.
 constexpr int kUnit = 64;           // tokens
+constexpr int kSetup = 2;           // units
 constexpr int kRun = 32;            // tokens a warp takes at a time
-constexpr int kRows = 16;           // rows of a tile (M of the MMA)
 constexpr int kStreamWarps = 4;
 constexpr int kMinUnits = 2;        // a block takes at least this many
-constexpr float kWeightBias = 14.0f;
+// Weights are 2^(7 + x - ref).  ref follows the running maximum only when a score passes it by more than 2^8: sums and
+// accumulators are rescaled once or twice in a context and not at every new maximum, and a weight stays below 2^15.
+constexpr float kWeightBias = 7.0f, kWeightMost = 15.0f;
 
-template <int DP> __host__ __device__ constexpr int stream_stages() { return DP == 64 ? 4 : 3; }
 template <int DP> __host__ __device__ constexpr int stage_bytes() { return 2 * kRun * DP + 32; }             // keys, values, four maxima
-template <int DP> __host__ __device__ constexpr int stream_blocks() { return DP == 256 ? 1 : 2; }            // per SM
-template <int DP, bool WIDE> __host__ __device__ constexpr int query_bytes() { return (WIDE ? 2 : 1) * kRows * DP * 2; }
-template <int DP, bool WIDE>
+template <int DP, int NR> __host__ __device__ constexpr int stream_blocks() { return DP == 256 ? 1 : DP == 128 ? (NR == 4 ? 2 : 3) : (NR == 1 ? 4 : 3); }    // per SM
+template <int DP, int NR> __host__ __device__ constexpr int stream_stages() { return DP == 256 ? 3 : DP == 128 ? (NR == 4 ? 3 : 2) : (NR == 1 ? 3 : 4); }
+template <int DP, int NR, bool WIDE> __host__ __device__ constexpr int query_bytes() { return (WIDE ? 2 : 1) * 8 * NR * DP * 2; }
+template <int DP, int NR, bool WIDE>
 __host__ __device__ constexpr int stream_smem() {
-  return query_bytes<DP, WIDE>() + kStreamWarps * stream_stages<DP>() * stage_bytes<DP>();
+  return query_bytes<DP, NR, WIDE>() + kStreamWarps * stream_stages<DP, NR>() * stage_bytes<DP>();
 }
-constexpr int kMaxStreamGrid = 148 * 2;
+constexpr int kMaxStreamGrid = 148 * 4;
 
 struct PartMeta {         // of a block: the cut tile that its first segment finishes
   int64_t row0;           // first row of the entry
@@ -64,7 +73,7 @@ struct PartMeta {         // of a block: the cut tile that its first segment fin
   int rows, tile, head;
   int pad[2];
 };
-template <int DP> __host__ __device__ constexpr int64_t part_floats() { return kRows * DP + 2 * kRows; }     // accumulators, maxima, sums
+template <int DP, int NR> __host__ __device__ constexpr int64_t part_floats() { return 8 * NR * DP + 16 * NR; }     // accumulators, maxima, sums
 
 __device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
 __device__ __forceinline__ uint32_t pack_h2(float a, float b) { return h2_bits(__floats2half2_rn(a, b)); }
@@ -76,6 +85,12 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Transposes an 8 x 8 matrix of 16-bit elements: lane 4 g + t holds elements 2 t and 2 t + 1 of row g before and after
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t o;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(o) : "r"(v));
+  return o;
 }
 // Bytes `lo`, `hi` (selector 0x4H4L) of a word of codes plus 128 as two fp16 codes: 0x6400 + b is 1024 + b
 template <uint32_t SEL>
@@ -116,8 +131,9 @@ __device__ __forceinline__ uint32_t chunk_at(int row, int chunk) {
 // What an entry of the batch asks for.
 struct Entry {
   int64_t row0, rows;
-  int s, len, tiles, units;      // tiles of 16 rows, units per tile and head
+  int s, len, tiles, units;      // tiles of 8 * NR rows, units per tile and head
 };
+template <int NR>
 __device__ __forceinline__ Entry entry_of(const AttnArgs& a, int i) {
   Entry e;
   int64_t hi;
@@ -125,8 +141,8 @@ __device__ __forceinline__ Entry entry_of(const AttnArgs& a, int i) {
   e.rows = hi - e.row0;
   e.s = a.batch.seqs[i];
   e.len = e.s < 0 || e.s >= a.pool.max_seqs ? 0 : seq_len(a.pool, e.s);
-  e.tiles = (int)((e.rows * (a.q_heads / a.cache.heads) + kRows - 1) / kRows);
-  e.units = e.len ? (e.len + kUnit - 1) / kUnit : 1;
+  e.tiles = (int)((e.rows * (a.q_heads / a.cache.heads) + 8 * NR - 1) / (8 * NR));
+  e.units = kSetup + (e.len ? (e.len + kUnit - 1) / kUnit : 1);
   return e;
 }
 __device__ __forceinline__ int64_t entry_units(const AttnArgs& a, const Entry& e) { return (int64_t)e.tiles * e.units * a.cache.heads; }
@@ -138,14 +154,14 @@ __device__ __forceinline__ int share_of(int64_t total, int blocks, int64_t unit)
   return unit < more * (each + 1) ? (int)(unit / (each + 1)) : (int)(more + (unit - more * (each + 1)) / each);
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_attention_stream(const AttnArgs a) {
+template <typename T, int DP, int NR>
+__global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv_attention_stream(const AttnArgs a) {
   pdl_entry();
   constexpr bool WIDE = sizeof(T) == 4;
-  constexpr int ST = stream_stages<DP>(), SB = stage_bytes<DP>(), NT = DP / 8;
+  constexpr int ST = stream_stages<DP, NR>(), SB = stage_bytes<DP>(), MT = DP / 16, ROWS = 8 * NR;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int64_t scan[kStreamWarps], found[2];
-  __shared__ float row_scale[kRows], merge_top[kStreamWarps][kRows], merge_sum[kStreamWarps][kRows];
+  __shared__ float row_scale[ROWS], merge_top[kStreamWarps][ROWS], merge_sum[kStreamWarps][ROWS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   const int group = a.q_heads / a.cache.heads, dim = a.cache.dim, page = a.pool.page;
   PartMeta* meta = reinterpret_cast<PartMeta*>(a.work);
@@ -155,7 +171,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
   int64_t total = 0;
   for (int i0 = 0; i0 < a.batch.n; i0 += 32 * kStreamWarps) {
     const int i = i0 + tid;
-    int64_t u = i < a.batch.n ? entry_units(a, entry_of(a, i)) : 0;
+    int64_t u = i < a.batch.n ? entry_units(a, entry_of<NR>(a, i)) : 0;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
     __syncthreads();
@@ -164,7 +180,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
 #pragma unroll
     for (int w = 0; w < kStreamWarps; ++w) total += scan[w];
   }
-  const int blocks = (int)max((int64_t)1, min((int64_t)gridDim.x, total / kMinUnits));
+  const int blocks = (int)max((int64_t)1, min((int64_t)gridDim.x, total / (kSetup + kMinUnits)));
   const int me = blockIdx.x;
   if (tid == 0) meta[me].first = -1;
   if (me >= blocks || total == 0) return;
@@ -177,7 +193,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
     bool done = false;
     for (int i0 = 0; i0 < a.batch.n && !done; i0 += 32 * kStreamWarps) {
       const int i = i0 + tid;
-      const int64_t u = i < a.batch.n ? entry_units(a, entry_of(a, i)) : 0;
+      const int64_t u = i < a.batch.n ? entry_units(a, entry_of<NR>(a, i)) : 0;
       int64_t s = u;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -200,92 +216,101 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
     entry = (int)found[0];
     entry_at = found[1];
   }
-  Entry E = entry_of(a, entry);
+  Entry E = entry_of<NR>(a, entry);
 
   const uint32_t q_sm = smem_at(smem);
-  const uint32_t ring = q_sm + query_bytes<DP, WIDE>() + warp * ST * SB;
-  float* merged = reinterpret_cast<float*>(smem + query_bytes<DP, WIDE>());     // the ring again, once it is empty
+  const uint32_t ring = q_sm + query_bytes<DP, NR, WIDE>() + warp * ST * SB;
+  float* merged = reinterpret_cast<float*>(smem + query_bytes<DP, NR, WIDE>());     // the ring again, once it is empty
 
   while (at < end) {
     while (at >= entry_at + entry_units(a, E)) {
       entry_at += entry_units(a, E);
-      E = entry_of(a, ++entry);
+      E = entry_of<NR>(a, ++entry);
     }
-    if (tid == 0 && E.s >= a.pool.max_seqs) atomicOr(a.err, ERR_PAGE);
     const int64_t item = (at - entry_at) / E.units;
-    const int u0 = (int)((at - entry_at) % E.units), u1 = (int)min((int64_t)E.units, u0 + (end - at));
+    const int v0 = (int)((at - entry_at) % E.units), v1 = (int)min((int64_t)E.units, v0 + (end - at));
+    const int n_units = E.units - kSetup, u0 = max(v0 - kSetup, 0), u1 = max(v1 - kSetup, 0);
+    at += v1 - v0;
+    if (u1 == 0) continue;                                 // ends before the tile's first token
+    if (tid == 0 && E.s >= a.pool.max_seqs) atomicOr(a.err, ERR_PAGE);
     const int hk = (int)(item / E.tiles), tile = (int)(item % E.tiles);
-    const int64_t r_first = (int64_t)tile * kRows;         // first row of the tile in the entry
-    const int r_count = (int)min((int64_t)kRows, E.rows * group - r_first);
+    const int64_t r_first = (int64_t)tile * ROWS;          // first row of the tile in the entry
+    const int r_count = (int)min((int64_t)ROWS, E.rows * group - r_first);
 
-    // ---- queries: eight threads a row, in the order the MMA's A operand wants
-    {
-      const int r = tid >> 3, part = tid & 7;
-      const int64_t row = (r_first + r) / group;
-      const int head = hk * group + (int)((r_first + r) % group);
-      const T* q = reinterpret_cast<const T*>(a.q) + (E.row0 + row) * a.q_row + head * a.q_head;
-      constexpr int V = Vec<T>::N;
-      float v[DP / 8];
-      unsigned top = 0;
+    // ---- queries, in the order the MMA's B operand wants: eight threads a row
 #pragma unroll
-      for (int c = 0; c < DP / 8 / V; ++c) {
-        float f[V];
-        const int d = (c * 8 + part) * V;
-        if (r < r_count && d < dim) load_vec<T>(q + d, f);
-        else {
+    for (int r0 = 0; r0 < ROWS; r0 += 16) {
+      const int r = r0 + (tid >> 3), part = tid & 7;
+      if (ROWS >= 16 || r < ROWS) {
+        const int64_t row = (r_first + r) / group;
+        const int head = hk * group + (int)((r_first + r) % group);
+        const T* q = reinterpret_cast<const T*>(a.q) + (E.row0 + row) * a.q_row + head * a.q_head;
+        constexpr int V = Vec<T>::N;
+        float v[DP / 8];
+        unsigned top = 0;
 #pragma unroll
-          for (int j = 0; j < V; ++j) f[j] = 0.0f;
+        for (int c = 0; c < DP / 8 / V; ++c) {
+          float f[V];
+          const int d = (c * 8 + part) * V;
+          if (r < r_count && d < dim) load_vec<T>(q + d, f);
+          else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[j] = 0.0f;
+          }
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            v[c * V + j] = f[j];
+            const unsigned b = abs_bits(f[j]);
+            top = b > top ? b : top;
+          }
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          v[c * V + j] = f[j];
-          const unsigned b = abs_bits(f[j]);
+        for (int o = 1; o < 8; o <<= 1) {
+          const unsigned b = __shfl_xor_sync(__activemask(), top, o);
           top = b > top ? b : top;
         }
+        // 2^(12 - exponent of the largest): its inverse goes into the row's factor
+        int shift = 12 - ((int)(top >> 23) - 127);
+        if (top == 0 || top >= 0x7f800000u) shift = 0;
+        shift = shift > 120 ? 120 : shift;
+        const float up = __uint_as_float((unsigned)(127 + shift) << 23);
+#pragma unroll
+        for (int c = 0; c < DP / 8 / V; ++c)
+#pragma unroll
+          for (int j = 0; j < V; j += 2) {
+            const int d = (c * 8 + part) * V + j;
+            const int ln = (r & 7) * 4 + ((d & 63) >> 4), step = (d & 15) >> 2, reg = (step & 1) * 2 + ((d & 3) >> 1);
+            const uint32_t to = q_sm + (((((r >> 3) * (DP / 64) + (d >> 6)) * 2 + (step >> 1)) * 32 + ln) * 4 + reg) * 4;
+            const float x = v[c * V + j] * up, y = v[c * V + j + 1] * up;
+            const __half2 hi = __floats2half2_rn(x, y);
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(h2_bits(hi)) : "memory");
+            if (WIDE)
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + ROWS * DP * 2),
+                           "r"(pack_h2(x - __low2float(hi), y - __high2float(hi))) : "memory");
+          }
+        if (part == 0) row_scale[r] = a.scale * __uint_as_float((unsigned)(127 - shift) << 23);
       }
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) {
-        const unsigned b = __shfl_xor_sync(0xffffffffu, top, o);
-        top = b > top ? b : top;
-      }
-      // 2^(12 - exponent of the largest): its inverse goes into the row's factor
-      int shift = 12 - ((int)(top >> 23) - 127);
-      if (top == 0 || top >= 0x7f800000u) shift = 0;
-      shift = shift > 120 ? 120 : shift;
-      const float up = __uint_as_float((unsigned)(127 + shift) << 23);
-#pragma unroll
-      for (int c = 0; c < DP / 8 / V; ++c)
-#pragma unroll
-        for (int j = 0; j < V; j += 2) {
-          const int d = (c * 8 + part) * V + j;
-          const int step = (d >> 6) * 4 + ((d & 15) >> 2), ln = (r & 7) * 4 + ((d & 63) >> 4), reg = (r >> 3) + (d & 2);
-          const uint32_t to = q_sm + ((step * 32 + ln) * 4 + reg) * 4;
-          const float x = v[c * V + j] * up, y = v[c * V + j + 1] * up;
-          const __half2 hi = __floats2half2_rn(x, y);
-          asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(h2_bits(hi)) : "memory");
-          if (WIDE)
-            asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + kRows * DP * 2),
-                         "r"(pack_h2(x - __low2float(hi), y - __high2float(hi))) : "memory");
-        }
-      if (part == 0) row_scale[r] = a.scale * __uint_as_float((unsigned)(127 - shift) << 23);
     }
     __syncthreads();
 
-    // ---- what this thread's two rows see, and what all rows do
-    int lo[2], hi[2], all_lo = 0, all_hi = 0x7fffffff, any_lo = 0x7fffffff, any_hi = 0;
-    float f_row[2];
+    // ---- what this thread's rows (8 n + 2 t4 + z) see, and what all rows do; rows that do not exist see everything
+    int lo[NR][2], hi[NR][2], all_lo = 0, all_hi = 0x7fffffff, any_lo = 0x7fffffff, any_hi = 0;
+    float f_row[NR][2];
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const int r = g + 8 * z;
-      lo[z] = 0;
-      hi[z] = 0;
-      if (r < r_count) seen_range(a, E.len - E.rows + (r_first + r) / group, E.len, lo[z], hi[z]);
-      f_row[z] = row_scale[r];
-      all_lo = max(all_lo, lo[z]);
-      all_hi = min(all_hi, hi[z]);
-      any_lo = min(any_lo, r < r_count && hi[z] > lo[z] ? lo[z] : 0x7fffffff);
-      any_hi = max(any_hi, hi[z]);
-    }
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int r = 8 * n + 2 * t4 + z;
+        lo[n][z] = 0;
+        hi[n][z] = 0x7fffffff;
+        f_row[n][z] = row_scale[r];
+        if (r >= r_count) continue;
+        seen_range(a, E.len - E.rows + (r_first + r) / group, E.len, lo[n][z], hi[n][z]);
+        all_lo = max(all_lo, lo[n][z]);
+        all_hi = min(all_hi, hi[n][z]);
+        any_lo = min(any_lo, hi[n][z] > lo[n][z] ? lo[n][z] : 0x7fffffff);
+        any_hi = max(any_hi, hi[n][z]);
+      }
     all_lo = __reduce_max_sync(0xffffffffu, all_lo);
     all_hi = __reduce_min_sync(0xffffffffu, all_hi);
     any_lo = __reduce_min_sync(0xffffffffu, any_lo);
@@ -295,11 +320,16 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
     const int run_hi = min(u1 * (kUnit / kRun), (any_hi + kRun - 1) / kRun);
     const int n_runs = run_hi - run_lo > warp ? (run_hi - run_lo - warp + kStreamWarps - 1) / kStreamWarps : 0;
 
-    float acc[NT][4], top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f}, unit = 0.0f;
+    float acc[MT][NR][4], ref[NR][2], sum[NR][2], unit = 0.0f;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NR; ++n) {
+      ref[n][0] = ref[n][1] = -INFINITY;
+      sum[n][0] = sum[n][1] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[n][j] = 0.0f;
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[m][n][j] = 0.0f;
+    }
 
     // pages of the next 32 runs: lane l holds those of run l of the window, for its first and second 16 tokens
     int pages[2] = {-1, -1}, window_at = -32;
@@ -324,7 +354,10 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
           const int p = __shfl_sync(0xffffffffu, pages[z], i - window_at);
-          if (p < 0) continue;
+          if (p < 0) {                 // no such tokens: a maximum of -1 says so
+            if (lane < 2) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + 2 * kRun * DP + (2 * lane + z) * 4), "r"(0xbf800000u) : "memory");
+            continue;
+          }
           const int64_t block = (int64_t)p * a.cache.heads + hk;
           const int64_t from = block * page * dim + (int64_t)((tok + 16 * z) % page) * dim;
           auto copy = [&](int c, int chunks) {
@@ -347,140 +380,151 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
 #pragma unroll
     for (int i = 0; i < ST - 1; ++i) issue(i);
 
-    int valid_at = -32;                // the same window's validity, kept apart: issue() runs ahead of the use
-    unsigned valid[2] = {0, 0};
     for (int i = 0; i < n_runs; ++i) {
-      if (i >= valid_at + 32) {
-        valid_at = i;
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const int tok = (run_lo + warp + (i + lane) * kStreamWarps) * kRun + 16 * z;
-          bool ok = i + lane < n_runs && tok < E.len;
-          if (ok) {
-            const int p = a.pool.table[(int64_t)E.s * a.pool.max_pages + tok / page];
-            ok = p >= 0 && p < a.pool.n_pages;
-          }
-          valid[z] = __ballot_sync(0xffffffffu, ok);
-        }
-      }
       cp_wait<ST - 2>();
       __syncwarp();
       const uint32_t ks = ring + (i % ST) * SB, vs = ks + kRun * DP;
       const int tok = (run_lo + warp + i * kStreamWarps) * kRun;
-      const bool ok0 = valid[0] >> (i - valid_at) & 1u, ok1 = valid[1] >> (i - valid_at) & 1u;
 
-      // scores
-      float s[4][4];
+      // scores^T: tile p are the tokens 16 p .. 16 p + 15, row r of it the token with r's bits 0 and 1, 2 exchanged
+      float s[2][NR][4];
 #pragma unroll
-      for (int n = 0; n < 4; ++n)
+      for (int p = 0; p < 2; ++p)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[n][j] = 0.0f;
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[p][n][j] = 0.0f;
+      const int key = (g >> 1) + 4 * (g & 1);
 #pragma unroll
       for (int h = 0; h < DP / 64; ++h) {
-        uint32_t qa[4][4], ql[WIDE ? 4 : 1][4];
+        uint32_t q[NR][8], ql[WIDE ? NR : 1][8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint4 w = lds128(q_sm + ((h * 4 + k) * 32 + lane) * 16);
-          qa[k][0] = w.x; qa[k][1] = w.y; qa[k][2] = w.z; qa[k][3] = w.w;
-          if (WIDE) {
-            const uint4 l = lds128(q_sm + kRows * DP * 2 + ((h * 4 + k) * 32 + lane) * 16);
-            ql[k][0] = l.x; ql[k][1] = l.y; ql[k][2] = l.z; ql[k][3] = l.w;
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint4 w = lds128(q_sm + (((n * (DP / 64) + h) * 2 + k) * 32 + lane) * 16);
+            q[n][4 * k] = w.x; q[n][4 * k + 1] = w.y; q[n][4 * k + 2] = w.z; q[n][4 * k + 3] = w.w;
+            if (WIDE) {
+              const uint4 l = lds128(q_sm + ROWS * DP * 2 + (((n * (DP / 64) + h) * 2 + k) * 32 + lane) * 16);
+              ql[n][4 * k] = l.x; ql[n][4 * k + 1] = l.y; ql[n][4 * k + 2] = l.z; ql[n][4 * k + 3] = l.w;
+            }
           }
-        }
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          const int row = n * 8 + (g >> 1) + 4 * (g & 1);
-          const uint4 w = lds128(ks + chunk_at<DP>(row, h * 4 + t4));
-          const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+        for (int p = 0; p < 2; ++p) {
+          const uint4 x = lds128(ks + chunk_at<DP>(16 * p + key, h * 4 + t4)), y = lds128(ks + chunk_at<DP>(16 * p + 8 + key, h * 4 + t4));
+          const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint32_t b = words[k] ^ 0x80808080u;
-            const uint32_t b0 = two_codes<0x4140>(b), b1 = two_codes<0x4342>(b);
-            mma16816(s[n], qa[k], b0, b1);
-            if (WIDE) mma16816(s[n], ql[k], b0, b1);
+            const uint32_t xb = xw[k] ^ 0x80808080u, yb = yw[k] ^ 0x80808080u;
+            const uint32_t op[4] = {two_codes<0x4140>(xb), two_codes<0x4140>(yb), two_codes<0x4342>(xb), two_codes<0x4342>(yb)};
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+              mma16816(s[p][n], op, q[n][2 * k], q[n][2 * k + 1]);
+              if (WIDE) mma16816(s[p][n], op, ql[n][2 * k], ql[n][2 * k + 1]);
+            }
           }
         }
       }
-      // scales of the two halves
-      float amax[4];
+      // scales of the two tiles; a page of zeros must not set the unit, a maximum of -1 marks tokens that are not there
+      float kf[2], vf[2];
+      bool ok[2];
       {
         const uint4 w = lds128(ks + 2 * kRun * DP);
-        amax[0] = __uint_as_float(w.x); amax[1] = __uint_as_float(w.y); amax[2] = __uint_as_float(w.z); amax[3] = __uint_as_float(w.w);
-      }
-      float kf[2] = {scale_of(amax[0]), scale_of(amax[1])};
-      // a page of zeros must not set the unit
-      float vf[2] = {ok0 ? __fdiv_rn(amax[2], kQmax8) : 0.0f, ok1 ? __fdiv_rn(amax[3], kQmax8) : 0.0f};
-      if (!ok0) kf[0] = 1.0f;
-      if (!ok1) kf[1] = 1.0f;
-
-      if (tok < all_lo || tok + kRun > all_hi || !ok0 || !ok1) {
+        const float k_max[2] = {__uint_as_float(w.x), __uint_as_float(w.y)}, v_max[2] = {__uint_as_float(w.z), __uint_as_float(w.w)};
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int t = tok + n * 8 + t4 + 4 * (j & 1);
-            if (t < lo[j >> 1] || t >= hi[j >> 1] || !(n < 2 ? ok0 : ok1)) s[n][j] = -INFINITY;
-          }
-      }
-      // softmax: factors are positive, so the largest product comes from the largest score
-      float f[2][2], shift[2], keep[2];
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-#pragma unroll
-        for (int p = 0; p < 2; ++p) f[z][p] = fmaxf(f_row[z] * kf[p], 1.2e-38f);
-        float m = fmaxf(fmaxf(fmaxf(s[0][2 * z], s[0][2 * z + 1]), fmaxf(s[1][2 * z], s[1][2 * z + 1])) * f[z][0],
-                        fmaxf(fmaxf(s[2][2 * z], s[2][2 * z + 1]), fmaxf(s[3][2 * z], s[3][2 * z + 1])) * f[z][1]);
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        m = fmaxf(m, top[z]);
-        const float ref = m == -INFINITY ? 0.0f : m;
-        keep[z] = ex2(top[z] - ref);
-        top[z] = m;
-        shift[z] = kWeightBias - ref;
-        sum[z] *= keep[z];
-      }
-      float now = fmaxf(unit, fmaxf(vf[0], vf[1]));
-      if (now > 0.0f) now = fmaxf(now, 1.2e-38f);
-      const float inv = now > 0.0f ? __fdiv_rn(1.0f, now) : 0.0f, change = unit * inv;
-      unit = now;
-      if (__any_sync(0xffffffffu, keep[0] * change != 1.0f || keep[1] * change != 1.0f)) {
-        const float c0 = keep[0] * change, c1 = keep[1] * change;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          acc[n][0] *= c0;
-          acc[n][1] *= c0;
-          acc[n][2] *= c1;
-          acc[n][3] *= c1;
+        for (int p = 0; p < 2; ++p) {
+          ok[p] = !(k_max[p] < 0.0f);
+          kf[p] = ok[p] ? scale_of(k_max[p]) : 1.0f;
+          vf[p] = ok[p] ? __fdiv_rn(v_max[p], kQmax8) : 0.0f;
         }
       }
-      uint32_t pa[2][4], pl[WIDE ? 2 : 1][4];
+      if (tok < all_lo || tok + kRun > all_hi || !ok[0] || !ok[1]) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int t = tok + 16 * p + key + 8 * (j >> 1);
+              if (t < lo[n][j & 1] || t >= hi[n][j & 1] || !ok[p]) s[p][n][j] = -INFINITY;
+            }
+      }
+      // exponents of the weights against the reference in use
+      float over = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const float shift = kWeightBias - (ref[n][z] == -INFINITY ? 0.0f : ref[n][z]);
+          const float least = ref[n][z] == -INFINITY ? INFINITY : 0.0f;        // no reference yet: any score is too large
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const float f = fmaxf(f_row[n][z] * kf[p], 1.2e-38f);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float& x = s[p][n][2 * j + z];
+              x = fmaf(x, f, shift);
+              over = fmaxf(over, x == -INFINITY ? x : x + least);
+            }
+          }
+        }
+      float now = fmaxf(unit, fmaxf(vf[0], vf[1]));
+      if (now > 0.0f) now = fmaxf(now, 1.2e-38f);
+      if (__any_sync(0xffffffffu, over > kWeightMost || now != unit)) {
+        const float change = now > 0.0f ? __fdiv_rn(unit, now) : 0.0f;
+        unit = now;
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const float was = ref[n][z] == -INFINITY ? 0.0f : ref[n][z];
+            float m = fmaxf(fmaxf(s[0][n][z], s[0][n][2 + z]), fmaxf(s[1][n][z], s[1][n][2 + z]));
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            m = fmaxf(m - kWeightBias + was, ref[n][z]);
+            const float base = m == -INFINITY ? 0.0f : m;
+            const float keep = ex2(ref[n][z] - base);
+            ref[n][z] = m;
+            sum[n][z] *= keep;
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) s[p][n][2 * j + z] += was - base;
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+              acc[t][n][z] *= keep * change;
+              acc[t][n][2 + z] *= keep * change;
+            }
+          }
+      }
+      const float inv = unit > 0.0f ? __fdiv_rn(1.0f, unit) : 0.0f;
+      uint32_t w_hi[2][NR][2], w_lo[WIDE ? 2 : 1][NR][2];
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         const float share = vf[p] * inv;
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < NR; ++n)
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const float e0 = ex2(fmaf(s[2 * p + n][2 * z], f[z][p], shift[z]));
-            const float e1 = ex2(fmaf(s[2 * p + n][2 * z + 1], f[z][p], shift[z]));
-            sum[z] += e0 + e1;
+          for (int j = 0; j < 2; ++j) {
+            const float e0 = ex2(s[p][n][2 * j]), e1 = ex2(s[p][n][2 * j + 1]);
+            sum[n][0] += e0;
+            sum[n][1] += e1;
             const float w0 = e0 * share, w1 = e1 * share;
             const __half2 h = __floats2half2_rn(w0, w1);
-            pa[p][2 * n + z] = h2_bits(h);
-            if (WIDE) pl[p][2 * n + z] = pack_h2(w0 - __low2float(h), w1 - __high2float(h));
+            w_hi[p][n][j] = transpose8(h2_bits(h));
+            if (WIDE) w_lo[p][n][j] = transpose8(pack_h2(w0 - __low2float(h), w1 - __high2float(h)));
           }
       }
-      // values
+      // out^T: byte 2 m of a thread's elements is row g of tile m, byte 2 m + 1 row g + 8
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const int row = 16 * p + t4;
         constexpr int LINES = DP >= 128 ? DP / 128 : 1, WORDS = DP >= 128 ? 4 : 2;
 #pragma unroll
         for (int h = 0; h < LINES; ++h) {
           uint32_t w[4][WORDS];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const int r = row + 4 * k;
+            const int r = 16 * p + t4 + 4 * k;
             if (DP >= 128) {
               const uint4 x = lds128(vs + chunk_at<DP>(r, h * 8 + g));
               w[k][0] = x.x; w[k][1] = x.y; w[k][WORDS - 2] = x.z; w[k][WORDS - 1] = x.w;
@@ -492,13 +536,15 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
 #pragma unroll
           for (int q = 0; q < WORDS; ++q) {
             const uint32_t x0 = w[0][q] ^ 0x80808080u, x1 = w[1][q] ^ 0x80808080u, x2 = w[2][q] ^ 0x80808080u, x3 = w[3][q] ^ 0x80808080u;
-            const uint32_t y[2][2] = {{__byte_perm(x0, x1, 0x5140), __byte_perm(x0, x1, 0x7362)}, {__byte_perm(x2, x3, 0x5140), __byte_perm(x2, x3, 0x7362)}};
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              const uint32_t b0 = b & 1 ? two_codes<0x4342>(y[0][b >> 1]) : two_codes<0x4140>(y[0][b >> 1]);
-              const uint32_t b1 = b & 1 ? two_codes<0x4342>(y[1][b >> 1]) : two_codes<0x4140>(y[1][b >> 1]);
-              mma16816(acc[(h * WORDS + q) * 4 + b], pa[p], b0, b1);
-              if (WIDE) mma16816(acc[(h * WORDS + q) * 4 + b], pl[p], b0, b1);
+            for (int b = 0; b < 2; ++b) {
+              const uint32_t y0 = __byte_perm(x0, x1, b ? 0x7362 : 0x5140), y1 = __byte_perm(x2, x3, b ? 0x7362 : 0x5140);
+              const uint32_t op[4] = {two_codes<0x4140>(y0), two_codes<0x4342>(y0), two_codes<0x4140>(y1), two_codes<0x4342>(y1)};
+#pragma unroll
+              for (int n = 0; n < NR; ++n) {
+                mma16816(acc[(h * WORDS + q) * 2 + b][n], op, w_hi[p][n][0], w_hi[p][n][1]);
+                if (WIDE) mma16816(acc[(h * WORDS + q) * 2 + b][n], op, w_lo[p][n][0], w_lo[p][n][1]);
+              }
             }
           }
         }
@@ -510,44 +556,42 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
 
     // ---- the four warps' parts of the segment, then out
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      sum[z] += __shfl_xor_sync(0xffffffffu, sum[z], 1);
-      sum[z] += __shfl_xor_sync(0xffffffffu, sum[z], 2);
-      if (t4 == 0) merge_top[warp][g + 8 * z] = top[z];
-    }
-    __syncthreads();                   // also: every warp's ring is empty
-    float m_all[2], factor[2];
-#pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      m_all[z] = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) m_all[z] = fmaxf(m_all[z], merge_top[w][g + 8 * z]);
-      factor[z] = top[z] == -INFINITY ? 0.0f : ex2(top[z] - m_all[z]);
-      if (t4 == 0) merge_sum[warp][g + 8 * z] = sum[z] * factor[z];
-      factor[z] *= unit;
-    }
-    // column n * 8 + c of the accumulators is the element c * 16 + n of its 128-element line (64: c * 8 + n)
-    constexpr int PITCH = DP + 4;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int d = DP >= 128 ? (n / 16) * 128 + (2 * t4) * 16 + n % 16 : (2 * t4) * 8 + n;
-      constexpr int STEP = DP >= 128 ? 16 : 8;
+    for (int n = 0; n < NR; ++n)
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
-        float* to = merged + (warp * kRows + g + 8 * z) * PITCH + d;
-        to[0] = acc[n][2 * z] * factor[z];
-        to[STEP] = acc[n][2 * z + 1] * factor[z];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) sum[n][z] += __shfl_xor_sync(0xffffffffu, sum[n][z], o);
+        if (g == 0) merge_top[warp][8 * n + 2 * t4 + z] = ref[n][z];
       }
-    }
+    __syncthreads();                   // also: every warp's ring is empty
+    constexpr int PITCH = DP + 4;
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int r = 8 * n + 2 * t4 + z;
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, merge_top[w][r]);
+        float factor = ref[n][z] == -INFINITY ? 0.0f : ex2(ref[n][z] - m);
+        if (g == 0) merge_sum[warp][r] = sum[n][z] * factor;
+        factor *= unit;
+        float* to = merged + (warp * ROWS + r) * PITCH;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          const int d = DP >= 128 ? (t / 8) * 128 + g * 16 + (t % 8) * 2 : g * 8 + t * 2;
+          *reinterpret_cast<float2*>(to + d) = make_float2(acc[t][n][z] * factor, acc[t][n][2 + z] * factor);
+        }
+      }
     __syncthreads();
-    const bool whole = u0 == 0 && u1 == E.units;
-    float* part = parts + ((int64_t)me * 2 + (u0 > 0 ? 0 : 1)) * part_floats<DP>();
-    for (int e = tid; e < kRows * DP / 4; e += 32 * kStreamWarps) {
+    const bool whole = u0 == 0 && u1 == n_units;
+    float* part = parts + ((int64_t)me * 2 + (u0 > 0 ? 0 : 1)) * part_floats<DP, NR>();
+    for (int e = tid; e < ROWS * DP / 4; e += 32 * kStreamWarps) {
       const int r = e / (DP / 4), d = (e - r * (DP / 4)) * 4;
       float4 v = make_float4(0, 0, 0, 0);
 #pragma unroll
       for (int w = 0; w < kStreamWarps; ++w) {
-        const float4 x = *reinterpret_cast<const float4*>(merged + (w * kRows + r) * PITCH + d);
+        const float4 x = *reinterpret_cast<const float4*>(merged + (w * ROWS + r) * PITCH + d);
         v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
       }
       if (!whole) {
@@ -569,20 +613,20 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
       else *reinterpret_cast<uint2*>(out) = o.w2;
     }
     if (!whole) {
-      if (tid < kRows) {
+      if (tid < ROWS) {
         float m = -INFINITY, l = 0.0f;
 #pragma unroll
         for (int w = 0; w < kStreamWarps; ++w) {
           m = fmaxf(m, merge_top[w][tid]);
           l += merge_sum[w][tid];
         }
-        part[kRows * DP + tid] = m;
-        part[kRows * DP + kRows + tid] = l;
+        part[ROWS * DP + tid] = m;
+        part[ROWS * DP + ROWS + tid] = l;
       }
-      if (tid == 0 && u0 > 0 && u1 == E.units) {
+      if (tid == 0 && u0 > 0 && u1 == n_units) {
         PartMeta o;
         o.row0 = E.row0;
-        o.first = share_of(total, blocks, at - u0);
+        o.first = share_of(total, blocks, entry_at + item * E.units + kSetup);      // the block of the tile's first tokens
         o.rows = (int)E.rows;
         o.tile = tile;
         o.head = hk;
@@ -590,15 +634,14 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP>()) kv_att
       }
     }
     __syncthreads();
-    at += u1 - u0;
   }
 }
 
-// Joins the parts of the tile that block blockIdx.x of the kernel above finished: a slice of 16 elements of each row.
-constexpr int kJoinThreads = 64;
-template <typename T, int DP>
-__global__ void __launch_bounds__(kJoinThreads) kv_attention_join(const AttnArgs a) {
+// Joins the parts of the tile that block blockIdx.x of the kernel above finished: 16 elements of each row.
+template <typename T, int DP, int NR>
+__global__ void __launch_bounds__(32 * NR) kv_attention_join(const AttnArgs a) {
   pdl_entry();
+  constexpr int ROWS = 8 * NR;
   const PartMeta* meta = reinterpret_cast<const PartMeta*>(a.work);
   const float* parts = reinterpret_cast<const float*>(meta + kMaxStreamGrid);
   const int last = blockIdx.x, first = meta[last].first;
@@ -606,19 +649,19 @@ __global__ void __launch_bounds__(kJoinThreads) kv_attention_join(const AttnArgs
   const PartMeta o = meta[last];
   const int r = threadIdx.x >> 2, d = blockIdx.y * 16 + (threadIdx.x & 3) * 4;
   const int group = a.q_heads / a.cache.heads;
-  const int64_t r_at = (int64_t)o.tile * kRows + r;
+  const int64_t r_at = (int64_t)o.tile * ROWS + r;
   if (r_at >= (int64_t)o.rows * group || d >= a.cache.dim) return;
   // the first block's last segment is its second part, every later block's first segment its first
   float top = -INFINITY;
-  for (int b = first; b <= last; ++b) top = fmaxf(top, parts[((int64_t)b * 2 + (b == first)) * part_floats<DP>() + kRows * DP + r]);
+  for (int b = first; b <= last; ++b) top = fmaxf(top, parts[((int64_t)b * 2 + (b == first)) * part_floats<DP, NR>() + ROWS * DP + r]);
   float l = 0.0f;
   float4 v = make_float4(0, 0, 0, 0);
   for (int b = first; b <= last; ++b) {
-    const float* p = parts + ((int64_t)b * 2 + (b == first)) * part_floats<DP>();
-    const float m = p[kRows * DP + r];
+    const float* p = parts + ((int64_t)b * 2 + (b == first)) * part_floats<DP, NR>();
+    const float m = p[ROWS * DP + r];
     const float f = m == -INFINITY ? 0.0f : ex2(m - top);
     const float4 x = *reinterpret_cast<const float4*>(p + r * DP + d);
-    l += f * p[kRows * DP + kRows + r];
+    l += f * p[ROWS * DP + ROWS + r];
     v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
   }
   const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : (l == 0.0f ? 0.0f : l);
@@ -629,39 +672,51 @@ __global__ void __launch_bounds__(kJoinThreads) kv_attention_join(const AttnArgs
   out[3] = from_float<T>(v.w * inv);
 }
 
-template <int DP>
-constexpr int64_t stream_work() { return kMaxStreamGrid * (int64_t)sizeof(PartMeta) + 2 * kMaxStreamGrid * part_floats<DP>() * 4; }
+template <int DP, int NR>
+constexpr int64_t stream_work() { return kMaxStreamGrid * ((int64_t)sizeof(PartMeta) + 2 * part_floats<DP, NR>() * 4); }
 
-template <typename T, int DP>
+template <typename T, int DP, int NR>
 int stream_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
-  constexpr int smem = stream_smem<DP, sizeof(T) == 4>();
-  static_assert(smem >= query_bytes<DP, sizeof(T) == 4>() + kStreamWarps * kRows * (DP + 4) * 4, "the parts of a segment are joined where the ring was");
-  static_assert(stream_blocks<DP>() * (smem + 2048) <= 227 * 1024, "resident blocks");
-  const cudaError_t e = cudaFuncSetAttribute(kv_attention_stream<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  constexpr bool WIDE = sizeof(T) == 4;
+  constexpr int smem = stream_smem<DP, NR, WIDE>();
+  static_assert(smem >= query_bytes<DP, NR, WIDE>() + kStreamWarps * 8 * NR * (DP + 4) * 4, "the parts of a segment are joined where the ring was");
+  static_assert(stream_blocks<DP, NR>() * (smem + 2048) <= 227 * 1024, "resident blocks");
+  const cudaError_t e = cudaFuncSetAttribute(kv_attention_stream<T, DP, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return check_cuda(ctx, e, "kv_attention");
-  const int grid = std::min(sm_count(ctx) * stream_blocks<DP>(), kMaxStreamGrid);
-  launch_pdl(kv_attention_stream<T, DP>, dim3(grid), dim3(32 * kStreamWarps), smem, st, a);
-  launch_pdl(kv_attention_join<T, DP>, dim3(grid, DP / 16), dim3(kJoinThreads), 0, st, a);
+  const int grid = std::min(sm_count(ctx) * stream_blocks<DP, NR>(), kMaxStreamGrid);
+  launch_pdl(kv_attention_stream<T, DP, NR>, dim3(grid), dim3(32 * kStreamWarps), smem, st, a);
+  launch_pdl(kv_attention_join<T, DP, NR>, dim3(grid, DP / 16), dim3(32 * NR), 0, st, a);
   count_launch(ctx, 2);
   return check_cuda(ctx, cudaGetLastError(), "kv_attention");
 }
+// rows: of the longest entry, as far as known
 template <typename T>
-int stream_of(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
-  return a.cache.dim <= 64 ? stream_as<T, 64>(ctx, a, st) : a.cache.dim <= 128 ? stream_as<T, 128>(ctx, a, st) : stream_as<T, 256>(ctx, a, st);
+int stream_of(Ctx* ctx, const AttnArgs& a, int64_t rows, cudaStream_t st) {
+  if (a.cache.dim > 128) return rows <= 8 ? stream_as<T, 256, 1>(ctx, a, st) : stream_as<T, 256, 2>(ctx, a, st);
+  if (a.cache.dim > 64) {
+    if (rows <= 8) return stream_as<T, 128, 1>(ctx, a, st);
+    if constexpr (sizeof(T) == 2)
+      if (rows > 16) return stream_as<T, 128, 4>(ctx, a, st);
+    return stream_as<T, 128, 2>(ctx, a, st);
+  }
+  return rows <= 8 ? stream_as<T, 64, 1>(ctx, a, st) : rows <= 16 ? stream_as<T, 64, 2>(ctx, a, st) : stream_as<T, 64, 4>(ctx, a, st);
 }
 
 }  // namespace
 
 int64_t kv_attention_work(Ctx*, const CacheView& c, int, int64_t, int) {
-  return c.dim <= 64 ? stream_work<64>() : c.dim <= 128 ? stream_work<128>() : stream_work<256>();
+  return c.dim <= 64 ? stream_work<64, 4>() : c.dim <= 128 ? stream_work<128, 4>() : stream_work<256, 2>();
 }
 
 int launch_kv_attention(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const void* q, int64_t q_row, int64_t q_head,
-                        int q_heads, void* out, int64_t o_row, int64_t o_head, int dtype, int, int, float scale, int causal, int window, void* work,
-                        cudaStream_t st) {
+                        int q_heads, void* out, int64_t o_row, int64_t o_head, int dtype, int max_rows, int, float scale, int causal, int window,
+                        void* work, cudaStream_t st) {
   if (b.n == 0 || b.rows == 0) return QCFG_OK;
   const AttnArgs a{p, c, b, q, out, q_row, q_head, o_row, o_head, q_heads, causal, window, scale * 1.44269504088896f, work, err_word(ctx)};
-  return dtype == QCFG_FP32 ? stream_of<float>(ctx, a, st) : dtype == QCFG_BF16 ? stream_of<__nv_bfloat16>(ctx, a, st) : stream_of<__half>(ctx, a, st);
+  int64_t rows = !b.starts ? 1 : max_rows > 0 ? max_rows : (b.rows + b.n - 1) / b.n;
+  rows *= q_heads / c.heads;
+  return dtype == QCFG_FP32 ? stream_of<float>(ctx, a, rows, st) : dtype == QCFG_BF16 ? stream_of<__nv_bfloat16>(ctx, a, rows, st)
+                                                                                       : stream_of<__half>(ctx, a, rows, st);
 }
 
 }  // namespace qcfg
