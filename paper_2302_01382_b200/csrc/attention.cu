@@ -58,7 +58,7 @@ constexpr int kMinUnits = 2;        // a block takes at least this many
 constexpr float kWeightBias = 7.0f, kWeightMost = 15.0f;
 
 template <int DP> __host__ __device__ constexpr int stage_bytes() { return 2 * kRun * DP + 32; }             // keys, values, four maxima
-template <int DP, int NR> __host__ __device__ constexpr int stream_blocks() { return DP == 256 ? 1 : DP == 128 ? (NR == 4 ? 2 : 3) : (NR == 1 ? 4 : 3); }    // per SM
+template <int DP, int NR> __host__ __device__ constexpr int stream_blocks() { return DP == 256 ? 1 : DP == 128 ? (NR == 4 ? 2 : 3) : NR == 1 ? 4 : NR == 2 ? 3 : 2; }    // per SM
 template <int DP, int NR> __host__ __device__ constexpr int stream_stages() { return DP == 256 ? 3 : DP == 128 ? (NR == 4 ? 3 : 2) : (NR == 1 ? 3 : 4); }
 template <int DP, int NR, bool WIDE> __host__ __device__ constexpr int query_bytes() { return (WIDE ? 2 : 1) * 8 * NR * DP * 2; }
 template <int DP, int NR, bool WIDE>
@@ -120,7 +120,9 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
 }
 
 // Where 16-byte chunk `chunk` of token `row` (0..31) of a run lies.  A warp reads keys as rows {0,4},{1,5},.. x four chunks and values as rows
-// 0..3 or 4..7 x neighbouring chunks (16 or 8 bytes): the exclusive-or keeps both free of bank conflicts.
+// 0..3 or 4..7 x neighbouring chunks (16 or 8 bytes): the exclusive-or keeps both free of bank conflicts.  Everything in it that is
+// not a compile-time constant depends on the lane alone: the offsets below are computed once, and what else differs between a lane's
+// accesses is an immediate or the flip of bit 6.  (With the whole expression at each access a run took 1030 instructions, 575 this way.)
 template <int DP>
 __device__ __forceinline__ uint32_t chunk_at(int row, int chunk) {
   if (DP == 64) return (uint32_t)((row >> 1) * 128 + ((((row & 1) << 2) | chunk) ^ (2 * ((row >> 1) & 3))) * 16);
@@ -147,12 +149,25 @@ __device__ __forceinline__ Entry entry_of(const AttnArgs& a, int i) {
 }
 __device__ __forceinline__ int64_t entry_units(const AttnArgs& a, const Entry& e) { return (int64_t)e.tiles * e.units * a.cache.heads; }
 
-// First unit of block b of `blocks` sharing `total`
-__device__ __forceinline__ int64_t share_at(int64_t total, int blocks, int b) { return total / blocks * b + min((int64_t)b, total % blocks); }
-__device__ __forceinline__ int share_of(int64_t total, int blocks, int64_t unit) {      // the block that has it
-  const int64_t each = total / blocks, more = total % blocks;
-  return unit < more * (each + 1) ? (int)(unit / (each + 1)) : (int)(more + (unit - more * (each + 1)) / each);
+// a / b of numbers that are not negative: 64-bit divisions take a hundred instructions, and both fit 32 bits but in huge batches
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
+// How `total` units fall to `blocks` blocks: the first `more` get one more than `each`
+struct Shares {
+  int64_t each;
+  int more, blocks;
+  __device__ __forceinline__ Shares(int64_t total, int grid) {
+    blocks = (int)max((int64_t)1, min((int64_t)grid, quotient(total, kSetup + kMinUnits)));
+    each = quotient(total, blocks);
+    more = (int)(total - each * blocks);
+  }
+  __device__ __forceinline__ int64_t first(int b) const { return each * b + min(b, more); }
+  __device__ __forceinline__ int owner(int64_t unit) const {
+    const int64_t head = more * (each + 1);
+    return unit < head ? (int)quotient(unit, each + 1) : more + (int)quotient(unit - head, each);
+  }
+};
 
 template <typename T, int DP, int NR>
 __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv_attention_stream(const AttnArgs a) {
@@ -168,83 +183,85 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
   float* parts = reinterpret_cast<float*>(meta + kMaxStreamGrid);
 
   // ---- this block's share: the sum over all entries, then the entry its first unit lies in
-  int64_t total = 0;
-  for (int i0 = 0; i0 < a.batch.n; i0 += 32 * kStreamWarps) {
-    const int i = i0 + tid;
-    int64_t u = i < a.batch.n ? entry_units(a, entry_of<NR>(a, i)) : 0;
+  auto units_of = [&](int i) { return i < a.batch.n ? entry_units(a, entry_of<NR>(a, i)) : (int64_t)0; };
+  // inclusive sums over the block's threads; `sum` gets the total
+  auto scan_units = [&](int64_t u, int64_t& sum) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
-    __syncthreads();
-    if (lane == 0) scan[warp] = u;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kStreamWarps; ++w) total += scan[w];
-  }
-  const int blocks = (int)max((int64_t)1, min((int64_t)gridDim.x, total / (kSetup + kMinUnits)));
-  const int me = blockIdx.x;
-  if (tid == 0) meta[me].first = -1;
-  if (me >= blocks || total == 0) return;
-  int64_t at = share_at(total, blocks, me);
-  const int64_t end = share_at(total, blocks, me + 1);
-  int entry = 0;
-  int64_t entry_at = 0;            // first unit of the entry
-  {
-    int64_t before = 0;
-    bool done = false;
-    for (int i0 = 0; i0 < a.batch.n && !done; i0 += 32 * kStreamWarps) {
-      const int i = i0 + tid;
-      const int64_t u = i < a.batch.n ? entry_units(a, entry_of<NR>(a, i)) : 0;
-      int64_t s = u;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(0xffffffffu, s, o);
-        if (lane >= o) s += v;
-      }
-      __syncthreads();
-      if (lane == 31) scan[warp] = s;
-      __syncthreads();
-      int64_t mine = before;
-#pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) {
-        if (w < warp) mine += scan[w];
-        before += scan[w];
-      }
-      if (u > 0 && mine + s - u <= at && at < mine + s) { found[0] = i; found[1] = mine + s - u; }
-      done = at < before;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, u, o);
+      if (lane >= o) u += v;
     }
     __syncthreads();
-    entry = (int)found[0];
-    entry_at = found[1];
+    if (lane == 31) scan[warp] = u;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < kStreamWarps; ++w) {
+      if (w < warp) u += scan[w];
+      sum += scan[w];
+    }
+    return u;
+  };
+  int64_t total, mine = units_of(tid), upto = scan_units(mine, total);
+  for (int i0 = 32 * kStreamWarps; i0 < a.batch.n; i0 += 32 * kStreamWarps) {
+    int64_t sum;
+    scan_units(units_of(i0 + tid), sum);
+    total += sum;
   }
+  const Shares shares(total, gridDim.x);
+  const int me = blockIdx.x;
+  if (tid == 0) meta[me].first = -1;
+  if (me >= shares.blocks || total == 0) return;
+  int64_t at = shares.first(me);
+  const int64_t end = shares.first(me + 1);
+  for (int i0 = 0;;) {
+    if (mine > 0 && upto - mine <= at && at < upto) { found[0] = i0 + tid; found[1] = upto - mine; }
+    i0 += 32 * kStreamWarps;
+    if (i0 >= a.batch.n) break;
+    __syncthreads();
+    if (tid == 32 * kStreamWarps - 1) scan[0] = upto;
+    __syncthreads();
+    const int64_t before = scan[0];
+    int64_t sum;
+    mine = units_of(i0 + tid);
+    upto = before + scan_units(mine, sum);
+  }
+  __syncthreads();
+  int entry = (int)found[0];
+  int64_t entry_at = found[1];     // first unit of the entry
   Entry E = entry_of<NR>(a, entry);
 
   const uint32_t q_sm = smem_at(smem);
   const uint32_t ring = q_sm + query_bytes<DP, NR, WIDE>() + warp * ST * SB;
   float* merged = reinterpret_cast<float*>(smem + query_bytes<DP, NR, WIDE>());     // the ring again, once it is empty
+  const int key = (g >> 1) + 4 * (g & 1);                  // token of row g of a tile of scores^T
+  const uint32_t copy_at = chunk_at<DP>(lane / (DP / 16), lane % (DP / 16)), key_at = chunk_at<DP>(key, t4),
+                 val_at = kRun * DP + (DP == 64 ? chunk_at<DP>(t4, g >> 1) + (g & 1) * 8 : chunk_at<DP>(t4, g));
 
   while (at < end) {
     while (at >= entry_at + entry_units(a, E)) {
       entry_at += entry_units(a, E);
       E = entry_of<NR>(a, ++entry);
     }
-    const int64_t item = (at - entry_at) / E.units;
-    const int v0 = (int)((at - entry_at) % E.units), v1 = (int)min((int64_t)E.units, v0 + (end - at));
+    const int64_t item = quotient(at - entry_at, E.units);
+    const int v0 = (int)(at - entry_at - item * E.units), v1 = (int)min((int64_t)E.units, v0 + (end - at));
     const int n_units = E.units - kSetup, u0 = max(v0 - kSetup, 0), u1 = max(v1 - kSetup, 0);
     at += v1 - v0;
     if (u1 == 0) continue;                                 // ends before the tile's first token
     if (tid == 0 && E.s >= a.pool.max_seqs) atomicOr(a.err, ERR_PAGE);
-    const int hk = (int)(item / E.tiles), tile = (int)(item % E.tiles);
-    const int64_t r_first = (int64_t)tile * ROWS;          // first row of the tile in the entry
-    const int r_count = (int)min((int64_t)ROWS, E.rows * group - r_first);
+    const int hk = (int)quotient(item, E.tiles), tile = (int)(item - (int64_t)hk * E.tiles);
+    // the tile's first row: token t_first of the entry, head h_first of the group
+    const int64_t t_first = quotient((int64_t)tile * ROWS, group);
+    const unsigned h_first = (unsigned)((int64_t)tile * ROWS - t_first * group);
+    const int r_count = (int)min((int64_t)ROWS, E.rows * group - (int64_t)tile * ROWS);
 
     // ---- queries, in the order the MMA's B operand wants: eight threads a row
 #pragma unroll
     for (int r0 = 0; r0 < ROWS; r0 += 16) {
       const int r = r0 + (tid >> 3), part = tid & 7;
       if (ROWS >= 16 || r < ROWS) {
-        const int64_t row = (r_first + r) / group;
-        const int head = hk * group + (int)((r_first + r) % group);
-        const T* q = reinterpret_cast<const T*>(a.q) + (E.row0 + row) * a.q_row + head * a.q_head;
+        const unsigned row = (h_first + r) / (unsigned)group, head = hk * group + (h_first + r - row * group);
+        const T* q = reinterpret_cast<const T*>(a.q) + (E.row0 + t_first + row) * a.q_row + head * a.q_head;
         constexpr int V = Vec<T>::N;
         float v[DP / 8];
         unsigned top = 0;
@@ -305,7 +322,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
         hi[n][z] = 0x7fffffff;
         f_row[n][z] = row_scale[r];
         if (r >= r_count) continue;
-        seen_range(a, E.len - E.rows + (r_first + r) / group, E.len, lo[n][z], hi[n][z]);
+        seen_range(a, E.len - E.rows + t_first + (h_first + r) / (unsigned)group, E.len, lo[n][z], hi[n][z]);
         all_lo = max(all_lo, lo[n][z]);
         all_hi = min(all_hi, hi[n][z]);
         any_lo = min(any_lo, hi[n][z] > lo[n][z] ? lo[n][z] : 0x7fffffff);
@@ -320,7 +337,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
     const int run_hi = min(u1 * (kUnit / kRun), (any_hi + kRun - 1) / kRun);
     const int n_runs = run_hi - run_lo > warp ? (run_hi - run_lo - warp + kStreamWarps - 1) / kStreamWarps : 0;
 
-    float acc[MT][NR][4], ref[NR][2], sum[NR][2], unit = 0.0f;
+    float acc[MT][NR][4], ref[NR][2], sum[NR][2], unit = 0.0f, inv = 0.0f;
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       ref[n][0] = ref[n][1] = -INFINITY;
@@ -346,10 +363,11 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
         pages[z] = p;
       }
     };
+    uint32_t fill = 0;
     auto issue = [&](int i) {
       if (i < n_runs) {
         if (i >= window_at + 32) look_up(i);
-        const uint32_t to = ring + (i % ST) * SB;
+        const uint32_t to = ring + fill;
         const int tok = (run_lo + warp + i * kStreamWarps) * kRun;
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
@@ -359,31 +377,41 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
             continue;
           }
           const int64_t block = (int64_t)p * a.cache.heads + hk;
-          const int64_t from = block * page * dim + (int64_t)((tok + 16 * z) % page) * dim;
-          auto copy = [&](int c, int chunks) {
-            const int row = c / chunks, ch = c - row * chunks;
-            const uint32_t o = chunk_at<DP>(16 * z + row, ch);
-            cp_async16(to + o, a.cache.k + from + c * 16);
-            cp_async16(to + kRun * DP + o, a.cache.v + from + c * 16);
-          };
+          const int64_t from = (block * page + ((tok + 16 * z) & (page - 1))) * dim + lane * 16;
+          const int8_t *k_from = a.cache.k + from, *v_from = a.cache.v + from;
           if (dim == DP) {
+            const uint32_t even = to + z * 16 * DP + copy_at, odd = to + z * 16 * DP + (copy_at ^ 64u);
 #pragma unroll
-            for (int c = 0; c < DP / 32; ++c) copy(lane + 32 * c, DP / 16);
+            for (int c = 0; c < DP / 32; ++c) {                 // the copy's row is lane / (DP / 16) + c * (512 / DP)
+              const bool flip = DP == 64 ? false : DP == 128 ? (c & 1) : ((c ^ (c >> 1)) & 1);
+              cp_async16((flip ? odd : even) + c * 512, k_from + c * 512);
+              cp_async16((flip ? odd : even) + c * 512 + kRun * DP, v_from + c * 512);
+            }
           } else {
-            for (int c = lane; c < dim; c += 32) copy(c, dim / 16);
+            for (int c = lane; c < dim; c += 32) {
+              const int row = c / (dim / 16), ch = c - row * (dim / 16);
+              const uint32_t o = to + chunk_at<DP>(16 * z + row, ch);
+              cp_async16(o, k_from + (c - lane) * 16);
+              cp_async16(o + kRun * DP, v_from + (c - lane) * 16);
+            }
           }
           if (lane < 2) cp_async4(to + 2 * kRun * DP + (2 * lane + z) * 4, (lane ? a.cache.v_absmax : a.cache.k_absmax) + block);
         }
       }
+      fill = fill == (ST - 1) * SB ? 0 : fill + SB;
       cp_commit();
     };
 #pragma unroll
     for (int i = 0; i < ST - 1; ++i) issue(i);
 
+    uint32_t drain = 0;
+    bool fresh = true;                 // some row has no reference yet
     for (int i = 0; i < n_runs; ++i) {
       cp_wait<ST - 2>();
       __syncwarp();
-      const uint32_t ks = ring + (i % ST) * SB, vs = ks + kRun * DP;
+      const uint32_t stage = ring + drain;
+      const uint32_t k_even = stage + key_at, k_odd = stage + (key_at ^ 64u), v_even = stage + val_at, v_odd = stage + (val_at ^ 64u);
+      drain = drain == (ST - 1) * SB ? 0 : drain + SB;
       const int tok = (run_lo + warp + i * kStreamWarps) * kRun;
 
       // scores^T: tile p are the tokens 16 p .. 16 p + 15, row r of it the token with r's bits 0 and 1, 2 exchanged
@@ -394,7 +422,6 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
         for (int n = 0; n < NR; ++n)
 #pragma unroll
           for (int j = 0; j < 4; ++j) s[p][n][j] = 0.0f;
-      const int key = (g >> 1) + 4 * (g & 1);
 #pragma unroll
       for (int h = 0; h < DP / 64; ++h) {
         uint32_t q[NR][8], ql[WIDE ? NR : 1][8];
@@ -411,7 +438,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
           }
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-          const uint4 x = lds128(ks + chunk_at<DP>(16 * p + key, h * 4 + t4)), y = lds128(ks + chunk_at<DP>(16 * p + 8 + key, h * 4 + t4));
+          const uint32_t from = (DP > 64 && (h & 1) ? k_odd : k_even) + (h >> 1) * 128 + 16 * p * DP;
+          const uint4 x = lds128(from), y = lds128(from + 8 * DP);
           const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -429,13 +457,13 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
       float kf[2], vf[2];
       bool ok[2];
       {
-        const uint4 w = lds128(ks + 2 * kRun * DP);
+        const uint4 w = lds128(stage + 2 * kRun * DP);
         const float k_max[2] = {__uint_as_float(w.x), __uint_as_float(w.y)}, v_max[2] = {__uint_as_float(w.z), __uint_as_float(w.w)};
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
           ok[p] = !(k_max[p] < 0.0f);
-          kf[p] = ok[p] ? scale_of(k_max[p]) : 1.0f;
-          vf[p] = ok[p] ? __fdiv_rn(v_max[p], kQmax8) : 0.0f;
+          kf[p] = ok[p] && k_max[p] > 0.0f ? k_max[p] * (1.0f / kQmax8) : 1.0f;      // the scale but for its last bit
+          vf[p] = ok[p] ? v_max[p] * (1.0f / kQmax8) : 0.0f;
         }
       }
       if (tok < all_lo || tok + kRun > all_hi || !ok[0] || !ok[1]) {
@@ -456,7 +484,6 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
           const float shift = kWeightBias - (ref[n][z] == -INFINITY ? 0.0f : ref[n][z]);
-          const float least = ref[n][z] == -INFINITY ? INFINITY : 0.0f;        // no reference yet: any score is too large
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
             const float f = fmaxf(f_row[n][z] * kf[p], 1.2e-38f);
@@ -464,15 +491,17 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
             for (int j = 0; j < 2; ++j) {
               float& x = s[p][n][2 * j + z];
               x = fmaf(x, f, shift);
-              over = fmaxf(over, x == -INFINITY ? x : x + least);
+              over = fmaxf(over, x);
             }
           }
         }
       float now = fmaxf(unit, fmaxf(vf[0], vf[1]));
       if (now > 0.0f) now = fmaxf(now, 1.2e-38f);
-      if (__any_sync(0xffffffffu, over > kWeightMost || now != unit)) {
-        const float change = now > 0.0f ? __fdiv_rn(unit, now) : 0.0f;
+      if (__any_sync(0xffffffffu, over > kWeightMost || now != unit) || fresh) {
+        inv = now > 0.0f ? __fdiv_rn(1.0f, now) : 0.0f;
+        const float change = unit * inv;
         unit = now;
+        fresh = false;
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -485,6 +514,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
             const float base = m == -INFINITY ? 0.0f : m;
             const float keep = ex2(ref[n][z] - base);
             ref[n][z] = m;
+            fresh |= m == -INFINITY;
             sum[n][z] *= keep;
 #pragma unroll
             for (int p = 0; p < 2; ++p)
@@ -496,8 +526,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
               acc[t][n][2 + z] *= keep * change;
             }
           }
+        fresh = __any_sync(0xffffffffu, fresh);
       }
-      const float inv = unit > 0.0f ? __fdiv_rn(1.0f, unit) : 0.0f;
       uint32_t w_hi[2][NR][2], w_lo[WIDE ? 2 : 1][NR][2];
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
@@ -524,12 +554,12 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
           uint32_t w[4][WORDS];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const int r = 16 * p + t4 + 4 * k;
+            const uint32_t from = (k & 1 ? v_odd : v_even) + (16 * p + 4 * k) * DP + h * 128;
             if (DP >= 128) {
-              const uint4 x = lds128(vs + chunk_at<DP>(r, h * 8 + g));
+              const uint4 x = lds128(from);
               w[k][0] = x.x; w[k][1] = x.y; w[k][WORDS - 2] = x.z; w[k][WORDS - 1] = x.w;
             } else {
-              const uint2 x = lds64(vs + chunk_at<DP>(r, g >> 1) + (g & 1) * 8);
+              const uint2 x = lds64(from);
               w[k][0] = x.x; w[k][1] = x.y;
             }
           }
@@ -603,7 +633,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
 #pragma unroll
       for (int w = 0; w < kStreamWarps; ++w) l += merge_sum[w][r];
       const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : (l == 0.0f ? 0.0f : l);
-      T* out = reinterpret_cast<T*>(a.out) + (E.row0 + (r_first + r) / group) * a.o_row + (hk * group + (r_first + r) % group) * a.o_head + d;
+      const unsigned row = (h_first + r) / (unsigned)group, head = hk * group + (h_first + r - row * group);
+      T* out = reinterpret_cast<T*>(a.out) + (E.row0 + t_first + row) * a.o_row + head * a.o_head + d;
       union { T t[4]; uint4 w4; uint2 w2; } o;
       o.t[0] = from_float<T>(v.x * inv);
       o.t[1] = from_float<T>(v.y * inv);
@@ -626,7 +657,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
       if (tid == 0 && u0 > 0 && u1 == n_units) {
         PartMeta o;
         o.row0 = E.row0;
-        o.first = share_of(total, blocks, entry_at + item * E.units + kSetup);      // the block of the tile's first tokens
+        o.first = shares.owner(entry_at + item * E.units + kSetup);      // the block of the tile's first tokens
         o.rows = (int)E.rows;
         o.tile = tile;
         o.head = hk;
@@ -637,35 +668,59 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
   }
 }
 
-// Joins the parts of the tile that block blockIdx.x of the kernel above finished: 16 elements of each row.
+// Joins the parts of the tile that block blockIdx.x of the kernel above finished: 16 elements of each row, every kJoinWays-th part to a
+// group of threads.
+constexpr int kJoinWays = 8;
 template <typename T, int DP, int NR>
-__global__ void __launch_bounds__(32 * NR) kv_attention_join(const AttnArgs a) {
+__global__ void __launch_bounds__(32 * NR * kJoinWays) kv_attention_join(const AttnArgs a) {
   pdl_entry();
   constexpr int ROWS = 8 * NR;
+  __shared__ float4 values[kJoinWays][32 * NR];
+  __shared__ float tops[kJoinWays][ROWS], sums[kJoinWays][ROWS];
   const PartMeta* meta = reinterpret_cast<const PartMeta*>(a.work);
   const float* parts = reinterpret_cast<const float*>(meta + kMaxStreamGrid);
   const int last = blockIdx.x, first = meta[last].first;
   if (first < 0) return;
   const PartMeta o = meta[last];
-  const int r = threadIdx.x >> 2, d = blockIdx.y * 16 + (threadIdx.x & 3) * 4;
+  const int way = threadIdx.x / (32 * NR), e = threadIdx.x % (32 * NR);
+  const int r = e >> 2, d = blockIdx.y * 16 + (e & 3) * 4;
+  // the first block's last segment is its second part, every later block's first segment its first
+  float top = -INFINITY, l = 0.0f;
+  float4 v = make_float4(0, 0, 0, 0);
+  for (int b = first + way; b <= last; b += kJoinWays) {
+    const float* p = parts + ((int64_t)b * 2 + (b == first)) * part_floats<DP, NR>();
+    const float m = p[ROWS * DP + r], s = p[ROWS * DP + ROWS + r];
+    const float4 x = *reinterpret_cast<const float4*>(p + r * DP + d);
+    const float now = fmaxf(top, m), base = now == -INFINITY ? 0.0f : now, keep = ex2(top - base), f = ex2(m - base);
+    top = now;
+    l = l * keep + s * f;
+    v.x = v.x * keep + x.x * f;
+    v.y = v.y * keep + x.y * f;
+    v.z = v.z * keep + x.z * f;
+    v.w = v.w * keep + x.w * f;
+  }
+  values[way][e] = v;
+  if ((e & 3) == 0) { tops[way][r] = top; sums[way][r] = l; }
+  __syncthreads();
+  if (way) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWays; ++w) top = fmaxf(top, tops[w][r]);
+  const float base = top == -INFINITY ? 0.0f : top;
+  l = 0.0f;
+  v = make_float4(0, 0, 0, 0);
+#pragma unroll
+  for (int w = 0; w < kJoinWays; ++w) {
+    const float f = ex2(tops[w][r] - base);
+    const float4 x = values[w][e];
+    l += sums[w][r] * f;
+    v.x += x.x * f; v.y += x.y * f; v.z += x.z * f; v.w += x.w * f;
+  }
   const int group = a.q_heads / a.cache.heads;
   const int64_t r_at = (int64_t)o.tile * ROWS + r;
   if (r_at >= (int64_t)o.rows * group || d >= a.cache.dim) return;
-  // the first block's last segment is its second part, every later block's first segment its first
-  float top = -INFINITY;
-  for (int b = first; b <= last; ++b) top = fmaxf(top, parts[((int64_t)b * 2 + (b == first)) * part_floats<DP, NR>() + ROWS * DP + r]);
-  float l = 0.0f;
-  float4 v = make_float4(0, 0, 0, 0);
-  for (int b = first; b <= last; ++b) {
-    const float* p = parts + ((int64_t)b * 2 + (b == first)) * part_floats<DP, NR>();
-    const float m = p[ROWS * DP + r];
-    const float f = m == -INFINITY ? 0.0f : ex2(m - top);
-    const float4 x = *reinterpret_cast<const float4*>(p + r * DP + d);
-    l += f * p[ROWS * DP + ROWS + r];
-    v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
-  }
+  const int64_t row = quotient(r_at, group);
   const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : (l == 0.0f ? 0.0f : l);
-  T* out = reinterpret_cast<T*>(a.out) + (o.row0 + r_at / group) * a.o_row + (o.head * group + r_at % group) * a.o_head + d;
+  T* out = reinterpret_cast<T*>(a.out) + (o.row0 + row) * a.o_row + (o.head * group + (r_at - row * group)) * a.o_head + d;
   out[0] = from_float<T>(v.x * inv);
   out[1] = from_float<T>(v.y * inv);
   out[2] = from_float<T>(v.z * inv);
@@ -685,7 +740,7 @@ int stream_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return check_cuda(ctx, e, "kv_attention");
   const int grid = std::min(sm_count(ctx) * stream_blocks<DP, NR>(), kMaxStreamGrid);
   launch_pdl(kv_attention_stream<T, DP, NR>, dim3(grid), dim3(32 * kStreamWarps), smem, st, a);
-  launch_pdl(kv_attention_join<T, DP, NR>, dim3(grid, DP / 16), dim3(32 * NR), 0, st, a);
+  launch_pdl(kv_attention_join<T, DP, NR>, dim3(grid, DP / 16), dim3(32 * NR * kJoinWays), 0, st, a);
   count_launch(ctx, 2);
   return check_cuda(ctx, cudaGetLastError(), "kv_attention");
 }
