@@ -92,10 +92,12 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(o) : "r"(v));
   return o;
 }
-// Bytes `lo`, `hi` (selector 0x4H4L) of a word of codes plus 128 as two fp16 codes: 0x6400 + b is 1024 + b
+// Two bytes of a word of codes plus 128 as fp16 codes: 0x6400 + b is 1024 + b.  `magic` is 0x64646464, read from shared memory once: a
+// constant the compiler knows it keeps in a uniform register and copies anew in front of almost every permutation, 118 of a run's
+// 870 instructions.
 template <uint32_t SEL>
-__device__ __forceinline__ uint32_t two_codes(uint32_t biased) {
-  const uint32_t w = __byte_perm(biased, 0x64646464u, SEL);
+__device__ __forceinline__ uint32_t two_codes(uint32_t biased, uint32_t magic) {
+  const uint32_t w = __byte_perm(biased, magic, SEL);
   const __half2 off = __floats2half2_rn(1152.0f, 1152.0f);
   return h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&w), off));
 }
@@ -176,11 +178,14 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
   constexpr int ST = stream_stages<DP, NR>(), SB = stage_bytes<DP>(), MT = DP / 16, ROWS = 8 * NR;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int64_t scan[kStreamWarps], found[2];
+  __shared__ uint32_t magic_word;
   __shared__ float row_scale[ROWS], merge_top[kStreamWarps][ROWS], merge_sum[kStreamWarps][ROWS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   const int group = a.q_heads / a.cache.heads, dim = a.cache.dim, page = a.pool.page;
   PartMeta* meta = reinterpret_cast<PartMeta*>(a.work);
   float* parts = reinterpret_cast<float*>(meta + kMaxStreamGrid);
+
+  if (tid == 0) magic_word = 0x64646464u;
 
   // ---- this block's share: the sum over all entries, then the entry its first unit lies in
   auto units_of = [&](int i) { return i < a.batch.n ? entry_units(a, entry_of<NR>(a, i)) : (int64_t)0; };
@@ -227,6 +232,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
     upto = before + scan_units(mine, sum);
   }
   __syncthreads();
+  const uint32_t magic = *(volatile uint32_t*)&magic_word;
   int entry = (int)found[0];
   int64_t entry_at = found[1];     // first unit of the entry
   Entry E = entry_of<NR>(a, entry);
@@ -408,7 +414,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
     bool fresh = true;                 // some row has no reference yet
     for (int i = 0; i < n_runs; ++i) {
       cp_wait<ST - 2>();
-      __syncwarp();
+      __syncwarp();                    // the run has arrived for all lanes, and all are done with the one before, whose stage is filled again
+      issue(i + ST - 1);
       const uint32_t stage = ring + drain;
       const uint32_t k_even = stage + key_at, k_odd = stage + (key_at ^ 64u), v_even = stage + val_at, v_odd = stage + (val_at ^ 64u);
       drain = drain == (ST - 1) * SB ? 0 : drain + SB;
@@ -444,7 +451,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const uint32_t xb = xw[k] ^ 0x80808080u, yb = yw[k] ^ 0x80808080u;
-            const uint32_t op[4] = {two_codes<0x4140>(xb), two_codes<0x4140>(yb), two_codes<0x4342>(xb), two_codes<0x4342>(yb)};
+            const uint32_t op[4] = {two_codes<0x4140>(xb, magic), two_codes<0x4140>(yb, magic), two_codes<0x4342>(xb, magic), two_codes<0x4342>(yb, magic)};
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
               mma16816(s[p][n], op, q[n][2 * k], q[n][2 * k + 1]);
@@ -569,7 +576,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
               const uint32_t y0 = __byte_perm(x0, x1, b ? 0x7362 : 0x5140), y1 = __byte_perm(x2, x3, b ? 0x7362 : 0x5140);
-              const uint32_t op[4] = {two_codes<0x4140>(y0), two_codes<0x4342>(y0), two_codes<0x4140>(y1), two_codes<0x4342>(y1)};
+              const uint32_t op[4] = {two_codes<0x4140>(y0, magic), two_codes<0x4342>(y0, magic), two_codes<0x4140>(y1, magic), two_codes<0x4342>(y1, magic)};
 #pragma unroll
               for (int n = 0; n < NR; ++n) {
                 mma16816(acc[(h * WORDS + q) * 2 + b][n], op, w_hi[p][n][0], w_hi[p][n][1]);
@@ -579,8 +586,6 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
           }
         }
       }
-      __syncwarp();
-      issue(i + ST - 1);
     }
     cp_wait<0>();
 
@@ -736,7 +741,8 @@ int stream_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
   constexpr int smem = stream_smem<DP, NR, WIDE>();
   static_assert(smem >= query_bytes<DP, NR, WIDE>() + kStreamWarps * 8 * NR * (DP + 4) * 4, "the parts of a segment are joined where the ring was");
   static_assert(stream_blocks<DP, NR>() * (smem + 2048) <= 227 * 1024, "resident blocks");
-  const cudaError_t e = cudaFuncSetAttribute(kv_attention_stream<T, DP, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static DeviceOnce once;
+  const cudaError_t e = once.smem(device_of(ctx), (const void*)kv_attention_stream<T, DP, NR>, smem);
   if (e != cudaSuccess) return check_cuda(ctx, e, "kv_attention");
   const int grid = std::min(sm_count(ctx) * stream_blocks<DP, NR>(), kMaxStreamGrid);
   launch_pdl(kv_attention_stream<T, DP, NR>, dim3(grid), dim3(32 * kStreamWarps), smem, st, a);

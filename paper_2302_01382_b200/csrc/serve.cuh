@@ -3,9 +3,23 @@
 
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace qcfg {
+
+// Raises a kernel's shared-memory limit when a device first launches it (a driver call of a microsecond).
+struct DeviceOnce {
+  std::atomic<uint64_t> done{0};
+  cudaError_t smem(int device, const void* kernel, int bytes) {
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && device < 64) done.fetch_or(bit, std::memory_order_release);
+    return e;
+  }
+};
 
 struct PoolView {
   int32_t* table;      // [max_seqs][max_pages]
