@@ -360,9 +360,9 @@ int qcfg_kv_read(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* c
  * overlap q_dev.  Sums, maxima and accumulators are fp32.
  * max_rows, max_len: the longest entry's rows and the longest sequence's tokens as far as the caller
  * knows them (0: unknown).  They only choose how the work is spread; the results hold for any value.
- * work_dev: qcfg_kv_attention_work bytes on a 256-byte boundary, for the parts of rows whose context is
- * split; its contents need not be set.                                                          */
-int64_t qcfg_kv_attention_work(qcfg_ctx* ctx, const qcfg_kv_cache* cache, int32_t n, int64_t n_rows, int32_t q_heads);
+ * work_dev: qcfg_kv_attention_work bytes (of the same n_rows and max_len; 0: may be NULL) on a 256-byte
+ * boundary, for the parts of rows whose context is split; its contents need not be set.          */
+int64_t qcfg_kv_attention_work(qcfg_ctx* ctx, const qcfg_kv_cache* cache, int64_t n_rows, int32_t max_len);
 int qcfg_kv_attention(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch, const void* q_dev,
                       int64_t q_row_stride, int64_t q_head_stride, int32_t q_heads, void* out_dev, int64_t out_row_stride,
                       int64_t out_head_stride, int dtype, int32_t max_rows, int32_t max_len, float sm_scale, int causal,

@@ -6,7 +6,6 @@ use; if it is missing and cannot be built the call fails loudly -- there is no f
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from typing import List, Optional, Sequence
@@ -140,7 +139,7 @@ def load_library() -> C.CDLL:
     lib.qcfg_launch_count.restype = i64
     lib.qcfg_linear_i8_work.argtypes = [i64, i64]
     lib.qcfg_linear_i8_work.restype = i64
-    lib.qcfg_kv_attention_work.argtypes = [vp, cache, i32, i64, i32]
+    lib.qcfg_kv_attention_work.argtypes = [vp, cache, i64, i32]
     lib.qcfg_kv_attention_work.restype = i64
     _lib = lib
     return lib
@@ -326,7 +325,7 @@ class Context:
     # ---- linear layers with a scale for each token
     def _on_device(self, *tensors):
         for t in tensors:
-            if t is not None and (t.device.type != "cuda" or t.device.index != self.device):
+            if t is not None and t.get_device() != self.device:
                 raise QcfgError(EINVAL, f"tensor on {t.device}, the context is on cuda:{self.device}")
 
     def quantize_tokens(self, x: torch.Tensor, bits: int = 8, ldq: Optional[int] = None, stream=None):
@@ -336,11 +335,10 @@ class Context:
         rows, cols = x.shape
         if ldq is None:
             ldq = (cols + 15) // 16 * 16
-        with _stream_scope(stream):
-            q = torch.empty((rows, ldq), dtype=torch.int8, device=x.device)
-            scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-        self._check(self.lib.qcfg_quantize_tokens(self.h, _ptr(x), _dtype(x.dtype), rows, cols, _ld(x), bits, _ptr(q), ldq, _ptr(scale),
-                                                  self._here(stream)))
+        q = _empty((rows, ldq), torch.int8, x.device, stream)
+        scale = _empty(rows, torch.float32, x.device, stream)
+        self._check(self.lib.qcfg_quantize_tokens(self.h, x.data_ptr(), _dtype(x.dtype), rows, cols, _ld(x), bits, q.data_ptr(), ldq,
+                                                  scale.data_ptr(), self._here(stream)))
         return q, scale
 
     def gemm_i8_token(self, qx: torch.Tensor, qw: torch.Tensor, k: int, scale_x: torch.Tensor, scale_w: torch.Tensor,
@@ -357,8 +355,9 @@ class Context:
         _vector(scale_w, n)
         _vector(bias, n)
         out = _output(out, (m, n), dtype, qx.device, stream)
-        self._check(self.lib.qcfg_gemm_i8_token(self.h, _ptr(qx), _ld(qx), _ptr(qw), _ld(qw), m, n, k, _ptr(scale_x), _ptr(scale_w),
-                                                _ptr(bias), act, _ptr(out), _dtype(out.dtype), _ld(out), self._here(stream)))
+        self._check(self.lib.qcfg_gemm_i8_token(self.h, qx.data_ptr(), _ld(qx), qw.data_ptr(), _ld(qw), m, n, k, scale_x.data_ptr(),
+                                                scale_w.data_ptr(), _at(bias), act, out.data_ptr(), _dtype(out.dtype), _ld(out),
+                                                self._here(stream)))
         return out
 
     def linear_i8(self, x: torch.Tensor, qw: torch.Tensor, scale_w: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -375,14 +374,16 @@ class Context:
         _vector(scale_w, n)
         _vector(bias, n)
         out = _output(out, (m, n), dtype or x.dtype, x.device, stream)
-        work, size = _work(self.lib.qcfg_linear_i8_work(m, k), x.device, stream)
-        self._check(self.lib.qcfg_linear_i8(self.h, _ptr(x), _dtype(x.dtype), _ld(x), bits, _ptr(qw), _ld(qw), m, n, k, _ptr(scale_w),
-                                            _ptr(bias), act, _ptr(out), _dtype(out.dtype), _ld(out), _ptr(work), size, self._here(stream)))
+        size = self.lib.qcfg_linear_i8_work(m, k)
+        work = _empty(size, torch.uint8, x.device, stream) if size else None
+        self._check(self.lib.qcfg_linear_i8(self.h, x.data_ptr(), _dtype(x.dtype), _ld(x), bits, qw.data_ptr(), _ld(qw), m, n, k,
+                                            scale_w.data_ptr(), _at(bias), act, out.data_ptr(), _dtype(out.dtype), _ld(out), _at(work), size,
+                                            self._here(stream)))
         return out
 
-    def _here(self, stream) -> C.c_void_p:
+    def _here(self, stream) -> int:
         """The stream's handle; without one the current stream of the context's device."""
-        return C.c_void_p((stream if stream is not None else torch.cuda.current_stream(self.device)).cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
 
 
 def _rows_of(x: torch.Tensor, dtype: Optional[torch.dtype] = None):
@@ -407,26 +408,25 @@ def _dtype(t: torch.dtype) -> int:
     return DTYPES[t]
 
 
-def _stream_scope(stream):
-    """Memory allocated inside belongs to the stream that will use it (None: the current one)."""
-    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+def _empty(shape, dtype, device, stream):
+    """Memory that belongs to the stream that will use it (None: the current one)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _output(out, shape, dtype, device, stream):
     if out is None:
         _dtype(dtype)
-        with _stream_scope(stream):
-            return torch.empty(shape, dtype=dtype, device=device)
+        return _empty(shape, dtype, device, stream)
     if tuple(out.shape) != tuple(shape) or out.stride(-1) != 1:
         raise QcfgError(ESHAPE, f"out must be {tuple(shape)} with adjacent columns")
     return out
 
 
-def _work(size: int, device, stream):
-    if size == 0:
-        return None, 0
-    with _stream_scope(stream):
-        return torch.empty(size, dtype=torch.uint8, device=device), size
+def _at(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
 def _int32(x: Optional[torch.Tensor], n: Optional[int] = None):
@@ -450,40 +450,45 @@ class KvPool:
             _int32(t, n)
         self.n_pages, self.page_tokens, self.max_seqs, self.max_pages = n_pages, page_tokens, max_seqs, max_pages
         self._c = PoolStruct(self.table.data_ptr(), self.lens.data_ptr(), self.refs.data_ptr(), n_pages, page_tokens, max_seqs, max_pages)
+        self._ref = C.byref(self._c)
 
-    def _batch(self, seqs: torch.Tensor, starts: Optional[torch.Tensor], rows: int) -> BatchStruct:
+    def _batch(self, seqs: torch.Tensor, starts: Optional[torch.Tensor], rows: int):
         n = seqs.numel()
         _int32(seqs)
-        _int32(starts, n + 1)
         self.ctx._on_device(seqs, starts)
-        return BatchStruct(seqs.data_ptr(), None if starts is None else starts.data_ptr(), n, rows)
+        if starts is None:
+            return C.byref(BatchStruct(seqs.data_ptr(), None, n, rows))
+        _int32(starts, n + 1)
+        return C.byref(BatchStruct(seqs.data_ptr(), starts.data_ptr(), n, rows))
 
     def extend(self, seqs: torch.Tensor, starts: Optional[torch.Tensor] = None, rows: Optional[int] = None, stream=None):
         """Every sequence of `seqs` gets room for its rows (starts[i+1] - starts[i]; one each without starts)."""
-        b = self._batch(seqs, starts, 0x7fffffff - 4096 if rows is None else rows)
-        self.ctx._check(self.ctx.lib.qcfg_kv_extend(self.ctx.h, C.byref(self._c), C.byref(b), self.ctx._here(stream)))
+        ctx = self.ctx
+        ctx._check(ctx.lib.qcfg_kv_extend(ctx.h, self._ref, self._batch(seqs, starts, 0x7fffffff - 4096 if rows is None else rows),
+                                          ctx._here(stream)))
 
     def free(self, seqs: torch.Tensor, stream=None):
+        ctx = self.ctx
         _int32(seqs)
-        self.ctx._on_device(seqs)
-        self.ctx._check(self.ctx.lib.qcfg_kv_free(self.ctx.h, C.byref(self._c), _ptr(seqs), seqs.numel(), self.ctx._here(stream)))
+        ctx._on_device(seqs)
+        ctx._check(ctx.lib.qcfg_kv_free(ctx.h, self._ref, seqs.data_ptr(), seqs.numel(), ctx._here(stream)))
 
     def fork(self, parents: torch.Tensor, children: torch.Tensor, stream=None):
         """Returns (src, dst): the pages that copy_pages has to copy in every layer's cache."""
+        ctx, n = self.ctx, parents.numel()
         _int32(parents)
-        _int32(children, parents.numel())
-        self.ctx._on_device(parents, children)
-        with _stream_scope(stream):
-            src, dst = torch.empty_like(parents), torch.empty_like(parents)
-        self.ctx._check(self.ctx.lib.qcfg_kv_fork(self.ctx.h, C.byref(self._c), _ptr(parents), _ptr(children), parents.numel(), _ptr(src),
-                                                  _ptr(dst), self.ctx._here(stream)))
+        _int32(children, n)
+        ctx._on_device(parents, children)
+        src, dst = _empty((2, n), torch.int32, parents.device, stream).unbind()
+        ctx._check(ctx.lib.qcfg_kv_fork(ctx.h, self._ref, parents.data_ptr(), children.data_ptr(), n, src.data_ptr(), dst.data_ptr(),
+                                        ctx._here(stream)))
         return src, dst
 
     def compact(self, stream=None) -> torch.Tensor:
         """Returns the new number of every page in use, -1 for free ones: copy_pages(None, that) moves the contents."""
-        with _stream_scope(stream):
-            where = torch.empty(2 * self.n_pages, dtype=torch.int32, device=self.refs.device)
-        self.ctx._check(self.ctx.lib.qcfg_kv_compact(self.ctx.h, C.byref(self._c), _ptr(where), self.ctx._here(stream)))
+        ctx = self.ctx
+        where = _empty(2 * self.n_pages, torch.int32, self.refs.device, stream)
+        ctx._check(ctx.lib.qcfg_kv_compact(ctx.h, self._ref, where.data_ptr(), ctx._here(stream)))
         return where[:self.n_pages]
 
 
@@ -504,6 +509,7 @@ class KvCache:
             if tuple(t.shape) != want or t.dtype != dt or not t.is_contiguous():
                 raise QcfgError(ESHAPE, f"a dense {dt} tensor of {want} is needed")
         self._c = CacheStruct(self.k.data_ptr(), self.v.data_ptr(), self.k_absmax.data_ptr(), self.v_absmax.data_ptr(), kv_heads, head_dim)
+        self._ref = C.byref(self._c)
 
     def _heads_of(self, x: torch.Tensor, heads: Optional[int]):
         if x.dim() != 3 or x.shape[2] != self.head_dim or x.stride(2) != 1 or (heads is not None and x.shape[1] != heads):
@@ -511,56 +517,59 @@ class KvCache:
 
     def append(self, k: torch.Tensor, v: torch.Tensor, seqs: torch.Tensor, starts: Optional[torch.Tensor] = None, stream=None):
         """Writes the last tokens of every sequence of the batch (KvPool.extend has made room for them)."""
-        self.ctx._on_device(k, v)
+        ctx = self.ctx
+        ctx._on_device(k, v)
         self._heads_of(k, self.kv_heads)
         self._heads_of(v, self.kv_heads)
-        if k.shape != v.shape or k.dtype != v.dtype or k.stride()[:2] != v.stride()[:2]:
+        strides = k.stride()
+        if k.shape != v.shape or k.dtype != v.dtype or strides != v.stride():
             raise QcfgError(ESHAPE, "keys and values must agree in shape, type and strides")
-        b = self.pool._batch(seqs, starts, k.shape[0])
-        self.ctx._check(self.ctx.lib.qcfg_kv_append(self.ctx.h, C.byref(self.pool._c), C.byref(self._c), C.byref(b), _ptr(k), _ptr(v),
-                                                    _dtype(k.dtype), k.stride(0), k.stride(1), self.ctx._here(stream)))
+        ctx._check(ctx.lib.qcfg_kv_append(ctx.h, self.pool._ref, self._ref, self.pool._batch(seqs, starts, k.shape[0]), k.data_ptr(),
+                                          v.data_ptr(), _dtype(k.dtype), strides[0], strides[1], ctx._here(stream)))
 
     def read(self, seqs: torch.Tensor, first: torch.Tensor, starts: Optional[torch.Tensor], rows: int, dtype: torch.dtype = torch.float32,
              stream=None):
         """Values of the tokens first[i] .. of every sequence, as many as its rows: (k, v), each [rows, kv_heads, head_dim].
         Rows behind the last sequence's are left as they are (unset)."""
-        b = self.pool._batch(seqs, starts, rows)
+        ctx = self.ctx
         _int32(first, seqs.numel())
-        self.ctx._on_device(first)
-        shape = (rows, self.kv_heads, self.head_dim)
-        k, v = (_output(None, shape, dtype, self.k.device, stream) for _ in range(2))
-        self.ctx._check(self.ctx.lib.qcfg_kv_read(self.ctx.h, C.byref(self.pool._c), C.byref(self._c), C.byref(b), _ptr(first), _ptr(k), _ptr(v),
-                                                  _dtype(dtype), self.ctx._here(stream)))
+        ctx._on_device(first)
+        kind = _dtype(dtype)
+        k, v = _empty((2, rows, self.kv_heads, self.head_dim), dtype, self.k.device, stream).unbind()
+        ctx._check(ctx.lib.qcfg_kv_read(ctx.h, self.pool._ref, self._ref, self.pool._batch(seqs, starts, rows), first.data_ptr(), k.data_ptr(),
+                                        v.data_ptr(), kind, ctx._here(stream)))
         return k, v
 
     def copy_pages(self, src: Optional[torch.Tensor], dst: torch.Tensor, stream=None):
         """Page src[i] (i itself without src) to page dst[i]; entries of -1 are passed over."""
+        ctx, n = self.ctx, dst.numel()
         _int32(dst)
-        _int32(src, dst.numel())
-        self.ctx._on_device(src, dst)
-        self.ctx._check(self.ctx.lib.qcfg_kv_copy_pages(self.ctx.h, C.byref(self.pool._c), C.byref(self._c), _ptr(src), _ptr(dst), dst.numel(),
-                                                        self.ctx._here(stream)))
+        _int32(src, n)
+        ctx._on_device(src, dst)
+        ctx._check(ctx.lib.qcfg_kv_copy_pages(ctx.h, self.pool._ref, self._ref, _at(src), dst.data_ptr(), n, ctx._here(stream)))
 
     def attention(self, q: torch.Tensor, seqs: torch.Tensor, starts: Optional[torch.Tensor] = None, sm_scale: Optional[float] = None,
                   causal: bool = True, window: int = 0, max_new: int = 0, max_len: int = 0, out: Optional[torch.Tensor] = None,
                   stream=None) -> torch.Tensor:
         """softmax(sm_scale * q k^T) v of the last tokens of every sequence: q [rows, q_heads, head_dim], out like q.
         sm_scale: 1 / sqrt(head_dim) unless given; max_new, max_len: the longest entry and sequence, where known."""
-        self.ctx._on_device(q, out)
+        ctx, shape = self.ctx, q.shape
+        ctx._on_device(q, out)
         self._heads_of(q, None)
+        kind = _dtype(q.dtype)
         if out is None:
-            out = _output(None, q.shape, q.dtype, q.device, stream)
-        self._heads_of(out, q.shape[1])
-        if out.dtype != q.dtype or out.shape != q.shape:
-            raise QcfgError(ESHAPE, "out must be like q")
-        b = self.pool._batch(seqs, starts, q.shape[0])
-        lib, h = self.ctx.lib, self.ctx.h
-        work, size = _work(lib.qcfg_kv_attention_work(h, C.byref(self._c), b.n, b.n_rows, q.shape[1]), q.device, stream)
-        self.ctx._check(lib.qcfg_kv_attention(h, C.byref(self.pool._c), C.byref(self._c), C.byref(b), _ptr(q), q.stride(0), q.stride(1), q.shape[1],
-                                              _ptr(out), out.stride(0), out.stride(1), _dtype(q.dtype), max_new, max_len,
-                                              self.head_dim ** -0.5 if sm_scale is None else float(sm_scale), int(causal), window, _ptr(work), size,
-                                              self.ctx._here(stream)))
+            out = _empty(shape, q.dtype, q.device, stream)
+        elif out.dtype != q.dtype or out.shape != shape or out.stride(2) != 1:
+            raise QcfgError(ESHAPE, "out must be like q, with adjacent elements")
+        size = ctx.lib.qcfg_kv_attention_work(ctx.h, self._ref, shape[0], max_len)
+        work = _empty(size, torch.uint8, q.device, stream) if size else None
+        qs, os_ = q.stride(), out.stride()
+        ctx._check(ctx.lib.qcfg_kv_attention(ctx.h, self.pool._ref, self._ref, self.pool._batch(seqs, starts, shape[0]), q.data_ptr(), qs[0], qs[1],
+                                             shape[1], out.data_ptr(), os_[0], os_[1], kind, max_new, max_len,
+                                             self.head_dim ** -0.5 if sm_scale is None else sm_scale, causal, window, _at(work), size,
+                                             ctx._here(stream)))
         return out
+
 
 class Model:
     """Owns one qcfg_model built from a list of layer descriptions and device weights."""

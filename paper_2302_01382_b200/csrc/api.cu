@@ -1256,9 +1256,9 @@ int qcfg_kv_read(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* c
   return launch_kv_read(c, view(pool), view(cache), view(batch), first_dev, k_dev, v_dev, dtype, (cudaStream_t)stream);
 }
 
-int64_t qcfg_kv_attention_work(qcfg_ctx* ctx, const qcfg_kv_cache* cache, int32_t n, int64_t n_rows, int32_t q_heads) {
-  if (!ctx || !cache || n <= 0 || n_rows <= 0 || q_heads <= 0) return 0;
-  return kv_attention_work(&ctx->c, view(cache), n, n_rows, q_heads);
+int64_t qcfg_kv_attention_work(qcfg_ctx* ctx, const qcfg_kv_cache* cache, int64_t n_rows, int32_t max_len) {
+  if (!ctx || !cache || n_rows <= 0) return 0;
+  return kv_attention_work(&ctx->c, view(cache), max_len);
 }
 
 int qcfg_kv_attention(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch, const void* q_dev,
@@ -1282,7 +1282,7 @@ int qcfg_kv_attention(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cac
   if ((uintptr_t)q_dev % 16 || (uintptr_t)out_dev % 16 || (q_row_stride * es) % 16 || (q_head_stride * es) % 16 || (out_row_stride * es) % 16 ||
       (out_head_stride * es) % 16)
     return set_error(c, QCFG_EALIGN, "kv_attention: pointers and strides must be multiples of 16 bytes");
-  const int64_t need = qcfg_kv_attention_work(ctx, cache, batch->n, batch->n_rows, q_heads);
+  const int64_t need = qcfg_kv_attention_work(ctx, cache, batch->n_rows, max_len);
   if (need > 0 && (!work_dev || work_bytes < need)) return set_error(c, QCFG_EINVAL, "kv_attention: %lld bytes of working memory needed", (long long)need);
   if (need > 0 && (uintptr_t)work_dev % 256) return set_error(c, QCFG_EALIGN, "kv_attention: working memory must be 256-byte aligned");
   DeviceScope dev(c);

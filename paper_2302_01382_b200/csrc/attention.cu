@@ -22,6 +22,7 @@ struct AttnArgs {
   void* out;
   int64_t q_row, q_head, o_row, o_head;
   int q_heads, causal, window;
+  int uncut;                // every tile to one block (see kUncutTokens)
   float scale;              // sm_scale * log2(e)
   void* work;
   unsigned* err;
@@ -149,7 +150,7 @@ __device__ __forceinline__ Entry entry_of(const AttnArgs& a, int i) {
   e.units = kSetup + (e.len ? (e.len + kUnit - 1) / kUnit : 1);
   return e;
 }
-__device__ __forceinline__ int64_t entry_units(const AttnArgs& a, const Entry& e) { return (int64_t)e.tiles * e.units * a.cache.heads; }
+__device__ __forceinline__ int64_t entry_units(const AttnArgs& a, const Entry& e) { return (int64_t)e.tiles * (a.uncut ? 1 : e.units) * a.cache.heads; }
 
 // a / b of numbers that are not negative: 64-bit divisions take a hundred instructions, and both fit 32 bits but in huge batches
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
@@ -159,8 +160,8 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 struct Shares {
   int64_t each;
   int more, blocks;
-  __device__ __forceinline__ Shares(int64_t total, int grid) {
-    blocks = (int)max((int64_t)1, min((int64_t)grid, quotient(total, kSetup + kMinUnits)));
+  __device__ __forceinline__ Shares(int64_t total, int grid, int least) {
+    blocks = (int)max((int64_t)1, min((int64_t)grid, quotient(total, least)));
     each = quotient(total, blocks);
     more = (int)(total - each * blocks);
   }
@@ -213,9 +214,9 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
     scan_units(units_of(i0 + tid), sum);
     total += sum;
   }
-  const Shares shares(total, gridDim.x);
+  const Shares shares(total, gridDim.x, a.uncut ? 1 : kSetup + kMinUnits);
   const int me = blockIdx.x;
-  if (tid == 0) meta[me].first = -1;
+  if (tid == 0 && !a.uncut) meta[me].first = -1;
   if (me >= shares.blocks || total == 0) return;
   int64_t at = shares.first(me);
   const int64_t end = shares.first(me + 1);
@@ -249,9 +250,10 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
       entry_at += entry_units(a, E);
       E = entry_of<NR>(a, ++entry);
     }
-    const int64_t item = quotient(at - entry_at, E.units);
-    const int v0 = (int)(at - entry_at - item * E.units), v1 = (int)min((int64_t)E.units, v0 + (end - at));
-    const int n_units = E.units - kSetup, u0 = max(v0 - kSetup, 0), u1 = max(v1 - kSetup, 0);
+    const int per_tile = a.uncut ? 1 : E.units, n_units = E.units - kSetup;
+    const int64_t item = quotient(at - entry_at, per_tile);
+    const int v0 = (int)(at - entry_at - item * per_tile), v1 = (int)min((int64_t)per_tile, v0 + (end - at));
+    const int u0 = a.uncut ? 0 : max(v0 - kSetup, 0), u1 = a.uncut ? n_units : max(v1 - kSetup, 0);
     at += v1 - v0;
     if (u1 == 0) continue;                                 // ends before the tile's first token
     if (tid == 0 && E.s >= a.pool.max_seqs) atomicOr(a.err, ERR_PAGE);
@@ -746,8 +748,11 @@ int stream_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return check_cuda(ctx, e, "kv_attention");
   const int grid = std::min(sm_count(ctx) * stream_blocks<DP, NR>(), kMaxStreamGrid);
   launch_pdl(kv_attention_stream<T, DP, NR>, dim3(grid), dim3(32 * kStreamWarps), smem, st, a);
-  launch_pdl(kv_attention_join<T, DP, NR>, dim3(grid, DP / 16), dim3(32 * NR * kJoinWays), 0, st, a);
-  count_launch(ctx, 2);
+  count_launch(ctx);
+  if (!a.uncut) {
+    launch_pdl(kv_attention_join<T, DP, NR>, dim3(grid, DP / 16), dim3(32 * NR * kJoinWays), 0, st, a);
+    count_launch(ctx);
+  }
   return check_cuda(ctx, cudaGetLastError(), "kv_attention");
 }
 // rows: of the longest entry, as far as known
@@ -765,15 +770,20 @@ int stream_of(Ctx* ctx, const AttnArgs& a, int64_t rows, cudaStream_t st) {
 
 }  // namespace
 
-int64_t kv_attention_work(Ctx*, const CacheView& c, int, int64_t, int) {
+// Contexts known to be no longer than this are not cut: the second kernel and its working memory cost more than an uneven load.
+constexpr int kUncutTokens = 512;
+
+int64_t kv_attention_work(Ctx*, const CacheView& c, int max_len) {
+  if (max_len > 0 && max_len <= kUncutTokens) return 0;
   return c.dim <= 64 ? stream_work<64, 4>() : c.dim <= 128 ? stream_work<128, 4>() : stream_work<256, 2>();
 }
 
 int launch_kv_attention(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const void* q, int64_t q_row, int64_t q_head,
-                        int q_heads, void* out, int64_t o_row, int64_t o_head, int dtype, int max_rows, int, float scale, int causal, int window,
+                        int q_heads, void* out, int64_t o_row, int64_t o_head, int dtype, int max_rows, int max_len, float scale, int causal, int window,
                         void* work, cudaStream_t st) {
   if (b.n == 0 || b.rows == 0) return QCFG_OK;
-  const AttnArgs a{p, c, b, q, out, q_row, q_head, o_row, o_head, q_heads, causal, window, scale * 1.44269504088896f, work, err_word(ctx)};
+  const int uncut = max_len > 0 && max_len <= kUncutTokens;
+  const AttnArgs a{p, c, b, q, out, q_row, q_head, o_row, o_head, q_heads, causal, window, uncut, scale * 1.44269504088896f, work, err_word(ctx)};
   int64_t rows = !b.starts ? 1 : max_rows > 0 ? max_rows : (b.rows + b.n - 1) / b.n;
   rows *= q_heads / c.heads;
   return dtype == QCFG_FP32 ? stream_of<float>(ctx, a, rows, st) : dtype == QCFG_BF16 ? stream_of<__nv_bfloat16>(ctx, a, rows, st)

@@ -52,7 +52,7 @@ int launch_kv_read(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchV
                    cudaStream_t st);
 
 // ----- attention.cu ---------------------------------------------------------------------
-int64_t kv_attention_work(Ctx* ctx, const CacheView& c, int n, int64_t rows, int q_heads);
+int64_t kv_attention_work(Ctx* ctx, const CacheView& c, int max_len);
 int launch_kv_attention(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const void* q, int64_t q_row, int64_t q_head,
                         int q_heads, void* out, int64_t o_row, int64_t o_head, int dtype, int max_rows, int max_len, float scale, int causal,
                         int window, void* work, cudaStream_t st);

@@ -456,6 +456,7 @@ def test_attention_of_single_tokens(ctx, page, q_heads, heads, dim, dtype):
     check_attention(ctx, cache, co, order, ones, q_heads, dtype, rng, behind=3, layout="packed", max_new=1, max_len=700)
     check_attention(ctx, cache, co, order, ones, q_heads, dtype, rng, layout="heads", window=page + 2, sm_scale=0.3)
     check_attention(ctx, cache, co, [6], [1], q_heads, dtype, rng, causal=False)
+    check_attention(ctx, cache, co, order, ones, q_heads, dtype, rng, max_new=1, max_len=300)      # a hint that is wrong
 
 
 @pytest.mark.parametrize("page,q_heads,heads,dim", CACHES)
