@@ -130,6 +130,9 @@ struct GemmArgs {
   const float* residual; int64_t ldr;  // optional fp32 addend (before act)
   int32_t* acc;                 // optional raw accumulators (int8 only) [m x n]
   CodeSlot slots[kMaxSlots];
+  const float* scale_rows = nullptr;   // optional, int8 only: a scale for each row in place of scale_x (then with `bias`, [n] or null,
+  const float* bias = nullptr;         // and y of the type y_kind: 3 fp32, 2 bf16, 5 fp16; no other output, alone in its launch)
+  int y_kind = 3;
   float* amax = nullptr;        // optional: max |output| (after shortcut and activation) is folded into *amax, which
                                 // the caller has set to zero (calibration: the range of the consumers' input)
   // implicit-GEMM convolution (conv_kh > 0): `a` is the NHWC code tensor [batch*H*W x C] of the layer's

@@ -28,6 +28,8 @@
 #include <unordered_map>
 
 #include "common.cuh"
+#include <cuda_fp16.h>
+
 #include "ptx.cuh"
 
 namespace qcfg {
@@ -125,7 +127,12 @@ struct SlabDesc {
 constexpr int kMaxSlabs = 4;
 constexpr int kSlabRoom = kSmemMax - kSmemHeader - kCsBytes - 1024;      // shared memory for slabs and weights
 constexpr int kMaxDeps = 4;
+struct TokenDesc {            // FL_TOKEN: a scale for each row, an addend for each column (or null)
+  const float* scale_rows;
+  const float* bias;
+};
 struct GemmParams {
+  TokenDesc token;
   int32_t m, k_blocks, bn, tiles_m, tiles_n, stages, is_bf16;   // tiles_n: column tiles of all groups together
   int32_t epi_bytes;          // staging bytes per epilogue warp
   int32_t alternate;          // tiles of 64 columns: half of the epilogue warps take the even tiles, half the odd ones
@@ -897,6 +904,106 @@ __device__ __forceinline__ void epilogue_rows(const GroupDesc& G, uint32_t tbase
   }
 }
 
+// One warp's 32 rows of a layer with a scale for each row (FL_TOKEN): act(float(acc) * (sx * sw) + bias), the product of the scales
+// first.  sw, bias: the warp's columns; sx: this lane's row.  32 columns at a time, through one staging slot: by TMA (rows of 128
+// bytes, 128B swizzle, or of 64 bytes, 64B swizzle), or, where rows are not 16-byte aligned, row by row with an element per lane.
+template <bool PAIR>
+__device__ __forceinline__ void epilogue_token(const GroupDesc& G, const CUtensorMap* map, uint32_t tbase, const float* sw, const float* bias, float sx,
+                                               uint32_t stage, int nch, int m, int row0, int col0, int lane, uint32_t tempty_bar) {
+  const OutDesc& o = G.outs[1];
+  const int act = G.act;
+  const bool wide = o.kind == 3;
+  const float2 sx2 = make_float2(sx, sx);
+#pragma unroll 1
+  for (int c = 0; c < nch; ++c) {
+    uint32_t v[32];
+    tmem_ld32_issue(tbase + 32 * c, v);
+    if (o.tma) {         // the slot's last store has read it
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      __syncwarp();
+    }
+    tmem_ld_wait();
+    if (c == nch - 1) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) { if (PAIR) mbar_arrive_leader(tempty_bar); else mbar_arrive(tempty_bar); }
+    }
+    const float4* sw4 = reinterpret_cast<const float4*>(sw + 32 * c);
+    const float4* b4 = reinterpret_cast<const float4*>(bias + 32 * c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {          // eight columns
+      uint32_t w[8];
+      float2 y[4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float4 s = sw4[2 * j + i], b = b4[2 * j + i];
+        const uint32_t* a = v + 8 * j + 4 * i;
+        y[2 * i] = __fadd2_rn(__fmul2_rn(make_float2((float)(int32_t)a[0], (float)(int32_t)a[1]), __fmul2_rn(sx2, make_float2(s.x, s.y))), make_float2(b.x, b.y));
+        y[2 * i + 1] = __fadd2_rn(__fmul2_rn(make_float2((float)(int32_t)a[2], (float)(int32_t)a[3]), __fmul2_rn(sx2, make_float2(s.z, s.w))), make_float2(b.z, b.w));
+      }
+      if (act == QCFG_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = make_float2(fmaxf(y[i].x, 0.0f), fmaxf(y[i].y, 0.0f));
+      } else if (act == QCFG_ACT_GELU_TANH) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = gelu_tanh2(y[i]);
+      }
+      if (wide) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          st_shared_v4(stage + lane * 128 + (((2 * j + i) ^ (lane & 7)) << 4), __float_as_uint(y[2 * i].x), __float_as_uint(y[2 * i].y),
+                       __float_as_uint(y[2 * i + 1].x), __float_as_uint(y[2 * i + 1].y));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (o.kind == 2) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(y[i].x, y[i].y);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+          } else {
+            const __half2 h = __floats2half2_rn(y[i].x, y[i].y);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+        }
+        st_shared_v4(stage + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
+      }
+    }
+    const int left = G.n - col0 - 32 * c;
+    if (left <= 0) continue;
+    if (o.tma) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) tma_store_2d(map, stage, col0 + 32 * c, row0);
+      continue;
+    }
+    __syncwarp();
+    const int64_t at = (int64_t)row0 * o.ld + col0 + 32 * c + lane;
+    const int rows = m - row0 < 32 ? m - row0 : 32;
+    constexpr int kBatch = 8;              // reads first, then stores
+#pragma unroll 1
+    for (int r = 0; r < 32; r += kBatch) {
+      uint32_t x[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int q = r + i;
+        if (wide) {
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x[i]) : "r"(stage + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4));
+        } else {
+          unsigned short h;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(stage + q * 64 + (((lane >> 3) ^ ((q >> 1) & 3)) << 4) + (lane & 7) * 2));
+          x[i] = h;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (r + i >= rows || lane >= left) continue;
+        if (wide) reinterpret_cast<uint32_t*>(o.ptr)[at + (r + i) * o.ld] = x[i];
+        else reinterpret_cast<unsigned short*>(o.ptr)[at + (r + i) * o.ld] = (unsigned short)x[i];
+      }
+    }
+    __syncwarp();
+  }
+}
+
 // ---------------------------------------------------------------------------- the kernel
 
 // One launch runs one GEMM record or, in the CHAIN flavour, up to kChainMax records one after the
@@ -914,7 +1021,7 @@ __device__ __forceinline__ void epilogue_rows(const GroupDesc& G, uint32_t tbase
 // FL: what the single-GEMM flavours carry besides the plain matrix product.  Convolutions and shortcut layers have
 // instantiations of their own: their code inside the plain kernel slowed its short launches by a tenth to a fifth
 // (100352 x 128 x 512: 20.0 -> 24.5 us).
-enum : int { FL_PLAIN = 0, FL_CONV = 1, FL_SHORTCUT = 2, FL_SLAB = 3, FL_SLAB64 = 4, FL_ROWS = 5 };
+enum : int { FL_PLAIN = 0, FL_CONV = 1, FL_SHORTCUT = 2, FL_SLAB = 3, FL_SLAB64 = 4, FL_ROWS = 5, FL_TOKEN = 6 };
 template <bool BF16, bool PAIR, bool GROUPED, bool CHAIN, int FL = FL_PLAIN>
 __global__ void __launch_bounds__(FL == FL_CONV || CHAIN ? kGemmThreadsConv : kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
@@ -1477,7 +1584,7 @@ gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
     while (inflight > 0) landed();
   } else {
     // ------------------------------------------------------------------ epilogue
-    constexpr bool kRowsOut = FL == FL_ROWS;
+    constexpr bool kRowsOut = FL == FL_ROWS, kToken = FL == FL_TOKEN;
     const int ew = warp - 2;
     const int quad = warp & 3;                 // TMEM lanes 32*quad .. 32*quad+31 belong to this warp
     const bool alternate = !PAIR && !GROUPED && !CHAIN && FL != FL_SHORTCUT && p.alternate;
@@ -1518,7 +1625,16 @@ gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
         if (c_begin + j < c_end && col < G.n) w[j] = __ldg(G.scale_w + col);
       }
     };
-    float sw_next[2];
+    float sw_next[2], bias_next[2] = {0.f, 0.f}, sx_next = 0.f;
+    auto load_token = [&](int tile_tm, int tile_tn) {      // the same for the addends and this lane's row
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int col = tile_tn * p.bn + (c_begin + j) * 32 + lane;
+        bias_next[j] = p.token.bias && c_begin + j < c_end && col < q->grp[0].n ? __ldg(p.token.bias + col) : 0.0f;
+      }
+      const int row = tile_tm * rows_per_tile + rank * BM + quad * 32 + lane;
+      sx_next = row < q->m ? __ldg(p.token.scale_rows + row) : 0.0f;
+    };
     // shortcut blocks: brought in one tile ahead, into the two blocks in turn
     const bool shortcut = FL == FL_SHORTCUT && c_begin < c_end;
     const uint32_t res_bar0 = smem_u32(smem + kResBarOffset) + 16 * ew;
@@ -1547,6 +1663,7 @@ gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
       }
     } else {
       load_scales(q, tile < num_tiles, tn, sw_next);
+      if (kToken && tile < num_tiles) load_token(tm, tn);
     }
     for (; tile < total_tiles && (ok || kRowsOut); tile += e_step, t += alternate ? 2 : 1) {
       if (CHAIN) {     // record of this tile, column tile fastest inside it
@@ -1571,6 +1688,17 @@ gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
       } else {
         wrap(tm_next, tn_next);
         load_scales(q, tile + e_step < num_tiles, tn_next, sw_next);
+      }
+      float sx = 0.f;
+      if (kToken) {
+        sx = sx_next;
+        float* bias_tab = reinterpret_cast<float*>(epi_stage + ew * p.epi_bytes + 4096);
+        cs_tab[lane] = cs[0];
+        cs_tab[32 + lane] = cs[1];
+        bias_tab[lane] = bias_next[0];
+        bias_tab[32 + lane] = bias_next[1];
+        __syncwarp();
+        if (tile + e_step < num_tiles) load_token(tm_next, tn_next);
       }
       // Chains: the previous tile is reported once its stores have completed.  When this tile's
       // accumulator is already there the check is left to the body (after its first piece, when
@@ -1622,6 +1750,15 @@ gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
         else if (ok) {
           __syncwarp();
           if (lane == 0) { if (PAIR) mbar_arrive_leader(tempty_bar); else mbar_arrive(tempty_bar); }
+        }
+        __syncwarp();
+      } else if (kToken) {
+        if (nch == 0 || row0 >= q->m || col_base >= G.n) {
+          __syncwarp();
+          if (lane == 0) { if (PAIR) mbar_arrive_leader(tempty_bar); else mbar_arrive(tempty_bar); }
+        } else {
+          epilogue_token<PAIR>(G, &mp[MAP_FAST], tbase, cs_tab, reinterpret_cast<const float*>(epi_stage + ew * p.epi_bytes + 4096), sx, stage, nch, q->m, row0,
+                               col_base, lane, tempty_bar);
         }
         __syncwarp();
       } else if (kSlab) {
@@ -1939,6 +2076,13 @@ bool make_out_map(CUtensorMap* map, const OutDesc& o, int64_t m, int64_t n) {
 
 // Tensor map of the output a fast epilogue body writes: 32-row boxes of 64 int8 columns (64B
 // swizzle), of 64 bf16 or of 32 fp32 columns (128B swizzle).
+// FL_TOKEN: pieces of 32 rows x 32 columns
+bool make_token_map(CUtensorMap* map, const OutDesc& o, int64_t m, int64_t n) {
+  const int esz = o.kind == 3 ? 4 : 2;
+  if (((uintptr_t)o.ptr & 15) || ((o.ld * esz) & 15)) return false;
+  return encode_2d(map, o.kind == 3 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, o.ptr, (uint64_t)n, (uint64_t)m, (uint64_t)(o.ld * esz),
+                   32u, 32u, o.kind == 3 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
+}
 bool make_fast_map(CUtensorMap* map, const OutDesc& o, int64_t m, int64_t n) {
   const bool codes = o.kind == 1, half = o.kind == 2;
   const int esz = codes ? 1 : half ? 2 : 4;
@@ -2302,6 +2446,7 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
   p.bn = bn;
   // pair flavour (two CTAs per 256-row tile, cta_group::2) for wide outputs with at least two
   // row tiles: it halves the B bytes each SM stages per k-block
+  const bool token = count == 1 && g0.scale_rows != nullptr;
   bool pair = ctx_pair_enabled(ctx) && bn == 256 && (slab ? row_tiles > 1 && sd.chunk == 128 : g0.m > BM) && sm_count(ctx) >= 2;
   // ... and for wide outputs whose tiles were narrowed to 128 columns, while the pairs still have one tile each: a
   // stage is 24 KB instead of 32 and the ring one or two stages deeper (noise table of the block above:
@@ -2353,7 +2498,12 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
     }
     if (!G.need_y && !G.outs[0].kind) return set_error(ctx, QCFG_EINVAL, "gemm: no output requested");
     if (G.need_y && !g.is_bf16 && !g.scale_w) return set_error(ctx, QCFG_EINVAL, "gemm: scale_w is null");
-    for (int j = 0; j < kNumOuts; ++j)
+    if (token) {
+      G.outs[1].kind = g.y_kind;
+      G.outs[1].tma = make_token_map(&maps[MAP_FAST], G.outs[1], g.m, g.n) ? 1 : 0;
+      p.token = {g.scale_rows, g.bias};
+    }
+    for (int j = 0; j < kNumOuts && !token; ++j)
       if (G.outs[j].kind) G.outs[j].tma = make_out_map(&maps[i * kMapsPerGroup + MAP_OUT + j], G.outs[j], g.m, g.n) ? 1 : 0;
     // staging per epilogue warp: two slots of 1 KB when only int8 codes are written, else of 2 KB
     for (int j = 0; j < kNumOuts; ++j) if (G.outs[j].kind >= 3 || (G.outs[j].kind == 2 && G.outs[j].tma)) wide = true;
@@ -2364,11 +2514,11 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
     if (bn == 256 && !G.residual && !G.outs[0].kind && !G.outs[1].kind && G.outs[2].kind == 2 && !G.outs[3].kind && !G.outs[4].kind &&
         make_fast_map(&maps[i * kMapsPerGroup + MAP_FAST], G.outs[2], g.m, g.n))
       G.mode = EPI_BF16;
-    if (bn == 256 && !G.residual && !G.amax && !G.outs[0].kind && !G.outs[3].kind && !G.outs[4].kind) {
+    if (bn == 256 && !token && !G.residual && !G.amax && !G.outs[0].kind && !G.outs[3].kind && !G.outs[4].kind) {
       if (!G.outs[1].kind && G.outs[2].kind == 1 && make_fast_map(&maps[i * kMapsPerGroup + MAP_FAST], G.outs[2], g.m, g.n)) G.mode = EPI_CODES1;
       else if (G.outs[1].kind && !G.outs[2].kind && make_fast_map(&maps[i * kMapsPerGroup + MAP_FAST], G.outs[1], g.m, g.n)) { G.mode = EPI_Y; wide = true; }
     }
-    if (bn < 256 && (!pair || count > 1) && !shortcut && !g.is_bf16 && g.conv_kh == 0 && !G.residual && !G.amax && !G.outs[0].kind && G.outs[1].kind && !G.outs[2].kind && !G.outs[3].kind &&
+    if (bn < 256 && !token && (!pair || count > 1) && !shortcut && !g.is_bf16 && g.conv_kh == 0 && !G.residual && !G.amax && !G.outs[0].kind && G.outs[1].kind && !G.outs[2].kind && !G.outs[3].kind &&
         !G.outs[4].kind && make_fast_map(&maps[i * kMapsPerGroup + MAP_FAST], G.outs[1], g.m, g.n))
       G.mode = EPI_Y32;
     if (shortcut) {      // MAP_OUT, the raw accumulators' place, holds the shortcut's map
@@ -2387,7 +2537,7 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
   }
   p.tiles_n = tn_total;
   // an fp32 matrix that TMA cannot write, in whole 256-column tiles, and nothing else (narrower tiles keep the general body)
-  const bool rows_out = count == 1 && bn == 256 && rows_body_pays(g0) && g0.conv_kh == 0 && !g0.residual && !g0.amax && !p.grp[0].outs[0].kind && p.grp[0].outs[1].kind &&
+  const bool rows_out = count == 1 && !token && bn == 256 && rows_body_pays(g0) && g0.conv_kh == 0 && !g0.residual && !g0.amax && !p.grp[0].outs[0].kind && p.grp[0].outs[1].kind &&
                         !p.grp[0].outs[1].tma && !p.grp[0].outs[2].kind && !p.grp[0].outs[3].kind && !p.grp[0].outs[4].kind;
   const bool conv = g0.conv_kh > 0;
   if (conv) {
@@ -2414,10 +2564,10 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
   if (!cs) return set_error(ctx, QCFG_ESTATE, "gemm: context not initialised");
   // (a GEMM with fewer tiles than CTA pairs has nothing to overlap with: the wait for its
   // producer's rows would cost more than the launch boundary it saves)
-  const bool chainable = cs->open && ctx_chain_enabled(ctx) && pair && !conv && !rows_out && bn == 256 && prof_mode(ctx) != 1 && p.tiles_m <= kChainMaxTilesM &&
+  const bool chainable = cs->open && !token && ctx_chain_enabled(ctx) && pair && !conv && !rows_out && bn == 256 && prof_mode(ctx) != 1 && p.tiles_m <= kChainMaxTilesM &&
                          2 * p.tiles_m * p.tiles_n >= sm_count(ctx);
   p.alternate = !pair && bn == 64 && (slab || p.grp[0].mode == EPI_CODES32);
-  p.epi_bytes = slab ? 0 : shortcut ? kShortcutBytes : (wide || chainable) ? 4096 : 2048;
+  p.epi_bytes = slab ? 0 : token ? 4096 + 1024 : shortcut ? kShortcutBytes : (wide || chainable) ? 4096 : 2048;
   if (slab) {
     if (sd.resident && (pair || p.tiles_n != 1)) return set_error(ctx, QCFG_ESHAPE, "gemm: resident weights need one column tile");
     p.slab = sd;
@@ -2599,7 +2749,7 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
                                        gemm_kernel<false, true, false, false, FL_SLAB>};
   static const Kern rows_kernels[4] = {gemm_kernel<false, false, false, false, FL_ROWS>, gemm_kernel<false, true, false, false, FL_ROWS>,
                                        gemm_kernel<true, false, false, false, FL_ROWS>, gemm_kernel<true, true, false, false, FL_ROWS>};
-  const Kern kern = rows_out ? rows_kernels[(g0.is_bf16 ? 2 : 0) + (pair ? 1 : 0)] : slab ? slab_kernels[sd.chunk == 64 ? 0 : pair ? 2 : 1] : shortcut ? gemm_kernel<false, false, false, false, FL_SHORTCUT>
+  const Kern kern = token ? (pair ? gemm_kernel<false, true, false, false, FL_TOKEN> : gemm_kernel<false, false, false, false, FL_TOKEN>) : rows_out ? rows_kernels[(g0.is_bf16 ? 2 : 0) + (pair ? 1 : 0)] : slab ? slab_kernels[sd.chunk == 64 ? 0 : pair ? 2 : 1] : shortcut ? gemm_kernel<false, false, false, false, FL_SHORTCUT>
                     : conv   ? conv_kernels[(g0.is_bf16 ? 2 : 0) + (pair ? 1 : 0)]
                              : kernels[(g0.is_bf16 ? 4 : 0) + (pair ? 2 : 0) + (count > 1 ? 1 : 0)];
   if (conv) count_form(ctx, p.conv.on == CONV_GATHER ? QCFG_FORM_CONV_GATHER : !slab ? QCFG_FORM_CONV_IM2COL : sd.resident ? QCFG_FORM_CONV_SLAB : QCFG_FORM_CONV_STREAMED);
