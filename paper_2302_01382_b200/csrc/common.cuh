@@ -133,6 +133,8 @@ struct GemmArgs {
   const float* scale_rows = nullptr;   // optional, int8 only: a scale for each row in place of scale_x (then with `bias`, [n] or null,
   const float* bias = nullptr;         // and y of the type y_kind: 3 fp32, 2 bf16, 5 fp16; no other output, alone in its launch)
   int y_kind = 3;
+  int64_t a_rows = 0;           // rows of `a` that can be read, where there are more than m: a TMA load that ends inside 32 rows is slow
+                                // (24 rows 21.1 us, 32 rows 12.2, at n = 16384 and k = 4096)
   float* amax = nullptr;        // optional: max |output| (after shortcut and activation) is folded into *amax, which
                                 // the caller has set to zero (calibration: the range of the consumers' input)
   // implicit-GEMM convolution (conv_kh > 0): `a` is the NHWC code tensor [batch*H*W x C] of the layer's

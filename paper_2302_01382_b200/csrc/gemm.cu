@@ -2530,7 +2530,7 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
         if (G.outs[j].kind && !G.outs[j].tma) return set_error(ctx, QCFG_ECUDA, "cuTensorMapEncodeTiled failed");
       G.mode = EPI_SHORTCUT;
     }
-    int rc = g.conv_kh > 0 ? QCFG_OK : make_map(ctx, &maps[i * kMapsPerGroup + MAP_A], g.a, g.is_bf16, g.k, g.m, g.lda, BM);
+    int rc = g.conv_kh > 0 ? QCFG_OK : make_map(ctx, &maps[i * kMapsPerGroup + MAP_A], g.a, g.is_bf16, g.k, g.a_rows > g.m ? g.a_rows : g.m, g.lda, BM);
     if (rc == QCFG_OK) rc = make_map(ctx, &maps[i * kMapsPerGroup + MAP_B], g.b, g.is_bf16, g.k, g.n, g.ldb, pair ? bn / 2 : bn, slab ? sd.chunk : kStageKBytes);
     if (rc != QCFG_OK) return rc;
     ops += 2.0 * (double)g.m * (double)g.n * (double)g.k;

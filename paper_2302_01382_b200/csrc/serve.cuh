@@ -67,6 +67,7 @@ struct TokenGemm {       // y = act(float(qx qw^T) * (sx[m] * sw[n]) + bias[n])
   const float* bias;     // optional
   int act;
   void* y; int dtype; int64_t ldy;
+  int64_t rows = 0;      // rows of qx that can be read, where there are more than m
 };
 int launch_quantize_tokens(Ctx* ctx, const void* x, int dtype, int64_t rows, int64_t cols, int64_t ld, int bits, int8_t* q, int64_t ldq, float* scale,
                            cudaStream_t st);

@@ -87,22 +87,23 @@ __global__ void __launch_bounds__(kTokenThreads) quantize_tokens_kernel(const T*
 
 // ---- a few tokens: the weights are the traffic ---------------------------------------------------
 //
-// acc^T = W X^T with the 16 weight rows of a unit as the rows of an MMA (int8, sums exact in any order) and the tokens as its columns,
-// NT tiles of 8.  One block per SM; its 16 warps share a unit's reduction, 128 bytes of a row at a time, and add up through shared
-// memory.  A warp keeps the next kAhead steps (64 bytes of 16 rows) of weights on their way to its registers: 16 warps x 4 x 1 KB in
-// flight per SM, asked for once and never cached in L1, where the tokens' codes stay.  A step's 16 bytes of a lane are
-// operand words of two products as they lie in memory, of the weights and of the codes alike, since the sum may run in any order.
+// acc^T = W X^T with 16 weight rows as the rows of an MMA (int8, sums exact in any order) and the tokens as its columns, NT tiles of 8.
+// One block per SM; it takes up to few_tiles<NT>() tiles of 16 rows at once, its 16 warps share their reduction, every 16th run of 128
+// bytes to a warp, and add up through shared memory once at the end (a sum behind each tile of 16 rows cost as much as its weights).
+// A step is one run of one tile, 2 KB: a warp copies it (cp.async) in whole lines into its own ring of kAhead steps, chunk c of row r at
+// c ^ (r & 7), and takes the MMAs' operands from there with ldmatrix.  96 KB of weights are in flight per SM; the tokens' codes come from L1.
 // Behind quantize_tokens (early) the first weights are fetched before its end: it lets this kernel begin only after everything in front
 // of it has completed, so the weights are there.
 // With X_RAW the tokens come as they are, and every block turns them into codes in shared memory while its first weights arrive.
-constexpr int kFewWarps = 16, kAhead = 4;
+constexpr int kFewWarps = 16, kAhead = 4, kStep = 2048;
+constexpr int kRingBytes = kFewWarps * kAhead * kStep;
 constexpr int kRawElements = 16384, kRawTokens = 8;      // X_RAW up to this many
-
-__device__ __forceinline__ uint4 load_once(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+template <int NT> __host__ __device__ constexpr int few_tiles() { return 8; }      // accumulators: NT x 4 registers each
+template <int NT> __host__ __device__ constexpr int sum_tiles() { return 4; }      // tiles added up at a time
+template <int NT> __host__ __device__ constexpr int few_bytes() {      // the ring, and the sums in its place once it is empty
+  return kRingBytes > kFewWarps * sum_tiles<NT>() * NT * 512 ? kRingBytes : kFewWarps * sum_tiles<NT>() * NT * 512;
 }
+
 __device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -121,6 +122,7 @@ __host__ __device__ constexpr int raw_pitch(int64_t k) { return (int)((k + 15) /
 
 template <typename TX, typename TY, int NT, bool X_RAW>
 __global__ void __launch_bounds__(32 * kFewWarps, 1) few_tokens_kernel(const FewArgs a) {
+  constexpr int RT = few_tiles<NT>(), ST = sum_tiles<NT>();
   extern __shared__ __align__(16) uint8_t few_smem[];
   __shared__ float raw_scale[kRawTokens];
   __shared__ unsigned raw_top[kFewWarps];
@@ -128,31 +130,37 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) few_tokens_kernel(const Few
   const int m = (int)a.t.m;
   const int64_t n = a.t.n;
   const int chunks = (int)((a.t.k + 15) / 16);                       // of 16 bytes
-  const int rounds = (chunks + 8 * kFewWarps - 1) / (8 * kFewWarps);  // of 128 bytes per warp
-  const int steps = (2 * rounds + kAhead - 1) / kAhead * kAhead;
-  const int units = (int)((n + 15) / 16);
-  int* sums = reinterpret_cast<int*>(few_smem);                      // [2][warp][NT * 4][32]
-  int8_t* codes = reinterpret_cast<int8_t*>(few_smem + 2 * kFewWarps * NT * 512);
+  const int runs_all = (chunks + 7) / 8, runs = runs_all > warp ? (runs_all - warp + kFewWarps - 1) / kFewWarps : 0;
+  // this block's tiles
+  const int64_t tiles = (n + 15) / 16;
+  const int tile_lo = (int)(tiles * blockIdx.x / gridDim.x), tile_hi = (int)(tiles * (blockIdx.x + 1) / gridDim.x);
+  int* sums = reinterpret_cast<int*>(few_smem);                      // [warp][tile][NT * 4][32]
+  int8_t* codes = reinterpret_cast<int8_t*>(few_smem + few_bytes<NT>());
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(few_smem) + warp * kAhead * kStep;
 
   if (!X_RAW && a.early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   else pdl_entry();
 
-  // step i of a warp: chunks of the 128 bytes (i / 2) * 16 + warp, first or second half
-  auto chunk_of = [&](int i) { return ((i >> 1) * kFewWarps + warp) * 8 + (i & 1) * 4 + t4; };
-  int load_unit = blockIdx.x, load_step = 0;
-  uint4 w[kAhead][2];
-  auto fetch = [&](uint4 (&to)[2]) {
-    const int c = chunk_of(load_step);
-    to[0] = to[1] = make_uint4(0, 0, 0, 0);
-    if (load_unit < units && c < chunks) {
-      const int64_t r0 = (int64_t)load_unit * 16 + g, r1 = r0 + 8;
-      if (r0 < n) to[0] = load_once(a.t.qw + r0 * a.t.ldw + c * 16);
-      if (r1 < n) to[1] = load_once(a.t.qw + r1 * a.t.ldw + c * 16);
+  // the weights of a pass (up to RT tiles), run by run, tile by tile
+  int pass_lo = tile_lo, count = min(RT, tile_hi - tile_lo), load_run = 0, load_tile = 0;
+  uint32_t fill = 0;
+  const uint32_t put_even = (lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4), put_odd = put_even ^ 64u;      // rows 0-3 and 8-11, 4-7 and 12-15
+  auto fetch = [&]() {
+    if (load_run < runs) {
+      const int c = min((load_run * kFewWarps + warp) * 8 + (lane & 7), chunks - 1);      // chunks behind the last meet codes of zero
+      const int64_t r0 = (int64_t)(pass_lo + load_tile) * 16 + (lane >> 3);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {      // rows behind the last are read as the last; their sums go nowhere
+        const int64_t r = min(r0 + 4 * i, n - 1);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + (i & 1 ? put_odd : put_even) + fill + i * 512), "l"(a.t.qw + r * a.t.ldw + c * 16) : "memory");
+      }
+      if (++load_tile == count) { load_tile = 0; ++load_run; }
     }
-    if (++load_step == steps) { load_step = 0; load_unit += gridDim.x; }
+    fill = fill == (kAhead - 1) * kStep ? 0 : fill + kStep;
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) fetch(w[i]);
+  for (int i = 0; i < kAhead - 1; ++i) fetch();
   if (!X_RAW && a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
 
   const int pitch = raw_pitch(a.t.k);
@@ -160,77 +168,145 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) few_tokens_kernel(const Few
     const int parts = kFewWarps / m, tok = warp / parts, part = warp - tok * parts;
     const TX* x = reinterpret_cast<const TX*>(a.x) + (int64_t)tok * a.ldx;
     const int k = (int)a.t.k;
+    // pieces of 16 bytes, kept in registers, where all rows allow it: kRawElements over the block's threads at most
+    constexpr int V = Vec<TX>::N, HELD = kRawElements / (32 * kFewWarps) / V;
+    const bool vec = ((uintptr_t)a.x | (uintptr_t)(a.ldx * sizeof(TX))) % 16 == 0 && k % V == 0 && HELD * parts * 32 * V >= k;
+    float held[HELD][V];
     unsigned top = 0, odd = 0;
-    if (tok < m)
-      for (int c = part * 32 + lane; c < k; c += 32 * parts) {
-        const unsigned b = abs_bits(to_float<TX>(x[c]));
-        if (b < 0x7f800000u) top = b > top ? b : top; else odd = 1;
+    auto see = [&](float f) {
+      const unsigned b = abs_bits(f);
+      if (b < 0x7f800000u) top = b > top ? b : top; else odd = 1;
+    };
+    if (tok < m) {
+      if (vec) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+          const int c = ((i * parts + part) * 32 + lane) * V;
+          if (c < k) load_vec<TX>(x + c, held[i]);
+          else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) held[i][j] = 0.0f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) see(held[i][j]);
+      } else {
+        for (int c = part * 32 + lane; c < k; c += 32 * parts) see(to_float<TX>(x[c]));
       }
+    }
     top = warp_max_u(top);
     if (lane == 0) raw_top[warp] = top;
     if (__syncthreads_or(odd) && tid == 0) atomicOr(a.err, ERR_NONFINITE);
     if (tok < m) {
       for (int p = 0; p < parts; ++p) top = raw_top[tok * parts + p] > top ? raw_top[tok * parts + p] : top;
       const float absmax = __uint_as_float(top), inv = inv_scale_of(absmax, a.qmax);
-      for (int c = part * 32 + lane; c < pitch; c += 32 * parts) {
-        const float f = c < k ? to_float<TX>(x[c]) : 0.0f;
-        codes[tok * pitch + c] = (int8_t)(finite_bits(f) ? code_of(f, inv, a.qmax) : 0);
+      auto code = [&](float f) { return (int8_t)(finite_bits(f) ? code_of(f, inv, a.qmax) : 0); };
+      if (vec) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+          const int c = ((i * parts + part) * 32 + lane) * V;
+          if (c >= k) continue;
+          union { uint2 w2; uint32_t w; int8_t b[8]; } o;
+#pragma unroll
+          for (int j = 0; j < V; ++j) o.b[j] = code(held[i][j]);
+          if (V == 8) *reinterpret_cast<uint2*>(codes + tok * pitch + c) = o.w2;
+          else *reinterpret_cast<uint32_t*>(codes + tok * pitch + c) = o.w;
+        }
+        for (int c = k + part * 32 + lane; c < pitch; c += 32 * parts) codes[tok * pitch + c] = 0;
+      } else {
+        for (int c = part * 32 + lane; c < pitch; c += 32 * parts) codes[tok * pitch + c] = c < k ? code(to_float<TX>(x[c])) : (int8_t)0;
       }
       if (part == 0 && lane == 0) raw_scale[tok] = scale_of(absmax, a.qmax);
     }
     __syncthreads();
   }
 
-  int buffer = 0;
-  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    int acc[NT][4];
+  // this lane's tokens; those behind the last are read as the last, their sums go nowhere
+  const int8_t* token[NT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+  for (int j = 0; j < NT; ++j) {
+    const int tok = min(8 * j + g, m - 1);
+    token[j] = X_RAW ? codes + tok * pitch : a.t.qx + (int64_t)tok * a.t.ldx;
+  }
+  uint32_t drain = 0;
+  // lanes 8 i .. 8 i + 7 give the rows of matrix i: rows 0-7 and 8-15 of the first 16 bytes, then of the next
+  const uint32_t get_row = lane & 15, get_at = ring + get_row * 128, get_flip = (lane >> 4) ^ (get_row & 7);
+  for (;;) {
+    int acc[RT][NT][4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) acc[j][c] = 0;
-    for (int i = 0; i < steps; i += kAhead) {
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int p = 0; p < kAhead; ++p) {
-        const uint4 w0 = w[p][0], w1 = w[p][1];
-        const int c = chunk_of(i + p);
-        uint4 x[NT];
+      for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const int tok = 8 * j + g;
-          x[j] = make_uint4(0, 0, 0, 0);
-          if (c < chunks && tok < m)
-            x[j] = X_RAW ? *reinterpret_cast<const uint4*>(codes + tok * pitch + c * 16)
-                         : __ldg(reinterpret_cast<const uint4*>(a.t.qx + (int64_t)tok * a.t.ldx + c * 16));
+        for (int c = 0; c < 4; ++c) acc[r][j][c] = 0;
+    for (int i = 0; i < runs; ++i) {
+      const int c = (i * kFewWarps + warp) * 8;
+      uint32_t x[4][NT][2];              // [32 bytes][tokens][half]
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t* from = reinterpret_cast<const uint32_t*>(token[j] + (c + 2 * k + h) * 16) + t4;
+            x[k][j][h] = 0;
+            if (c + 2 * k + h < chunks) x[k][j][h] = X_RAW ? *from : __ldg(from);
+          }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        if (r >= count) break;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory");
+        __syncwarp();                    // the step has arrived for all lanes, and all are done with the one before
+        fetch();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t w[4];
+          asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                       : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(get_at + drain + ((get_flip ^ (2 * k)) << 4)));
+#pragma unroll
+          for (int j = 0; j < NT; ++j) mma_s8(acc[r][j], w[0], w[1], w[2], w[3], x[k][j][0], x[k][j][1]);
         }
-        fetch(w[p]);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          mma_s8(acc[j], w0.x, w1.x, w0.y, w1.y, x[j].x, x[j].y);
-          mma_s8(acc[j], w0.z, w1.z, w0.w, w1.w, x[j].z, x[j].w);
-        }
+        drain = drain == (kAhead - 1) * kStep ? 0 : drain + kStep;
       }
     }
-    int* mine = sums + buffer * kFewWarps * NT * 128;
-    buffer ^= 1;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int r0 = 0; r0 < RT; r0 += ST) {
+      if (r0 >= count) break;
+      __syncthreads();                 // the ring is empty, or the tiles before have been added up
 #pragma unroll
-      for (int c = 0; c < 4; ++c) mine[(warp * NT * 4 + j * 4 + c) * 32 + lane] = acc[j][c];
-    __syncthreads();                   // the other buffer is free behind it: everybody is done with the unit before
-    for (int e = tid; e < 16 * m; e += 32 * kFewWarps) {
-      const int tok = e >> 4, r = e & 15;
-      const int64_t col = (int64_t)unit * 16 + r;
-      if (col >= n) continue;
-      const int* from = mine + ((tok >> 3) * 4 + (r >> 3) * 2 + (tok & 1)) * 32 + (r & 7) * 4 + ((tok & 7) >> 1);
-      int sum = 0;
+      for (int r = r0; r < r0 + ST && r < RT; ++r)
 #pragma unroll
-      for (int v = 0; v < kFewWarps; ++v) sum += from[v * NT * 128];
-      float y = __fmul_rn((float)sum, __fmul_rn(X_RAW ? raw_scale[tok] : __ldg(a.t.sx + tok), __ldg(a.t.sw + col)));
-      if (a.t.bias) y += __ldg(a.t.bias + col);
-      if (a.t.act == QCFG_ACT_RELU) y = fmaxf(y, 0.0f);
-      else if (a.t.act == QCFG_ACT_GELU_TANH) y = gelu_tanh(y);
-      reinterpret_cast<TY*>(a.t.y)[(int64_t)tok * a.t.ldy + col] = from_float<TY>(y);
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (r < count) sums[((warp * ST + r - r0) * NT * 4 + j * 4 + c) * 32 + lane] = acc[r][j][c];
+      __syncthreads();
+      const int here = min(ST, count - r0) * 16;             // rows
+      for (int e = tid; e < here * m; e += 32 * kFewWarps) {
+        const int tok = e / here, row = e - tok * here, r = row & 15;
+        const int64_t col = (int64_t)(pass_lo + r0) * 16 + row;
+        if (col >= n) continue;
+        const int* from = sums + (row >> 4) * NT * 128 + ((tok >> 3) * 4 + (r >> 3) * 2 + (tok & 1)) * 32 + (r & 7) * 4 + ((tok & 7) >> 1);
+        int sum = 0;
+#pragma unroll
+        for (int v = 0; v < kFewWarps; ++v) sum += from[v * ST * NT * 128];
+        float y = __fmul_rn((float)sum, __fmul_rn(X_RAW ? raw_scale[tok] : __ldg(a.t.sx + tok), __ldg(a.t.sw + col)));
+        if (a.t.bias) y += __ldg(a.t.bias + col);
+        if (a.t.act == QCFG_ACT_RELU) y = fmaxf(y, 0.0f);
+        else if (a.t.act == QCFG_ACT_GELU_TANH) y = gelu_tanh(y);
+        reinterpret_cast<TY*>(a.t.y)[(int64_t)tok * a.t.ldy + col] = from_float<TY>(y);
+      }
     }
+    pass_lo += count;
+    if (pass_lo >= tile_hi) return;
+    count = min(RT, tile_hi - pass_lo);
+    load_run = load_tile = 0;
+    __syncthreads();                   // the sums have been read
+#pragma unroll
+    for (int i = 0; i < kAhead - 1; ++i) fetch();
   }
 }
 
@@ -265,8 +341,8 @@ int launch_quantize_tokens(Ctx* ctx, const void* x, int dtype, int64_t rows, int
 
 template <typename TX, typename TY, int NT, bool X_RAW>
 static int few_as(Ctx* ctx, const FewArgs& a, cudaStream_t st) {
-  const int smem = 2 * kFewWarps * NT * 512 + (X_RAW ? (int)a.t.m * raw_pitch(a.t.k) : 0);
-  constexpr int most = 2 * kFewWarps * NT * 512 + (X_RAW ? 2 * kRawElements : 0);
+  const int smem = few_bytes<NT>() + (X_RAW ? (int)a.t.m * raw_pitch(a.t.k) : 0);
+  constexpr int most = few_bytes<NT>() + (X_RAW ? kRawElements + 32 * kRawTokens : 0);
   static DeviceOnce once;
   const cudaError_t e = once.smem(device_of(ctx), (const void*)few_tokens_kernel<TX, TY, NT, X_RAW>, most);
   if (e != cudaSuccess) return check_cuda(ctx, e, "linear_i8");
@@ -277,19 +353,16 @@ static int few_as(Ctx* ctx, const FewArgs& a, cudaStream_t st) {
 }
 template <typename TY>
 static int few_codes(Ctx* ctx, const FewArgs& a, cudaStream_t st) {
-  const int64_t m = a.t.m;
-  if (m <= 8) return few_as<float, TY, 1, false>(ctx, a, st);
-  if (m <= 16) return few_as<float, TY, 2, false>(ctx, a, st);
-  if (m <= 24) return few_as<float, TY, 3, false>(ctx, a, st);
-  if (m <= 32) return few_as<float, TY, 4, false>(ctx, a, st);
-  return few_as<float, TY, 6, false>(ctx, a, st);
+  return a.t.m <= 8 ? few_as<float, TY, 1, false>(ctx, a, st) : few_as<float, TY, 2, false>(ctx, a, st);
 }
 template <typename TX>
 static int few_raw(Ctx* ctx, const FewArgs& a, cudaStream_t st) {
   return a.t.dtype == QCFG_FP32 ? few_as<TX, float, 1, true>(ctx, a, st) : a.t.dtype == QCFG_BF16 ? few_as<TX, __nv_bfloat16, 1, true>(ctx, a, st)
                                                                                                  : few_as<TX, __half, 1, true>(ctx, a, st);
 }
-constexpr int kFewTokens = 48;
+// Products up to this many tokens go this way, more in the GEMM's tiles of 128 rows.  us, this way / tiles, codes ready, at k = 4096 and
+// n = 16384: 8 tokens 8.7 / 12.2, 16 tokens 11.9 / 12.2; with three column tiles 17.5 / 12.2.
+constexpr int kFewTokens = 16;
 static int launch_few(Ctx* ctx, const TokenGemm& t, int early, cudaStream_t st) {
   const FewArgs a{t, nullptr, 0, 0.0f, early, err_word(ctx)};
   return t.dtype == QCFG_FP32 ? few_codes<float>(ctx, a, st) : t.dtype == QCFG_BF16 ? few_codes<__nv_bfloat16>(ctx, a, st) : few_codes<__half>(ctx, a, st);
@@ -298,15 +371,15 @@ static int launch_few(Ctx* ctx, const TokenGemm& t, int early, cudaStream_t st) 
 int launch_gemm_token(Ctx* ctx, const TokenGemm& t, cudaStream_t st) {
   if (t.m <= kFewTokens) return launch_few(ctx, t, 0, st);
   GemmArgs g{};
-  g.a = t.qx; g.lda = t.ldx; g.b = t.qw; g.ldb = t.ldw; g.m = t.m; g.n = t.n; g.k = t.k;
+  g.a = t.qx; g.lda = t.ldx; g.b = t.qw; g.ldb = t.ldw; g.m = t.m; g.n = t.n; g.k = t.k; g.a_rows = t.rows;
   g.scale_x = 1.0f; g.scale_w = t.sw; g.scale_rows = t.sx; g.bias = t.bias; g.act = t.act;
   g.y = (float*)t.y; g.ldy = t.ldy;
   g.y_kind = t.dtype == QCFG_FP32 ? 3 : t.dtype == QCFG_BF16 ? 2 : 5;
   return launch_gemm(ctx, g, st);
 }
 
-// codes [m x ldq], then the scales
-int64_t linear_work(int64_t m, int64_t k) { return m <= kRawTokens && m * k <= kRawElements ? 0 : up(m * up(k, 16), 256) + up(m * 4, 256); }
+// codes [m x ldq] and room up to a multiple of 32 rows (see GemmArgs::a_rows), then the scales
+int64_t linear_work(int64_t m, int64_t k) { return m <= kRawTokens && m * k <= kRawElements ? 0 : up(up(m, 32) * up(k, 16), 256) + up(m * 4, 256); }
 int launch_linear(Ctx* ctx, const void* x, int x_dtype, int64_t ldx, int bits, const TokenGemm& t_in, void* work, cudaStream_t st) {
   if (t_in.m <= kRawTokens && t_in.m * t_in.k <= kRawElements) {
     const FewArgs a{t_in, x, ldx, qmax_of(bits), 0, err_word(ctx)};
@@ -315,7 +388,8 @@ int launch_linear(Ctx* ctx, const void* x, int x_dtype, int64_t ldx, int bits, c
   TokenGemm t = t_in;
   t.ldx = up(t.k, 16);
   int8_t* codes = (int8_t*)work;
-  float* scale = (float*)(codes + up(t.m * t.ldx, 256));
+  t.rows = up(t.m, 32);
+  float* scale = (float*)(codes + up(t.rows * t.ldx, 256));
   t.qx = codes;
   t.sx = scale;
   const int few = t.m <= kFewTokens;
