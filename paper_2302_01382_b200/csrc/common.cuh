@@ -133,6 +133,8 @@ struct GemmArgs {
   const float* scale_rows = nullptr;   // optional, int8 only: a scale for each row in place of scale_x (then with `bias`, [n] or null,
   const float* bias = nullptr;         // and y of the type y_kind: 3 fp32, 2 bf16, 5 fp16; no other output, alone in its launch)
   int y_kind = 3;
+  int b_early = 0;              // with scale_rows: nothing the stream may still be running writes b (the kernel in front lets this one begin
+                                // only after everything in front of it has completed)
   int64_t a_rows = 0;           // rows of `a` that can be read, where there are more than m: a TMA load that ends inside 32 rows is slow
                                 // (24 rows 21.1 us, 32 rows 12.2, at n = 16384 and k = 4096)
   float* amax = nullptr;        // optional: max |output| (after shortcut and activation) is folded into *amax, which

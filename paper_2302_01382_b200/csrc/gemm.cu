@@ -130,6 +130,8 @@ constexpr int kMaxDeps = 4;
 struct TokenDesc {            // FL_TOKEN: a scale for each row, an addend for each column (or null)
   const float* scale_rows;
   const float* bias;
+  int32_t a_box;              // rows of A a stage holds (fewer than BM where the matrix has few; the MMA's further rows are never read)
+  int32_t early;              // B is older than the kernel in front (see launch_gemm's caller): its first tiles are loaded before that one ends
 };
 struct GemmParams {
   TokenDesc token;
@@ -1047,9 +1049,10 @@ gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
   // counts 256-row tiles.
   const int rank = PAIR ? (int)cluster_ctarank() : 0;
   const int b_rows = PAIR ? (p.bn >> 1) : p.bn;                  // B rows held per stage by this CTA
+  const int a_rows = FL == FL_TOKEN && !PAIR ? p.token.a_box : BM;
   constexpr bool kSlab = FL == FL_SLAB || FL == FL_SLAB64;       // stages hold weights only, the input's slabs have a ring of their own
   constexpr int kChunk = FL == FL_SLAB64 ? 64 : 128;             // ... and the slab's channel bytes
-  const uint32_t stage_bytes = kSlab ? (uint32_t)(b_rows * kChunk) : (uint32_t)(BM + b_rows) * kStageKBytes;
+  const uint32_t stage_bytes = kSlab ? (uint32_t)(b_rows * kChunk) : (uint32_t)(a_rows + b_rows) * kStageKBytes;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kMaxStages;
   const uint32_t tfull0 = empty0 + 8 * kMaxStages, tempty0 = tfull0 + 16;
   // chains: per epilogue warp, the number of its tiles whose stores have completed (counters, not
@@ -1166,17 +1169,17 @@ gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
   };
   // bytes the TMA loads of one CTA put into a stage (the A tile is gathered in convolution launches)
   const uint32_t tma_bytes = conv_on ? (uint32_t)b_rows * kStageKBytes : stage_bytes;
-  auto issue_load = [&]() {   // whole warp 0; the stage's empty barrier must already have been passed
+  auto issue_load = [&](bool want_a = true, bool want_b = true) {   // whole warp 0; the stage's empty barrier must already have been passed
     if (elected) {
     if (PAIR) {
       // the first CTA's barrier collects the bytes of both CTAs' loads
-      if (rank == 0) mbar_expect_tx(ld_bar, 2 * tma_bytes);
-      if (!kConv || !(conv_on || conv_tma)) tma_load_2d_pair(ld_dst, ld_map_a, ld_bar, ld_x, ld_ya);
-      tma_load_2d_pair(ld_dst + BM * kStageKBytes, ld_map_b, ld_bar, ld_x, ld_yb);
+      if (want_b && rank == 0) mbar_expect_tx(ld_bar, 2 * tma_bytes);
+      if (want_a && (!kConv || !(conv_on || conv_tma))) tma_load_2d_pair(ld_dst, ld_map_a, ld_bar, ld_x, ld_ya);
+      if (want_b) tma_load_2d_pair(ld_dst + BM * kStageKBytes, ld_map_b, ld_bar, ld_x, ld_yb);
     } else {
-      mbar_expect_tx(ld_bar, tma_bytes);
-      if (!kConv || !(conv_on || conv_tma)) tma_load_2d(ld_dst, ld_map_a, ld_bar, ld_x, ld_ya);
-      tma_load_2d(ld_dst + BM * kStageKBytes, ld_map_b, ld_bar, ld_x, ld_yb);
+      if (want_b) mbar_expect_tx(ld_bar, tma_bytes);
+      if (want_a && (!kConv || !(conv_on || conv_tma))) tma_load_2d(ld_dst, ld_map_a, ld_bar, ld_x, ld_ya);
+      if (want_b) tma_load_2d(ld_dst + a_rows * kStageKBytes, ld_map_b, ld_bar, ld_x, ld_yb);
     }
     }
     if (kConv && conv_tma) load_patches();
@@ -1227,11 +1230,19 @@ gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
   }
   // Everything above touches no global memory, so under programmatic dependent launch it
   // overlaps the tail of the previous kernel in the stream; from here on its results are needed.
+  const bool early = FL == FL_TOKEN && p.token.early;
+  if (early && warp == 0) {       // the weights' half of the first stages; the walk then begins again for the other half
+    const int s_tile = ld_tile, s_tm = ld_tm, s_tn = ld_tn;
+    for (int i = 0; i < p.stages && ld_tile < num_tiles; ++i) issue_load(false, true);
+    ld_tile = s_tile; ld_tm = s_tm; ld_tn = s_tn;
+    ld_kb = 0; ld_s = 0; ld_ph = 0; ld_x = 0; ld_dst = stage0; ld_bar = full0;
+    set_tile_coords();
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (p.stamp && threadIdx.x == 32) atomicMin(p.stamp, (unsigned long long)global_timer());
   if (warp == 0) {
     // the ring is empty: fill it before the block-wide barrier so the first tiles are in flight
-    if (!CHAIN && !kSlab) for (int i = 0; i < p.stages && ld_tile < num_tiles; ++i) issue_load();
+    if (!CHAIN && !kSlab) for (int i = 0; i < p.stages && ld_tile < num_tiles; ++i) issue_load(true, !early);
   }
   tc_fence_before();
   __syncthreads();
@@ -1430,7 +1441,7 @@ gemm_kernel(const __grid_constant__ LaunchArgs<CHAIN> L) {
       constexpr uint32_t kDescHi = (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29);
       const uint32_t lo0 = ((stage0 >> 4) & 0x3FFFu) | (1u << 16);
       const uint32_t lo_step = stage_bytes >> 4;
-      constexpr uint32_t kBOff = (uint32_t)(BM * kStageKBytes) >> 4;
+      const uint32_t kBOff = (uint32_t)(a_rows * kStageKBytes) >> 4;
       uint32_t lo = lo0, fb = full0;
       int s = 0; uint32_t ph = 0;
       bool ok = true;
@@ -2460,7 +2471,8 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
   }
   const int tile_rows = pair ? 2 * BM : BM;
   p.tiles_m = slab ? (int32_t)(pair ? (row_tiles + 1) / 2 : row_tiles) : (int32_t)((g0.m + tile_rows - 1) / tile_rows);
-  const int stage_bytes = slab ? (pair ? bn / 2 : bn) * sd.chunk : (BM + (pair ? bn / 2 : bn)) * kStageKBytes;
+  const int a_box = token && !pair && g0.m <= 64 ? (g0.m <= 32 ? 32 : 64) : BM;
+  const int stage_bytes = slab ? (pair ? bn / 2 : bn) * sd.chunk : (a_box + (pair ? bn / 2 : bn)) * kStageKBytes;
   p.is_bf16 = g0.is_bf16;
   // instruction descriptor: D format (F32 = 1, S32 = 2) at bit 4, A/B format (BF16 = 1, S8 = 1)
   // at bits 7 and 10, both operands K-major, N/8 at bit 17, M/16 at bit 24
@@ -2501,7 +2513,7 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
     if (token) {
       G.outs[1].kind = g.y_kind;
       G.outs[1].tma = make_token_map(&maps[MAP_FAST], G.outs[1], g.m, g.n) ? 1 : 0;
-      p.token = {g.scale_rows, g.bias};
+      p.token = {g.scale_rows, g.bias, a_box, g.b_early};
     }
     for (int j = 0; j < kNumOuts && !token; ++j)
       if (G.outs[j].kind) G.outs[j].tma = make_out_map(&maps[i * kMapsPerGroup + MAP_OUT + j], G.outs[j], g.m, g.n) ? 1 : 0;
@@ -2530,7 +2542,7 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
         if (G.outs[j].kind && !G.outs[j].tma) return set_error(ctx, QCFG_ECUDA, "cuTensorMapEncodeTiled failed");
       G.mode = EPI_SHORTCUT;
     }
-    int rc = g.conv_kh > 0 ? QCFG_OK : make_map(ctx, &maps[i * kMapsPerGroup + MAP_A], g.a, g.is_bf16, g.k, g.a_rows > g.m ? g.a_rows : g.m, g.lda, BM);
+    int rc = g.conv_kh > 0 ? QCFG_OK : make_map(ctx, &maps[i * kMapsPerGroup + MAP_A], g.a, g.is_bf16, g.k, g.a_rows > g.m ? g.a_rows : g.m, g.lda, a_box);
     if (rc == QCFG_OK) rc = make_map(ctx, &maps[i * kMapsPerGroup + MAP_B], g.b, g.is_bf16, g.k, g.n, g.ldb, pair ? bn / 2 : bn, slab ? sd.chunk : kStageKBytes);
     if (rc != QCFG_OK) return rc;
     ops += 2.0 * (double)g.m * (double)g.n * (double)g.k;
@@ -2573,7 +2585,8 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
     p.slab = sd;
     p.k_blocks = 9 * sd.chunks;
   }
-  int stages = (kSmemMax - kSmemHeader - kCsBytes - 1024 - kEpiWarps * p.epi_bytes - (slab ? sd.count * sd.bytes : 0)) / stage_bytes;
+  const int a_slack = (BM - a_box) * kStageKBytes;      // the MMA reads BM rows of the last stage too
+  int stages = (kSmemMax - kSmemHeader - kCsBytes - 1024 - a_slack - kEpiWarps * p.epi_bytes - (slab ? sd.count * sd.bytes : 0)) / stage_bytes;
   if (stages > kMaxStages) stages = kMaxStages;
   if (slab && sd.resident) stages = p.k_blocks;
   if (stages <= (shortcut ? 1 : kGatherDepth)) return set_error(ctx, QCFG_ESHAPE, "gemm: too few pipeline stages");
@@ -2603,7 +2616,7 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
     grid = 2 * (*cached);
     if (grid > 2 * num_tiles && !chainable) grid = 2 * num_tiles;
   } else if (grid > num_tiles) grid = num_tiles;
-  const size_t smem = (size_t)kSmemHeader + kCsBytes + 1024 + (size_t)kEpiWarps * p.epi_bytes + (size_t)stages * stage_bytes +
+  const size_t smem = (size_t)kSmemHeader + kCsBytes + 1024 + a_slack + (size_t)kEpiWarps * p.epi_bytes + (size_t)stages * stage_bytes +
                       (slab ? (size_t)sd.count * sd.bytes : 0);
   // a chain record carries only the distinct maps it uses; one that needs more runs on its own
   CUtensorMap pool[kPoolChain];

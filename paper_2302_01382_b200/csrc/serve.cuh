@@ -68,6 +68,7 @@ struct TokenGemm {       // y = act(float(qx qw^T) * (sx[m] * sw[n]) + bias[n])
   int act;
   void* y; int dtype; int64_t ldy;
   int64_t rows = 0;      // rows of qx that can be read, where there are more than m
+  int early = 0;         // the kernel in front waits before it lets this one begin: qw may be read at once
 };
 int launch_quantize_tokens(Ctx* ctx, const void* x, int dtype, int64_t rows, int64_t cols, int64_t ld, int bits, int8_t* q, int64_t ldq, float* scale,
                            cudaStream_t st);

@@ -363,15 +363,15 @@ static int few_raw(Ctx* ctx, const FewArgs& a, cudaStream_t st) {
 // Products up to this many tokens go this way, more in the GEMM's tiles of 128 rows.  us, this way / tiles, codes ready, at k = 4096 and
 // n = 16384: 8 tokens 8.7 / 12.2, 16 tokens 11.9 / 12.2; with three column tiles 17.5 / 12.2.
 constexpr int kFewTokens = 16;
-static int launch_few(Ctx* ctx, const TokenGemm& t, int early, cudaStream_t st) {
-  const FewArgs a{t, nullptr, 0, 0.0f, early, err_word(ctx)};
+static int launch_few(Ctx* ctx, const TokenGemm& t, cudaStream_t st) {
+  const FewArgs a{t, nullptr, 0, 0.0f, t.early, err_word(ctx)};
   return t.dtype == QCFG_FP32 ? few_codes<float>(ctx, a, st) : t.dtype == QCFG_BF16 ? few_codes<__nv_bfloat16>(ctx, a, st) : few_codes<__half>(ctx, a, st);
 }
 
 int launch_gemm_token(Ctx* ctx, const TokenGemm& t, cudaStream_t st) {
-  if (t.m <= kFewTokens) return launch_few(ctx, t, 0, st);
+  if (t.m <= kFewTokens) return launch_few(ctx, t, st);
   GemmArgs g{};
-  g.a = t.qx; g.lda = t.ldx; g.b = t.qw; g.ldb = t.ldw; g.m = t.m; g.n = t.n; g.k = t.k; g.a_rows = t.rows;
+  g.a = t.qx; g.lda = t.ldx; g.b = t.qw; g.ldb = t.ldw; g.m = t.m; g.n = t.n; g.k = t.k; g.a_rows = t.rows; g.b_early = t.early;
   g.scale_x = 1.0f; g.scale_w = t.sw; g.scale_rows = t.sx; g.bias = t.bias; g.act = t.act;
   g.y = (float*)t.y; g.ldy = t.ldy;
   g.y_kind = t.dtype == QCFG_FP32 ? 3 : t.dtype == QCFG_BF16 ? 2 : 5;
@@ -392,9 +392,9 @@ int launch_linear(Ctx* ctx, const void* x, int x_dtype, int64_t ldx, int bits, c
   float* scale = (float*)(codes + up(t.rows * t.ldx, 256));
   t.qx = codes;
   t.sx = scale;
-  const int few = t.m <= kFewTokens;
-  const int rc = quantize_rows(ctx, x, x_dtype, t.m, t.k, ldx, bits, codes, t.ldx, scale, few, st);
-  return rc ? rc : few ? launch_few(ctx, t, 1, st) : launch_gemm_token(ctx, t, st);
+  t.early = 1;
+  const int rc = quantize_rows(ctx, x, x_dtype, t.m, t.k, ldx, bits, codes, t.ldx, scale, 1, st);
+  return rc ? rc : launch_gemm_token(ctx, t, st);
 }
 
 }  // namespace qcfg
