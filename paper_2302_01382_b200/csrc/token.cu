@@ -1,21 +1,34 @@
 // Linear layers with a scale for each token: codes of Eq. 1 row by row, and the int8 product whose rescale takes the row's scale.
+#include <type_traits>
+
 #include "serve.cuh"
 
 namespace qcfg {
 
 namespace {
 
-// WPR warps (1 or 8) for each row, which they read once and keep in registers while it fits: HELD pieces of 16 bytes a thread, or
-// with VEC false (rows not on 16-byte boundaries) single elements.  What does not fit is read twice, the second time from L2.
-constexpr int kTokenThreads = 256;
-template <typename T, bool VEC> __host__ __device__ constexpr int held_pieces() { return VEC ? 8 : 16; }
-template <typename T, int WPR, bool VEC>
-__global__ void __launch_bounds__(kTokenThreads) quantize_tokens_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, float qmax,
+// WPR warps (1 or 8) for each row, which they read once and keep in registers, as it came, while it fits: HELD pieces of 16 bytes a
+// thread (2, 4 or 8: the fewer, the more rows are on their way), or with VEC false (rows not on 16-byte boundaries) single elements.  What does not fit is read twice, the second time from L2.
+// HBM bounds it once an element costs no more than its share: clamp and round in two operations (magic number, low byte), the
+// test for NaN, Inf and an infinite inverse once a row.  12288 x 768 bf16 21.3 -> 8.1 us against the first form, which held floats.
+constexpr int kTokenThreads = 256, kHeldMost = 8;
+// Bytes of the codes of elements that are all finite, with a finite inverse
+__device__ __forceinline__ uint32_t code_bits(float x, float inv, float qmax) {
+  float c;
+  asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(c) : "f"(__fmul_rn(x, inv)), "f"(qmax));
+  return __float_as_uint(__fadd_rn(c, 12582912.0f));
+}
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+template <typename T, int WPR, int HELD, bool VEC>
+__global__ void __launch_bounds__(kTokenThreads, HELD == 2 ? 6 : HELD == 4 ? 5 : 4) quantize_tokens_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, float qmax,
                                                                         int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale, int late, unsigned* err) {
   // late: the next kernel may begin only once everything in front of this one has completed (see few_tokens_kernel)
   if (late) asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");
   else pdl_entry();
-  constexpr int V = VEC ? Vec<T>::N : 1, HELD = held_pieces<T, VEC>(), N = 32 * WPR;
+  constexpr int V = VEC ? Vec<T>::N : 1, N = 32 * WPR;
+  union Piece { uint4 u; T t[Vec<T>::N]; };
   __shared__ unsigned tops[8];
   const int64_t row = WPR == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int t = WPR == 8 ? threadIdx.x : threadIdx.x & 31;
@@ -23,65 +36,87 @@ __global__ void __launch_bounds__(kTokenThreads) quantize_tokens_kernel(const T*
   x += row * ld;
   q += row * ldq;
   const int pieces = (int)(cols / V);
-  float held[HELD][V];
-  unsigned top = 0, odd = 0;
-  auto get = [&](int p, float (&f)[V]) {
-    if (VEC) load_vec<T>(x + (int64_t)p * V, reinterpret_cast<float(&)[Vec<T>::N]>(f));
-    else f[0] = to_float<T>(x[p]);
+  Piece held[HELD];
+  unsigned top = 0;
+  auto get = [&](int p, Piece& f) {
+    if (VEC) f.u = __ldg(reinterpret_cast<const uint4*>(x) + p);
+    else f.t[0] = x[p];
   };
-  auto see = [&](float f) {
-    const unsigned a = abs_bits(f);
-    if (a < 0x7f800000u) top = a > top ? a : top; else odd = 1;
+  auto largest = [&](const Piece& f) {        // a NaN or Inf orders above all others
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const unsigned a = abs_bits(to_float<T>(f.t[j]));
+      top = a > top ? a : top;
+    }
   };
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
+    held[i].u = make_uint4(0, 0, 0, 0);
     if (t + i * N < pieces) get(t + i * N, held[i]);
-    else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) held[i][j] = 0.0f;
-    }
   }
 #pragma unroll
   for (int i = 0; i < HELD; ++i)
-#pragma unroll
-    for (int j = 0; j < V; ++j) see(held[i][j]);
+    if (t + i * N < pieces) largest(held[i]);
+  Piece f;
   for (int p = t + HELD * N; p < pieces; p += N) {
-    float f[V];
     get(p, f);
-#pragma unroll
-    for (int j = 0; j < V; ++j) see(f[j]);
+    largest(f);
   }
   const int64_t tail = (int64_t)pieces * V + t;          // fewer than V elements
-  const float last = tail < cols ? to_float<T>(x[tail]) : 0.0f;
-  see(last);
-  top = warp_max_u(top);
-  if (WPR == 8) {
-    if ((t & 31) == 0) tops[t >> 5] = top;
-    if (__syncthreads_or(odd) && t == 0) atomicOr(err, ERR_NONFINITE);
+  Piece last;
+  last.u = make_uint4(0, 0, 0, 0);
+  if (tail < cols) last.t[0] = x[tail];
+  {
+    const unsigned a = abs_bits(to_float<T>(last.t[0]));
+    top = a > top ? a : top;
+  }
+  auto over_row = [&](unsigned v) {
+    v = __reduce_max_sync(0xffffffffu, v);
+    if (WPR == 8) {
+      __syncthreads();
+      if ((t & 31) == 0) tops[t >> 5] = v;
+      __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 8; ++w) top = tops[w] > top ? tops[w] : top;
-  } else if (__any_sync(0xffffffffu, odd) && t == 0) {
-    atomicOr(err, ERR_NONFINITE);
+      for (int w = 0; w < 8; ++w) v = tops[w] > v ? tops[w] : v;
+    }
+    return v;
+  };
+  top = over_row(top);
+  const bool odd = top >= 0x7f800000u;
+  if (odd) {             // the largest of the others
+    if (t == 0) atomicOr(err, ERR_NONFINITE);
+    unsigned other = 0;
+    for (int64_t c = t; c < cols; c += N) {
+      const unsigned a = abs_bits(to_float<T>(x[c]));
+      if (a < 0x7f800000u && a > other) other = a;
+    }
+    top = over_row(other);
   }
   const float absmax = __uint_as_float(top), inv = inv_scale_of(absmax, qmax);
-  auto put = [&](int p, const float (&f)[V]) {
-    union { uint2 w2; uint32_t w; int8_t b[8]; } c;
+  if (odd || !finite_bits(inv)) {
+    for (int64_t c = t; c < ldq; c += N) {
+      const float v = c < cols ? to_float<T>(x[c]) : 0.0f;
+      q[c] = (int8_t)(finite_bits(v) ? code_of(v, inv, qmax) : 0);
+    }
+  } else {
+    auto put = [&](int p, const Piece& f) {
+      uint32_t b[Vec<T>::N];
 #pragma unroll
-    for (int j = 0; j < V; ++j) c.b[j] = (int8_t)(finite_bits(f[j]) ? code_of(f[j], inv, qmax) : 0);
-    int8_t* to = q + (int64_t)p * V;
-    if (V == 8) *reinterpret_cast<uint2*>(to) = c.w2;
-    else if (V == 4) *reinterpret_cast<uint32_t*>(to) = c.w;
-    else *to = c.b[0];
-  };
+      for (int j = 0; j < V; ++j) b[j] = code_bits(to_float<T>(f.t[j]), inv, qmax);
+      int8_t* to = q + (int64_t)p * V;
+      if constexpr (VEC && Vec<T>::N == 8) *reinterpret_cast<uint2*>(to) = make_uint2(low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
+      else if constexpr (VEC) *reinterpret_cast<uint32_t*>(to) = low_bytes(b[0], b[1], b[2], b[3]);
+      else *to = (int8_t)b[0];
+    };
 #pragma unroll
-  for (int i = 0; i < HELD; ++i)
-    if (t + i * N < pieces) put(t + i * N, held[i]);
-  for (int p = t + HELD * N; p < pieces; p += N) {
-    float f[V];
-    get(p, f);
-    put(p, f);
+    for (int i = 0; i < HELD; ++i)
+      if (t + i * N < pieces) put(t + i * N, held[i]);
+    for (int p = t + HELD * N; p < pieces; p += N) {
+      get(p, f);
+      put(p, f);
+    }
+    for (int64_t c = tail; c < ldq; c += N) q[c] = c == tail && c < cols ? (int8_t)code_bits(to_float<T>(last.t[0]), inv, qmax) : (int8_t)0;
   }
-  for (int64_t c = tail; c < ldq; c += N) q[c] = (int8_t)(c == tail && c < cols && finite_bits(last) ? code_of(last, inv, qmax) : 0);
   if (t == 0) scale[row] = scale_of(absmax, qmax);
 }
 
@@ -98,8 +133,8 @@ __global__ void __launch_bounds__(kTokenThreads) quantize_tokens_kernel(const T*
 constexpr int kFewWarps = 16, kAhead = 4, kStep = 2048;
 constexpr int kRingBytes = kFewWarps * kAhead * kStep;
 constexpr int kRawElements = 16384, kRawTokens = 8;      // X_RAW up to this many
-template <int NT> __host__ __device__ constexpr int few_tiles() { return 8; }      // accumulators: NT x 4 registers each
-template <int NT> __host__ __device__ constexpr int sum_tiles() { return 4; }      // tiles added up at a time
+template <int NT> __host__ __device__ constexpr int few_tiles() { return NT <= 2 ? 8 : 4; }      // accumulators: NT x 4 registers each
+template <int NT> __host__ __device__ constexpr int sum_tiles() { return NT <= 2 ? 4 : 2; }      // tiles added up at a time
 template <int NT> __host__ __device__ constexpr int few_bytes() {      // the ring, and the sums in its place once it is empty
   return kRingBytes > kFewWarps * sum_tiles<NT>() * NT * 512 ? kRingBytes : kFewWarps * sum_tiles<NT>() * NT * 512;
 }
@@ -318,11 +353,24 @@ template <typename T>
 static void quantize_as(Ctx* ctx, const T* x, int64_t rows, int64_t cols, int64_t ld, float qmax, int8_t* q, int64_t ldq, float* scale, int late, cudaStream_t st) {
   const bool vec = (uintptr_t)x % 16 == 0 && (rows == 1 || ld * (int64_t)sizeof(T) % 16 == 0);
   // a warp a row where a row fits its registers and there are rows enough to fill the GPU
-  const bool narrow = rows >= 8 * sm_count(ctx) && cols <= 32 * (vec ? Vec<T>::N * held_pieces<T, true>() : held_pieces<T, false>());
+  const int64_t pieces = vec ? (cols + Vec<T>::N - 1) / Vec<T>::N : cols;
+  const bool narrow = rows >= 8 * sm_count(ctx) && pieces <= 32 * kHeldMost;
+  const int64_t each = (pieces + (narrow ? 31 : 255)) / (narrow ? 32 : 256);      // of a thread
   const dim3 grid((unsigned)(narrow ? (rows + 7) / 8 : rows)), block(kTokenThreads);
   const auto go = [&](auto kernel) { launch_pdl(kernel, grid, block, 0, st, x, rows, cols, ld, qmax, q, ldq, scale, late, err_word(ctx)); };
-  if (narrow) vec ? go(quantize_tokens_kernel<T, 1, true>) : go(quantize_tokens_kernel<T, 1, false>);
-  else vec ? go(quantize_tokens_kernel<T, 8, true>) : go(quantize_tokens_kernel<T, 8, false>);
+  const auto held = [&](auto warps, auto aligned) {
+    constexpr int W = decltype(warps)::value;
+    constexpr bool A = decltype(aligned)::value;
+    if (each <= 2) go(quantize_tokens_kernel<T, W, 2, A>);
+    else if (each <= 4) go(quantize_tokens_kernel<T, W, 4, A>);
+    else go(quantize_tokens_kernel<T, W, 8, A>);
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  using One = std::integral_constant<int, 1>;
+  using Eight = std::integral_constant<int, 8>;
+  if (narrow) vec ? held(One(), Yes()) : held(One(), No());
+  else vec ? held(Eight(), Yes()) : held(Eight(), No());
 }
 static int quantize_rows(Ctx* ctx, const void* x, int dtype, int64_t rows, int64_t cols, int64_t ld, int bits, int8_t* q, int64_t ldq, float* scale,
                          int late, cudaStream_t st) {
@@ -353,23 +401,28 @@ static int few_as(Ctx* ctx, const FewArgs& a, cudaStream_t st) {
 }
 template <typename TY>
 static int few_codes(Ctx* ctx, const FewArgs& a, cudaStream_t st) {
-  return a.t.m <= 8 ? few_as<float, TY, 1, false>(ctx, a, st) : few_as<float, TY, 2, false>(ctx, a, st);
+  if (a.t.m <= 8) return few_as<float, TY, 1, false>(ctx, a, st);
+  if (a.t.m <= 16) return few_as<float, TY, 2, false>(ctx, a, st);
+  return a.t.m <= 24 ? few_as<float, TY, 3, false>(ctx, a, st) : few_as<float, TY, 4, false>(ctx, a, st);
 }
 template <typename TX>
 static int few_raw(Ctx* ctx, const FewArgs& a, cudaStream_t st) {
   return a.t.dtype == QCFG_FP32 ? few_as<TX, float, 1, true>(ctx, a, st) : a.t.dtype == QCFG_BF16 ? few_as<TX, __nv_bfloat16, 1, true>(ctx, a, st)
                                                                                                  : few_as<TX, __half, 1, true>(ctx, a, st);
 }
-// Products up to this many tokens go this way, more in the GEMM's tiles of 128 rows.  us, this way / tiles, codes ready, at k = 4096 and
-// n = 16384: 8 tokens 8.7 / 12.2, 16 tokens 11.9 / 12.2; with three column tiles 17.5 / 12.2.
-constexpr int kFewTokens = 16;
+// Whether a product goes this way or in the GEMM's tiles of 128 rows.  us, this way / tiles, codes ready, tokens x k x n:
+//   8 x 4096 x 16384 8.7 / 12.2    16 x 4096 x 16384 12.1 / 12.3    24 x 4096 x 16384 18.8 / 12.5    32 x 4096 x 16384 26.1 / 12.9
+//   24 x 768 x 768 2.9 / 4.6    24 x 1024 x 4096 4.7 / 5.8    24 x 4096 x 4096 8.1 / 11.4    24 x 16384 x 4096 20.2 / 33.3
+//   24 x 8192 x 8192 15.4 / 18.7    32 x 16384 x 4096 28.4 / 33.3
+// The GEMM narrows its tiles to 64 columns and fewer for these, and its ring of eight stages then holds too few weights.
+static bool few_pays(Ctx* ctx, int64_t m, int64_t n) { return m <= 16 || (m <= 32 && n <= 64 * (int64_t)sm_count(ctx)); }
 static int launch_few(Ctx* ctx, const TokenGemm& t, cudaStream_t st) {
   const FewArgs a{t, nullptr, 0, 0.0f, t.early, err_word(ctx)};
   return t.dtype == QCFG_FP32 ? few_codes<float>(ctx, a, st) : t.dtype == QCFG_BF16 ? few_codes<__nv_bfloat16>(ctx, a, st) : few_codes<__half>(ctx, a, st);
 }
 
 int launch_gemm_token(Ctx* ctx, const TokenGemm& t, cudaStream_t st) {
-  if (t.m <= kFewTokens) return launch_few(ctx, t, st);
+  if (few_pays(ctx, t.m, t.n)) return launch_few(ctx, t, st);
   GemmArgs g{};
   g.a = t.qx; g.lda = t.ldx; g.b = t.qw; g.ldb = t.ldw; g.m = t.m; g.n = t.n; g.k = t.k; g.a_rows = t.rows; g.b_early = t.early;
   g.scale_x = 1.0f; g.scale_w = t.sw; g.scale_rows = t.sx; g.bias = t.bias; g.act = t.act;
