@@ -8,7 +8,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libqcfg.so")
-SOURCES = ["api.cu", "elementwise.cu", "conv.cu", "sweep.cu", "gemm.cu", "stem.cu", "adjust.cu", "token.cu", "pages.cu", "attention.cu"]
+SOURCES = ["api.cu", "elementwise.cu", "conv.cu", "sweep.cu", "gemm.cu", "stem.cu", "adjust.cu", "token.cu", "pages.cu", "attention.cu", "prompt.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared"]
 
@@ -20,7 +20,7 @@ def _newest(paths):
 def build_library(force: bool = False, verbose: bool = False) -> str:
     """Compiles the CUDA sources into libqcfg.so next to this file and returns its path."""
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    deps = srcs + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "ptx.cuh"), os.path.join(CSRC, "serve.cuh"),
+    deps = srcs + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "ptx.cuh"), os.path.join(CSRC, "serve.cuh"), os.path.join(CSRC, "attention.cuh"),
                    os.path.join(os.path.dirname(PKG), "include", "qcfg.h")]
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest(deps):
         return LIB

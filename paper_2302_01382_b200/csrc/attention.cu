@@ -8,31 +8,11 @@
 // (fp32 calls: the sum of two), which leaves 28 binary orders below the largest weight before the fp16 grid coarsens.
 #include <algorithm>
 
-#include "serve.cuh"
+#include "attention.cuh"
 
 namespace qcfg {
 
 namespace {
-
-struct AttnArgs {
-  PoolView pool;
-  CacheView cache;
-  BatchView batch;
-  const void* q;
-  void* out;
-  int64_t q_row, q_head, o_row, o_head;
-  int q_heads, causal, window;
-  int uncut;                // every tile to one block (see kUncutTokens)
-  float scale;              // sm_scale * log2(e)
-  void* work;
-  unsigned* err;
-};
-
-// The tokens the row at position pos sees: [lo, hi), empty as hi <= lo.
-__device__ __forceinline__ void seen_range(const AttnArgs& a, int64_t pos, int len, int& lo, int& hi) {
-  hi = pos < 0 ? 0 : a.causal ? (int)(pos + 1) : len;
-  lo = a.window > 0 && pos + 1 > a.window ? (int)(pos + 1) - a.window : 0;
-}
 
 // ---- warps stream the cache ------------------------------------------------------------------------
 //
@@ -54,10 +34,6 @@ constexpr int kSetup = 2;           // units
 constexpr int kRun = 32;            // tokens a warp takes at a time
 constexpr int kStreamWarps = 4;
 constexpr int kMinUnits = 2;        // a block takes at least this many
-// Weights are 2^(7 + x - ref).  ref follows the running maximum only when a score passes it by more than 2^8: sums and
-// accumulators are rescaled once or twice in a context and not at every new maximum, and a weight stays below 2^15.
-constexpr float kWeightBias = 7.0f, kWeightMost = 15.0f;
-
 template <int DP> __host__ __device__ constexpr int stage_bytes() { return 2 * kRun * DP + 32; }             // keys, values, four maxima
 template <int DP, int NR> __host__ __device__ constexpr int stream_blocks() { return DP == 256 ? 1 : DP == 128 ? (NR == 4 ? 2 : 3) : NR == 1 ? 4 : NR == 2 ? 3 : 2; }    // per SM
 template <int DP, int NR> __host__ __device__ constexpr int stream_stages() { return DP == 256 ? 3 : DP == 128 ? (NR == 4 ? 3 : 2) : (NR == 1 ? 3 : 4); }
@@ -76,13 +52,6 @@ struct PartMeta {         // of a block: the cut tile that its first segment fin
 };
 template <int DP, int NR> __host__ __device__ constexpr int64_t part_floats() { return 8 * NR * DP + 16 * NR; }     // accumulators, maxima, sums
 
-__device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
-__device__ __forceinline__ uint32_t pack_h2(float a, float b) { return h2_bits(__floats2half2_rn(a, b)); }
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -92,15 +61,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t o;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(o) : "r"(v));
   return o;
-}
-// Two bytes of a word of codes plus 128 as fp16 codes: 0x6400 + b is 1024 + b.  `magic` is 0x64646464, read from shared memory once: a
-// constant the compiler knows it keeps in a uniform register and copies anew in front of almost every permutation, 118 of a run's
-// 870 instructions.
-template <uint32_t SEL>
-__device__ __forceinline__ uint32_t two_codes(uint32_t biased, uint32_t magic) {
-  const uint32_t w = __byte_perm(biased, magic, SEL);
-  const __half2 off = __floats2half2_rn(1152.0f, 1152.0f);
-  return h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&w), off));
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -294,11 +254,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
           const unsigned b = __shfl_xor_sync(__activemask(), top, o);
           top = b > top ? b : top;
         }
-        // 2^(12 - exponent of the largest): its inverse goes into the row's factor
-        int shift = 12 - ((int)(top >> 23) - 127);
-        if (top == 0 || top >= 0x7f800000u) shift = 0;
-        shift = shift > 120 ? 120 : shift;
-        const float up = __uint_as_float((unsigned)(127 + shift) << 23);
+        const int shift = row_shift(top);
+        const float up = exp2_of(shift);
 #pragma unroll
         for (int c = 0; c < DP / 8 / V; ++c)
 #pragma unroll
@@ -313,7 +270,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
               asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + ROWS * DP * 2),
                            "r"(pack_h2(x - __low2float(hi), y - __high2float(hi))) : "memory");
           }
-        if (part == 0) row_scale[r] = a.scale * __uint_as_float((unsigned)(127 - shift) << 23);
+        if (part == 0) row_scale[r] = a.scale * exp2_of(-shift);
       }
     }
     __syncthreads();
@@ -785,6 +742,7 @@ int launch_kv_attention(Ctx* ctx, const PoolView& p, const CacheView& c, const B
   const int uncut = max_len > 0 && max_len <= kUncutTokens;
   const AttnArgs a{p, c, b, q, out, q_row, q_head, o_row, o_head, q_heads, causal, window, uncut, scale * 1.44269504088896f, work, err_word(ctx)};
   int64_t rows = !b.starts ? 1 : max_rows > 0 ? max_rows : (b.rows + b.n - 1) / b.n;
+  if (prompt_pays(ctx, a, dtype, rows)) return launch_prompt(ctx, a, dtype, st);
   rows *= q_heads / c.heads;
   return dtype == QCFG_FP32 ? stream_of<float>(ctx, a, rows, st) : dtype == QCFG_BF16 ? stream_of<__nv_bfloat16>(ctx, a, rows, st)
                                                                                        : stream_of<__half>(ctx, a, rows, st);

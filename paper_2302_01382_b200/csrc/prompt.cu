@@ -1,0 +1,519 @@
+// Attention over the paged 8-bit cache for prompts: many query rows, so the products are the work and go to tcgen05.
+//
+// A block owns 256 query rows of one cache head, as two tiles of 128 rows (the M of an MMA); a row is a (query token, head of the
+// group).  It walks the tokens its rows see in steps of 128:
+//   warps 0-3, 4-7   one thread a row of tile 0 / tile 1: scores from TMEM, running reference, weights back to TMEM as fp16
+//                    (over the scores they come from), which is where the second product takes its A operand from.
+//   warps 8-11       bring the codes of the next step from global memory to registers, and turn the present ones into fp16 in shared
+//                    memory: 128-byte rows, 128B swizzle, for keys (K-major B operand) and values (MN-major) alike.
+//   warp 12          issues the MMAs: S0, S1, then for each step O0 += P0 V, S0 of the next step, O1 += P1 V, S1 of the next step.
+//                    While one tile's weights are computed, the tensor core works for the other.
+// Each step and tile costs 2 x 128 x 128 x dim products (1024 cycles for both tiles at dim 128, twice) and 128 x 128 exponentials
+// (16 per cycle: 2048 cycles for both tiles): the exponentials and the tensor core are equally long, and the issue slots nearly so.
+// Numbers as in the streaming kernel: codes are exact in fp16, a page's key scale multiplies the scores' factor, its value scale the
+// weights, here against the largest value scale of the whole range (found before the first step), as a term of the exponent.
+#include <algorithm>
+
+#include "attention.cuh"
+#include "ptx.cuh"
+
+namespace qcfg {
+
+namespace {
+
+constexpr int kTileRows = 128;
+constexpr int kStepTokens = 128;
+constexpr int kGroups = kStepTokens / 16;        // scales are looked up for each 16 tokens
+constexpr int kSoftWarps = 8, kConvWarps = 4;
+constexpr int kPromptThreads = 32 * (kSoftWarps + kConvWarps + 1);
+constexpr int kTables = 4;
+
+template <int D, bool WIDE> __host__ __device__ constexpr int q_tile_bytes() { return kTileRows * D * 2 * (WIDE ? 2 : 1); }
+template <int D> __host__ __device__ constexpr int kv_tile_bytes() { return kStepTokens * D * 2; }
+template <int D, bool WIDE> __host__ __device__ constexpr int prompt_smem() {
+  const int used = 1024 + 2 * q_tile_bytes<D, WIDE>() + 4 * kv_tile_bytes<D>();
+  return used < 118 * 1024 ? 118 * 1024 : used;  // one block per SM: it takes all of the TMEM
+}
+
+struct Scales {          // of a step
+  float key[kGroups];    // -1: no such tokens
+  float log_share[kGroups], inv_share[kGroups];
+};
+
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_f16_ta(uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+               ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+                 "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
+  uint32_t a[16], b[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) { a[i] = v[i]; b[i] = v[16 + i]; }
+  tmem_st16(taddr, a);
+  tmem_st16(taddr + 16, b);
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Descriptor of a tile of 128-byte rows, 128B swizzle: 8-row groups 1024 bytes apart, and (MN-major) 64-element blocks `lead` bytes apart
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t lead) {
+  return (uint64_t)((addr >> 4) & 0x3FFFu) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const AttnArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  constexpr bool WIDE = sizeof(T) == 4;
+  constexpr int HALVES = D / 64, HALF = kTileRows * 128;              // bytes of 64 columns of a tile
+  constexpr uint32_t kCols = 512;
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ uint64_t bars[14];
+  __shared__ uint32_t tmem_at, magic_word;
+  __shared__ int abort_word, seen_lo, seen_hi;
+  __shared__ float unit_word, unit_parts[kConvWarps];
+  __shared__ Scales scales[kTables];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int group = a.q_heads / a.cache.heads, page = a.pool.page, hk = blockIdx.y;
+  const int per_tile = kTileRows / group, per_block = 2 * per_tile;    // query tokens
+
+  // ---- which rows: entries own rows / per_block + 1 blocks each, the last tokens (the longest rows) first
+  int64_t first;
+  const int entry = entry_of_item(a.batch, blockIdx.x, per_block, 1, first);
+  if (entry < 0 || entry >= a.batch.n) return;
+  int64_t row0, row1;
+  entry_rows(a.batch, entry, row0, row1);
+  const int rows = (int)(row1 - row0), tiles = (rows + per_block - 1) / per_block;
+  const int64_t nth = blockIdx.x - first;
+  if (nth >= tiles) return;
+  const int t_first = (tiles - 1 - (int)nth) * per_block;              // first query token
+  const int s = entry_seq(a.batch, a.pool, entry, a.err);
+  const int len = s < 0 ? 0 : seq_len(a.pool, s);
+  const bool two = t_first + per_tile < rows;                          // the second tile has rows
+
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
+  const uint32_t q_sm = smem_u32(smem), k_sm = q_sm + 2 * q_tile_bytes<D, WIDE>(), v_sm = k_sm + 2 * kv_tile_bytes<D>();
+  const uint32_t bar = smem_u32(bars);
+  const uint32_t k_full = bar, k_empty = bar + 16, v_full = bar + 32, v_empty = bar + 48, s_full = bar + 64, p_ready = bar + 80, o_done = bar + 96;
+  volatile int* abort_flag = &abort_word;
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(k_full + 8 * i, kConvWarps);
+      mbar_init(v_full + 8 * i, kConvWarps);
+      mbar_init(k_empty + 8 * i, 1);
+      mbar_init(v_empty + 8 * i, 1);
+      mbar_init(s_full + 8 * i, 1);
+      mbar_init(p_ready + 8 * i, 4);
+      mbar_init(o_done + 8 * i, 1);
+    }
+    abort_word = 0;
+    seen_lo = 0x7fffffff;
+    seen_hi = 0;
+    magic_word = 0x64646464u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kSoftWarps + kConvWarps) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_at)), "r"(kCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  __syncthreads();
+  // The next kernel may begin only now: it could take the TMEM of an SM in front of this block, and then wait for it.
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---- queries: a thread a row
+  int lo = 0, hi = 0x7fffffff, out_row = -1, out_head = 0;
+  float row_f = 0.0f;
+  if (warp < kSoftWarps) {
+    const int tile = warp >> 2, r = tid & 127;
+    const int tok = t_first + tile * per_tile + r / group;
+    const bool real = r < per_tile * group && tok < rows;
+    const T* q = nullptr;
+    if (real) {
+      out_row = tok;
+      out_head = hk * group + r % group;
+      q = reinterpret_cast<const T*>(a.q) + (row0 + tok) * a.q_row + out_head * a.q_head;
+      seen_range(a, (int64_t)len - rows + tok, len, lo, hi);
+      if (hi > lo) {
+        atomicMin(&seen_lo, lo);
+        atomicMax(&seen_hi, hi);
+      }
+    }
+    constexpr int V = Vec<T>::N;
+    unsigned top = 0;
+#pragma unroll 4
+    for (int c = 0; c < D / V; ++c) {
+      float f[V];
+      if (real) {
+        load_vec<T>(q + c * V, f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) top = max(top, abs_bits(f[j]));
+      }
+    }
+    const int shift = row_shift(top);
+    const float up = exp2_of(shift);
+    row_f = a.scale * exp2_of(-shift);
+    const uint32_t base = q_sm + tile * q_tile_bytes<D, WIDE>() + r * 128;
+#pragma unroll 4
+    for (int c = 0; c < D / 8; ++c) {
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = 0.0f;
+      if (real) {
+        if constexpr (WIDE) {
+          load_vec<T>(q + c * 8, reinterpret_cast<float(&)[Vec<T>::N]>(f[0]));
+          load_vec<T>(q + c * 8 + 4, reinterpret_cast<float(&)[Vec<T>::N]>(f[4]));
+        } else {
+          load_vec<T>(q + c * 8, reinterpret_cast<float(&)[Vec<T>::N]>(f[0]));
+        }
+      }
+      uint32_t w[4], l[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x = f[2 * j] * up, y = f[2 * j + 1] * up;
+        const __half2 h = __floats2half2_rn(x, y);
+        w[j] = h2_bits(h);
+        if (WIDE) l[j] = pack_h2(x - __low2float(h), y - __high2float(h));
+      }
+      const uint32_t to = base + (c >> 3) * HALF + (((c & 7) ^ (r & 7)) << 4);
+      st_shared_v4(to, w[0], w[1], w[2], w[3]);
+      if (WIDE) st_shared_v4(to + kTileRows * D * 2, l[0], l[1], l[2], l[3]);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_at;
+  const int tok_lo = seen_hi > 0 ? seen_lo / kStepTokens * kStepTokens : 0;
+  const int steps = seen_hi > tok_lo ? (seen_hi - tok_lo + kStepTokens - 1) / kStepTokens : 0;
+  // TMEM columns: scores (and weights) of the tiles, accumulators, second halves of the weights
+  const uint32_t s_at = tmem, o_at = tmem + 256, l_at = tmem + 384;
+
+  if (steps > 0 && warp >= kSoftWarps && warp < kSoftWarps + kConvWarps) {
+    // ------------------------------------------------------------------ codes to fp16
+    const int cw = warp - kSoftWarps;              // tokens 32 cw .. 32 cw + 31 of a step
+    const uint32_t magic = *(volatile uint32_t*)&magic_word;
+    const int32_t* table = a.pool.table + (int64_t)(s < 0 ? 0 : s) * a.pool.max_pages;
+    // pages of the warp's two groups of 16 tokens, -1 for those that are not there
+    auto look_up = [&](int step, int (&p)[2]) {
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int tok = tok_lo + step * kStepTokens + 32 * cw + 16 * z;
+        p[z] = -1;
+        if (step < steps && tok < len) {
+          p[z] = __ldg(table + tok / page);
+          if (p[z] < 0 || p[z] >= a.pool.n_pages) {
+            if (lane == 0) atomicOr(a.err, ERR_PAGE);
+            p[z] = -1;
+          }
+        }
+      }
+    };
+    // the largest value scale of the range
+    float unit = 0.0f;
+    for (int64_t tok = tok_lo / page * page + (int64_t)(cw * 32 + lane) * page; tok < seen_hi && tok < len; tok += 128 * page) {
+      const int p = __ldg(table + tok / page);
+      if (p >= 0 && p < a.pool.n_pages) unit = fmaxf(unit, __ldg(a.cache.v_absmax + (int64_t)p * a.cache.heads + hk));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, o));
+    if (lane == 0) unit_parts[cw] = unit;
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+    for (int w = 0; w < kConvWarps; ++w) unit = fmaxf(unit, unit_parts[w]);
+    unit *= 1.0f / kQmax8;
+    if (unit > 0.0f) unit = fmaxf(unit, 1.2e-38f);
+    if (tid == 32 * kSoftWarps) unit_word = unit;
+    const float inv_unit = unit > 0.0f ? __fdiv_rn(1.0f, unit) : 0.0f;
+
+    // a warp-wide access: 8 tokens x 4 chunks of 16 codes; 4 of tokens x HALVES of columns per tile
+    const int r8 = lane >> 2, c4 = lane & 3;
+    const uint32_t put = (uint32_t)((32 * cw + r8) * 128), flip = (uint32_t)r8;
+    auto load = [&](const int8_t* base, const int (&p)[2], int step, uint4 (&to)[4 * HALVES]) {
+#pragma unroll
+      for (int o = 0; o < 4; ++o) {
+        const int z = o >> 1, tok = tok_lo + step * kStepTokens + 32 * cw + 8 * o;
+        const int8_t* from = base + (((int64_t)p[z] * a.cache.heads + hk) * page + (tok & (page - 1)) + r8) * D + c4 * 16;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) to[o * HALVES + h] = p[z] >= 0 ? __ldg(reinterpret_cast<const uint4*>(from + h * 64)) : make_uint4(0, 0, 0, 0);
+      }
+    };
+    auto store = [&](uint32_t tile, const uint4 (&from)[4 * HALVES]) {
+#pragma unroll
+      for (int o = 0; o < 4; ++o)
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+          const uint4 v = from[o * HALVES + h];
+          const uint32_t x = v.x ^ 0x80808080u, y = v.y ^ 0x80808080u, z = v.z ^ 0x80808080u, w = v.w ^ 0x80808080u;
+          const uint32_t at = tile + put + o * 1024 + h * HALF;
+          st_shared_v4(at + (((2 * c4) ^ flip) << 4), two_codes<0x4140>(x, magic), two_codes<0x4342>(x, magic), two_codes<0x4140>(y, magic), two_codes<0x4342>(y, magic));
+          st_shared_v4(at + (((2 * c4 + 1) ^ flip) << 4), two_codes<0x4140>(z, magic), two_codes<0x4342>(z, magic), two_codes<0x4140>(w, magic), two_codes<0x4342>(w, magic));
+        }
+    };
+    int now[2], next[2];
+    uint4 kc[4 * HALVES], vc[4 * HALVES];
+    float k_max = 0.0f, v_max = 0.0f;
+    auto load_scales = [&](const int (&p)[2]) {       // lanes 0 and 1: the warp's two groups
+      const int mine = lane & 1 ? p[1] : p[0];
+      k_max = v_max = -1.0f;
+      if (lane < 2 && mine >= 0) {
+        k_max = __ldg(a.cache.k_absmax + (int64_t)mine * a.cache.heads + hk);
+        v_max = __ldg(a.cache.v_absmax + (int64_t)mine * a.cache.heads + hk);
+      }
+    };
+    look_up(0, now);
+    look_up(1, next);
+    load(a.cache.k, now, 0, kc);
+    load_scales(now);
+    load(a.cache.v, now, 0, vc);
+    for (int j = 0; j < steps; ++j) {
+      const uint32_t st = j & 1, ph = (j >> 1) & 1;
+      if (j >= 2 && !mbar_wait_warp(k_empty + 8 * st, ph ^ 1, abort_flag, a.err)) break;
+      store(k_sm + st * kv_tile_bytes<D>(), kc);
+      if (lane < 2) {
+        Scales& sc = scales[j % kTables];
+        const int g = 2 * cw + lane;
+        const bool ok = k_max >= 0.0f;
+        sc.key[g] = !ok ? -1.0f : k_max > 0.0f ? k_max * (1.0f / kQmax8) : 1.0f;
+        // a page of zeros may have any weight
+        const float share = v_max > 0.0f ? fmaxf(v_max * (1.0f / kQmax8) * inv_unit, 8.7e-19f) : 1.0f;
+        sc.log_share[g] = log2f(share);
+        sc.inv_share[g] = __fdiv_rn(1.0f, share);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(k_full + 8 * st);
+      if (j + 1 < steps) {
+        load(a.cache.k, next, j + 1, kc);
+        load_scales(next);
+      }
+      if (j >= 2 && !mbar_wait_warp(v_empty + 8 * st, ph ^ 1, abort_flag, a.err)) break;
+      store(v_sm + st * kv_tile_bytes<D>(), vc);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(v_full + 8 * st);
+      if (j + 1 < steps) load(a.cache.v, next, j + 1, vc);
+      look_up(j + 2, next);
+    }
+  } else if (steps > 0 && warp == kSoftWarps + kConvWarps) {
+    // ------------------------------------------------------------------ products
+    // fp32 accumulators, fp16 operands; the second product's B operand (values) is MN-major
+    constexpr uint32_t kIdescS = (1u << 4) | ((uint32_t)(kStepTokens >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
+    constexpr uint32_t kIdescO = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
+    const bool elected = elect_one();
+    const int n_tiles = two ? 2 : 1;
+    bool ok = true;
+    auto product_s = [&](int i, int j) {
+      if (!elected) return;
+      const uint64_t k0 = tile_desc(k_sm + (j & 1) * kv_tile_bytes<D>(), 16);
+#pragma unroll
+      for (int part = 0; part < (WIDE ? 2 : 1); ++part) {
+        const uint64_t q0 = tile_desc(q_sm + i * q_tile_bytes<D, WIDE>() + part * kTileRows * D * 2, 16);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = ((k >> 2) * HALF + (k & 3) * 32) >> 4;
+          mma_f16(s_at + 128 * i, q0 + off, k0 + off, kIdescS, part + k > 0);
+        }
+      }
+      tc_commit(s_full + 8 * i);
+    };
+    auto product_o = [&](int i, int j) {
+      if (!elected) return;
+      const uint64_t v0 = tile_desc(v_sm + (j & 1) * kv_tile_bytes<D>(), HALF);
+#pragma unroll
+      for (int part = 0; part < (WIDE ? 2 : 1); ++part)
+#pragma unroll
+        for (int k = 0; k < kStepTokens / 16; ++k)
+          mma_f16_ta(o_at + D * i, (part ? l_at + 64 * i : s_at + 128 * i) + 8 * k, v0 + ((k * 2048) >> 4), kIdescO, j + part + k > 0);
+    };
+    ok = mbar_wait_warp(k_full, 0, abort_flag, a.err);
+    tc_fence_after();
+    if (ok) {
+      for (int i = 0; i < n_tiles; ++i) product_s(i, 0);
+      if (elected) tc_commit(k_empty);
+    }
+    for (int j = 0; j < steps && ok; ++j) {
+      const uint32_t st = j & 1, ph = (j >> 1) & 1, st1 = st ^ 1, ph1 = ((j + 1) >> 1) & 1;
+      ok = mbar_wait_warp(v_full + 8 * st, ph, abort_flag, a.err);
+      for (int i = 0; i < n_tiles && ok; ++i) {
+        ok = mbar_wait_warp(p_ready + 8 * i, j & 1, abort_flag, a.err);
+        if (!ok) break;
+        tc_fence_after();
+        product_o(i, j);
+        if (elected && i == n_tiles - 1) tc_commit(v_empty + 8 * st);
+        if (j + 1 < steps) {
+          if (i == 0) {
+            ok = mbar_wait_warp(k_full + 8 * st1, ph1, abort_flag, a.err);
+            if (!ok) break;
+            tc_fence_after();
+          }
+          product_s(i, j + 1);
+          if (elected && i == n_tiles - 1) tc_commit(k_empty + 8 * st1);
+        } else if (elected) {
+          tc_commit(o_done + 8 * i);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp < kSoftWarps) {
+    // ------------------------------------------------------------------ weights
+    const int i = warp >> 2;
+    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+    const uint32_t s_row = s_at + 128 * i + lanes, o_row = o_at + D * i + lanes, l_row = l_at + 64 * i + lanes;
+    float ref = -INFINITY, sum = 0.0f;
+    bool ok = true;
+    const int n = i == 0 || two ? steps : 0;
+    for (int j = 0; j < n; ++j) {
+      const int tok = tok_lo + j * kStepTokens;
+      const int from = lo - tok, to = hi - tok;               // of this step's tokens the row sees [from, to)
+      if (!mbar_wait_warp(s_full + 8 * i, j & 1, abort_flag, a.err)) { ok = false; break; }
+      tc_fence_after();
+      const Scales& sc = scales[j % kTables];
+      float f[kGroups];
+      bool some = false;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        f[g] = sc.key[g];
+        some |= f[g] < 0.0f;
+        f[g] = fmaxf(row_f * f[g], 1.2e-38f);
+      }
+      const bool masked = __any_sync(0xffffffffu, some || from > 0 || to < kStepTokens);
+      // scores that are not seen, of 32 columns
+      auto mask = [&](uint32_t (&v)[32], int c) {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          const int t = 32 * c + k;
+          if (t < from || t >= to || sc.key[2 * c + (k >> 4)] < 0.0f) v[k] = 0xff800000u;
+        }
+      };
+      float most = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t v[32];
+        tmem_ld32_issue(s_row + 32 * c, v);
+        tmem_ld_wait();
+        if (masked) mask(v, c);
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          float m = __uint_as_float(v[16 * z]);
+#pragma unroll
+          for (int k = 1; k < 16; ++k) m = fmaxf(m, __uint_as_float(v[16 * z + k]));
+          most = fmaxf(most, m * f[2 * c + z]);
+        }
+      }
+      if (__any_sync(0xffffffffu, most > ref + (kWeightMost - kWeightBias) || (ref == -INFINITY && most > -INFINITY))) {
+        const float now = fmaxf(ref, most), keep = ex2(ref - (now == -INFINITY ? 0.0f : now));
+        ref = now;
+        sum *= keep;
+        if (j > 0) {      // the products so far have been completed in front of these scores
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t v[32];
+            tmem_ld32_issue(o_row + 32 * c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * keep);
+            tmem_st32(o_row + 32 * c, v);
+          }
+        }
+      }
+      const float shift = kWeightBias - (ref == -INFINITY ? 0.0f : ref);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t v[32], p[16], l[WIDE ? 16 : 1];
+        tmem_ld32_issue(s_row + 32 * c, v);
+        tmem_ld_wait();
+        if (masked) mask(v, c);
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const float fg = f[2 * c + z], at = shift + sc.log_share[2 * c + z];
+          float part = 0.0f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float e0 = ex2(fmaf(__uint_as_float(v[16 * z + 2 * k]), fg, at)), e1 = ex2(fmaf(__uint_as_float(v[16 * z + 2 * k + 1]), fg, at));
+            part += e0 + e1;
+            const __half2 h = __floats2half2_rn(e0, e1);
+            p[8 * z + k] = h2_bits(h);
+            if (WIDE) l[8 * z + k] = pack_h2(e0 - __low2float(h), e1 - __high2float(h));
+          }
+          sum = fmaf(part, sc.inv_share[2 * c + z], sum);
+        }
+        tmem_st16(s_row + 16 * c, p);      // over columns read in this step's chunks up to c
+        if constexpr (WIDE) tmem_st16(l_row + 16 * c, l);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_ready + 8 * i);
+    }
+    // ---- out
+    if (n > 0 && ok) ok = mbar_wait_warp(o_done + 8 * i, 0, abort_flag, a.err);
+    if (ok && (i == 0 || two)) {
+      tc_fence_after();
+      float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : (sum == 0.0f ? 0.0f : sum);
+      if (n > 0) inv *= unit_word;
+      T* out = reinterpret_cast<T*>(a.out) + (row0 + out_row) * a.o_row + out_head * a.o_head;
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t v[32];
+        if (n > 0) {
+          tmem_ld32_issue(o_row + 32 * c, v);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] = 0u;
+        }
+        if (out_row < 0) continue;
+        constexpr int V = Vec<T>::N;
+#pragma unroll
+        for (int k = 0; k < 32; k += V) {
+          union { uint4 u; T t[V]; } w;
+#pragma unroll
+          for (int e = 0; e < V; ++e) w.t[e] = from_float<T>(sum == 0.0f ? 0.0f : __uint_as_float(v[k + e]) * inv);
+          *reinterpret_cast<uint4*>(out + 32 * c + k) = w.u;
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kSoftWarps + kConvWarps) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
+  }
+}
+
+template <typename T, int D>
+int prompt_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
+  constexpr int smem = prompt_smem<D, sizeof(T) == 4>();
+  static DeviceOnce once;
+  const cudaError_t e = once.smem(device_of(ctx), (const void*)kv_attention_prompt<T, D>, smem);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "kv_attention");
+  const int per_block = 2 * (kTileRows / (a.q_heads / a.cache.heads));
+  const int64_t items = a.batch.starts ? a.batch.rows / per_block + a.batch.n : 2 * (int64_t)a.batch.n;
+  launch_pdl(kv_attention_prompt<T, D>, dim3((unsigned)items, a.cache.heads), dim3(kPromptThreads), smem, st, a);
+  count_launch(ctx);
+  return check_cuda(ctx, cudaGetLastError(), "kv_attention");
+}
+
+}  // namespace
+
+bool prompt_pays(Ctx* ctx, const AttnArgs& a, int dtype, int64_t rows) {
+  const int group = a.q_heads / a.cache.heads;
+  if (group > kTileRows || (a.cache.dim != 64 && a.cache.dim != 128) || (dtype == QCFG_FP32 && a.cache.dim != 64)) return false;
+  return rows * group >= 64 && (a.batch.rows * group + 255) / 256 * a.cache.heads >= sm_count(ctx) / 4;
+}
+
+int launch_prompt(Ctx* ctx, const AttnArgs& a, int dtype, cudaStream_t st) {
+  if (dtype == QCFG_FP32) return prompt_as<float, 64>(ctx, a, st);
+  if (dtype == QCFG_BF16) return a.cache.dim == 64 ? prompt_as<__nv_bfloat16, 64>(ctx, a, st) : prompt_as<__nv_bfloat16, 128>(ctx, a, st);
+  return a.cache.dim == 64 ? prompt_as<__half, 64>(ctx, a, st) : prompt_as<__half, 128>(ctx, a, st);
+}
+
+}  // namespace qcfg
