@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
       for (int n = 0; n < NR; ++n)
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-          const float shift = kWeightBias - (ref[n][z] == -INFINITY ? 0.0f : ref[n][z]);
+          const float shift = weight_bias<WIDE>() - (ref[n][z] == -INFINITY ? 0.0f : ref[n][z]);
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
             const float f = fmaxf(f_row[n][z] * kf[p], 1.2e-38f);
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
         }
       float now = fmaxf(unit, fmaxf(vf[0], vf[1]));
       if (now > 0.0f) now = fmaxf(now, 1.2e-38f);
-      if (__any_sync(0xffffffffu, over > kWeightMost || now != unit) || fresh) {
+      if (__any_sync(0xffffffffu, over > weight_bias<WIDE>() + kWeightSlack || now != unit) || fresh) {
         inv = now > 0.0f ? __fdiv_rn(1.0f, now) : 0.0f;
         const float change = unit * inv;
         unit = now;
@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
             float m = fmaxf(fmaxf(s[0][n][z], s[0][n][2 + z]), fmaxf(s[1][n][z], s[1][n][2 + z]));
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            m = fmaxf(m - kWeightBias + was, ref[n][z]);
+            m = fmaxf(m - weight_bias<WIDE>() + was, ref[n][z]);
             const float base = m == -INFINITY ? 0.0f : m;
             const float keep = ex2(ref[n][z] - base);
             ref[n][z] = m;

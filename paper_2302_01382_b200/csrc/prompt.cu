@@ -48,6 +48,11 @@ __device__ __forceinline__ void mma_f16_ta(uint32_t d, uint32_t a_tmem, uint64_t
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                ::"r"(d), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+                 "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]) : "r"(taddr));
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
                ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
@@ -80,17 +85,17 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
   __shared__ float unit_word, unit_parts[kConvWarps];
   __shared__ Scales scales[kTables];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int group = a.q_heads / a.cache.heads, page = a.pool.page, hk = blockIdx.y;
+  const int group = a.q_heads / a.cache.heads, page = a.pool.page, item = blockIdx.x / a.cache.heads, hk = blockIdx.x - item * a.cache.heads;
   const int per_tile = kTileRows / group, per_block = 2 * per_tile;    // query tokens
 
-  // ---- which rows: entries own rows / per_block + 1 blocks each, the last tokens (the longest rows) first
+  // ---- which rows: entries own rows / per_block + 1 blocks each and head, the last tokens (the longest rows) first
   int64_t first;
-  const int entry = entry_of_item(a.batch, blockIdx.x, per_block, 1, first);
+  const int entry = entry_of_item(a.batch, item, per_block, 1, first);
   if (entry < 0 || entry >= a.batch.n) return;
   int64_t row0, row1;
   entry_rows(a.batch, entry, row0, row1);
   const int rows = (int)(row1 - row0), tiles = (rows + per_block - 1) / per_block;
-  const int64_t nth = blockIdx.x - first;
+  const int64_t nth = item - first;
   if (nth >= tiles) return;
   const int t_first = (tiles - 1 - (int)nth) * per_block;              // first query token
   const int s = entry_seq(a.batch, a.pool, entry, a.err);
@@ -192,7 +197,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
   const uint32_t tmem = tmem_at;
   const int tok_lo = seen_hi > 0 ? seen_lo / kStepTokens * kStepTokens : 0;
   const int steps = seen_hi > tok_lo ? (seen_hi - tok_lo + kStepTokens - 1) / kStepTokens : 0;
-  // TMEM columns: scores (and weights) of the tiles, accumulators, second halves of the weights
+  // TMEM columns: scores (then weights, with their second halves behind them) of the tiles, accumulators, and for fp32 those of the second
+  // halves: an MMA's sum is not rounded but cut, so small products are not added to large sums one by one
   const uint32_t s_at = tmem, o_at = tmem + 256, l_at = tmem + 384;
 
   if (steps > 0 && warp >= kSoftWarps && warp < kSoftWarps + kConvWarps) {
@@ -313,8 +319,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       if (!elected) return;
       const uint64_t k0 = tile_desc(k_sm + (j & 1) * kv_tile_bytes<D>(), 16);
 #pragma unroll
-      for (int part = 0; part < (WIDE ? 2 : 1); ++part) {
-        const uint64_t q0 = tile_desc(q_sm + i * q_tile_bytes<D, WIDE>() + part * kTileRows * D * 2, 16);
+      for (int part = 0; part < (WIDE ? 2 : 1); ++part) {       // the queries' second halves first: they are added up while the sum is small
+        const uint64_t q0 = tile_desc(q_sm + i * q_tile_bytes<D, WIDE>() + (WIDE && part == 0 ? kTileRows * D * 2 : 0), 16);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint32_t off = ((k >> 2) * HALF + (k & 3) * 32) >> 4;
@@ -330,7 +336,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       for (int part = 0; part < (WIDE ? 2 : 1); ++part)
 #pragma unroll
         for (int k = 0; k < kStepTokens / 16; ++k)
-          mma_f16_ta(o_at + D * i, (part ? l_at + 64 * i : s_at + 128 * i) + 8 * k, v0 + ((k * 2048) >> 4), kIdescO, j + part + k > 0);
+          mma_f16_ta((part ? l_at : o_at) + D * i, s_at + 128 * i + 64 * part + 8 * k, v0 + ((k * 2048) >> 4), kIdescO, j + k > 0);
     };
     ok = mbar_wait_warp(k_full, 0, abort_flag, a.err);
     tc_fence_after();
@@ -365,7 +371,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     // ------------------------------------------------------------------ weights
     const int i = warp >> 2;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
-    const uint32_t s_row = s_at + 128 * i + lanes, o_row = o_at + D * i + lanes, l_row = l_at + 64 * i + lanes;
+    const uint32_t s_row = s_at + 128 * i + lanes, o_row = o_at + D * i + lanes, l_row = l_at + D * i + lanes;
     float ref = -INFINITY, sum = 0.0f;
     bool ok = true;
     const int n = i == 0 || two ? steps : 0;
@@ -375,41 +381,69 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       if (!mbar_wait_warp(s_full + 8 * i, j & 1, abort_flag, a.err)) { ok = false; break; }
       tc_fence_after();
       const Scales& sc = scales[j % kTables];
-      float f[kGroups];
       bool some = false;
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        f[g] = sc.key[g];
-        some |= f[g] < 0.0f;
-        f[g] = fmaxf(row_f * f[g], 1.2e-38f);
-      }
+      for (int g = 0; g < kGroups; ++g) some |= sc.key[g] < 0.0f;
       const bool masked = __any_sync(0xffffffffu, some || from > 0 || to < kStepTokens);
-      // scores that are not seen, of 32 columns
-      auto mask = [&](uint32_t (&v)[32], int c) {
+      // scores of 16 tokens that are not seen
+      auto mask = [&](uint32_t (&v)[16], int g) {
+        const bool none = sc.key[g] < 0.0f;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          const int t = 32 * c + k;
-          if (t < from || t >= to || sc.key[2 * c + (k >> 4)] < 0.0f) v[k] = 0xff800000u;
+        for (int k = 0; k < 16; ++k) {
+          const int t = 16 * g + k;
+          if (t < from || t >= to || none) v[k] = 0xff800000u;
         }
       };
-      float most = -INFINITY;
+      // Weights of the step against a reference, in registers; `part` their sum (of the unscaled exponentials).  False: some sum of 16 is so
+      // large that a weight may not fit fp16.  The scores of the next 16 tokens are on their way while 16 are worked on.
+      uint32_t p[64], l[WIDE ? 64 : 1];
+      float part;
+      auto weigh = [&]() {
+        const float shift = weight_bias<WIDE>() - (ref == -INFINITY ? 0.0f : ref);
+        bool fits = true;
+        part = 0.0f;
+        uint32_t v[2][16];
+        tmem_ld16(s_row, v[0]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t v[32];
-        tmem_ld32_issue(s_row + 32 * c, v);
-        tmem_ld_wait();
-        if (masked) mask(v, c);
+        for (int g = 0; g < kGroups; ++g) {
+          const float f1 = fmaxf(row_f * sc.key[g], 1.2e-38f), at1 = shift + sc.log_share[g];
+          const float2 fg = make_float2(f1, f1), at = make_float2(at1, at1);
+          tmem_ld_wait();
+          if (g + 1 < kGroups) tmem_ld16(s_row + 16 * (g + 1), v[(g + 1) & 1]);
+          uint32_t (&x16)[16] = v[g & 1];
+          if (masked) mask(x16, g);
+          float2 acc = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          float m = __uint_as_float(v[16 * z]);
-#pragma unroll
-          for (int k = 1; k < 16; ++k) m = fmaxf(m, __uint_as_float(v[16 * z + k]));
-          most = fmaxf(most, m * f[2 * c + z]);
+          for (int k = 0; k < 8; ++k) {
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(x16[2 * k]), __uint_as_float(x16[2 * k + 1])), fg, at);
+            const float2 e = make_float2(ex2(x.x), ex2(x.y));
+            acc = __fadd2_rn(acc, e);
+            const __half2 h = __floats2half2_rn(e.x, e.y);
+            p[8 * g + k] = h2_bits(h);
+            if (WIDE) l[8 * g + k] = pack_h2(e.x - __low2float(h), e.y - __high2float(h));
+          }
+          const float of16 = acc.x + acc.y;
+          fits = fits && of16 <= 65504.0f;
+          part = fmaf(of16, sc.inv_share[g], part);
         }
-      }
-      if (__any_sync(0xffffffffu, most > ref + (kWeightMost - kWeightBias) || (ref == -INFINITY && most > -INFINITY))) {
-        const float now = fmaxf(ref, most), keep = ex2(ref - (now == -INFINITY ? 0.0f : now));
-        ref = now;
+        return fits;
+      };
+      // The reference is found anew only where the one in use does not do: at the first step, and when scores outgrow it.
+      if (__any_sync(0xffffffffu, ref == -INFINITY) || !__all_sync(0xffffffffu, weigh())) {
+        float most = ref;
+#pragma unroll 1
+        for (int g = 0; g < kGroups; ++g) {
+          uint32_t v[16];
+          tmem_ld16(s_row + 16 * g, v);
+          tmem_ld_wait();
+          if (masked) mask(v, g);
+          float m = __uint_as_float(v[0]);
+#pragma unroll
+          for (int k = 1; k < 16; ++k) m = fmaxf(m, __uint_as_float(v[k]));
+          most = fmaxf(most, m * fmaxf(row_f * sc.key[g], 1.2e-38f));
+        }
+        const float keep = ex2(ref - (most == -INFINITY ? 0.0f : most));
+        ref = most;
         sum *= keep;
         if (j > 0) {      // the products so far have been completed in front of these scores
 #pragma unroll 1
@@ -420,32 +454,29 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
 #pragma unroll
             for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * keep);
             tmem_st32(o_row + 32 * c, v);
+            if constexpr (WIDE) {
+              tmem_ld32_issue(l_row + 32 * c, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * keep);
+              tmem_st32(l_row + 32 * c, v);
+            }
           }
         }
+        weigh();
       }
-      const float shift = kWeightBias - (ref == -INFINITY ? 0.0f : ref);
+      sum += part;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t v[32], p[16], l[WIDE ? 16 : 1];
-        tmem_ld32_issue(s_row + 32 * c, v);
-        tmem_ld_wait();
-        if (masked) mask(v, c);
+      for (int c = 0; c < 4; ++c) {        // over the scores, all of which have been read
+        uint32_t x[16];
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const float fg = f[2 * c + z], at = shift + sc.log_share[2 * c + z];
-          float part = 0.0f;
+        for (int k = 0; k < 16; ++k) x[k] = p[16 * c + k];
+        tmem_st16(s_row + 16 * c, x);
+        if constexpr (WIDE) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float e0 = ex2(fmaf(__uint_as_float(v[16 * z + 2 * k]), fg, at)), e1 = ex2(fmaf(__uint_as_float(v[16 * z + 2 * k + 1]), fg, at));
-            part += e0 + e1;
-            const __half2 h = __floats2half2_rn(e0, e1);
-            p[8 * z + k] = h2_bits(h);
-            if (WIDE) l[8 * z + k] = pack_h2(e0 - __low2float(h), e1 - __high2float(h));
-          }
-          sum = fmaf(part, sc.inv_share[2 * c + z], sum);
+          for (int k = 0; k < 16; ++k) x[k] = l[16 * c + k];
+          tmem_st16(s_row + 64 + 16 * c, x);
         }
-        tmem_st16(s_row + 16 * c, p);      // over columns read in this step's chunks up to c
-        if constexpr (WIDE) tmem_st16(l_row + 16 * c, l);
       }
       tmem_st_wait();
       tc_fence_before();
@@ -465,6 +496,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
         if (n > 0) {
           tmem_ld32_issue(o_row + 32 * c, v);
           tmem_ld_wait();
+          if constexpr (WIDE) {
+            uint32_t u[32];
+            tmem_ld32_issue(l_row + 32 * c, u);
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + __uint_as_float(u[k]));
+          }
         } else {
 #pragma unroll
           for (int k = 0; k < 32; ++k) v[k] = 0u;
@@ -497,7 +535,7 @@ int prompt_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return check_cuda(ctx, e, "kv_attention");
   const int per_block = 2 * (kTileRows / (a.q_heads / a.cache.heads));
   const int64_t items = a.batch.starts ? a.batch.rows / per_block + a.batch.n : 2 * (int64_t)a.batch.n;
-  launch_pdl(kv_attention_prompt<T, D>, dim3((unsigned)items, a.cache.heads), dim3(kPromptThreads), smem, st, a);
+  launch_pdl(kv_attention_prompt<T, D>, dim3((unsigned)(items * a.cache.heads)), dim3(kPromptThreads), smem, st, a);
   count_launch(ctx);
   return check_cuda(ctx, cudaGetLastError(), "kv_attention");
 }
