@@ -4,9 +4,9 @@
 // group).  It walks the tokens its rows see in steps of 128:
 //   warps 0-3, 4-7   one thread a row of tile 0 / tile 1: scores from TMEM, running reference, weights back to TMEM as fp16
 //                    (over the scores they come from), which is where the second product takes its A operand from.
-//   warps 8-11       bring the codes of the next step from global memory to registers, and turn the present ones into fp16 in shared
+//   warps 8-10       bring the codes of the next step from global memory to registers, and turn the present ones into fp16 in shared
 //                    memory: 128-byte rows, 128B swizzle, for keys (K-major B operand) and values (MN-major) alike.
-//   warp 12          issues the MMAs: S0, S1, then for each step O0 += P0 V, S0 of the next step, O1 += P1 V, S1 of the next step.
+//   warp 11          issues the MMAs: S0, S1, then for each step O0 += P0 V, S0 of the next step, O1 += P1 V, S1 of the next step.
 //                    While one tile's weights are computed, the tensor core works for the other.
 // Each step and tile costs 2 x 128 x 128 x dim products (1024 cycles for both tiles at dim 128, twice) and 128 x 128 exponentials
 // (16 per cycle: 2048 cycles for both tiles): the exponentials and the tensor core are equally long, and the issue slots nearly so.
@@ -24,7 +24,7 @@ namespace {
 constexpr int kTileRows = 128;
 constexpr int kStepTokens = 128;
 constexpr int kGroups = kStepTokens / 16;        // scales are looked up for each 16 tokens
-constexpr int kSoftWarps = 8, kConvWarps = 4;
+constexpr int kSoftWarps = 8, kConvWarps = 3;      // and one that issues: three warps a scheduler, 168 registers a thread
 constexpr int kPromptThreads = 32 * (kSoftWarps + kConvWarps + 1);
 constexpr int kTables = 4;
 
@@ -35,7 +35,7 @@ template <int D, bool WIDE> __host__ __device__ constexpr int prompt_smem() {
   return used < 118 * 1024 ? 118 * 1024 : used;  // one block per SM: it takes all of the TMEM
 }
 
-struct Scales {          // of a step
+struct __align__(16) Scales {          // of a step
   float key[kGroups];    // -1: no such tokens
   float log_share[kGroups], inv_share[kGroups];
 };
@@ -53,17 +53,18 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
                : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
                  "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]) : "r"(taddr));
 }
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+               ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
                ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
                  "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
-  uint32_t a[16], b[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) { a[i] = v[i]; b[i] = v[16 + i]; }
-  tmem_st16(taddr, a);
-  tmem_st16(taddr + 16, b);
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -77,7 +78,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
   asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr bool WIDE = sizeof(T) == 4;
   constexpr int HALVES = D / 64, HALF = kTileRows * 128;              // bytes of 64 columns of a tile
-  constexpr uint32_t kCols = 512;
+  constexpr uint32_t kCols = 512, kPart = WIDE ? 16 : 8;             // columns of the weights of 16 tokens (fp32: two fp16 numbers each)
   extern __shared__ uint8_t raw_smem[];
   __shared__ uint64_t bars[14];
   __shared__ uint32_t tmem_at, magic_word;
@@ -197,40 +198,35 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
   const uint32_t tmem = tmem_at;
   const int tok_lo = seen_hi > 0 ? seen_lo / kStepTokens * kStepTokens : 0;
   const int steps = seen_hi > tok_lo ? (seen_hi - tok_lo + kStepTokens - 1) / kStepTokens : 0;
-  // TMEM columns: scores (then weights, with their second halves behind them) of the tiles, accumulators, and for fp32 those of the second
+  // TMEM columns: scores (then weights) of the tiles, accumulators, and for fp32 those of the second
   // halves: an MMA's sum is not rounded but cut, so small products are not added to large sums one by one
   const uint32_t s_at = tmem, o_at = tmem + 256, l_at = tmem + 384;
 
   if (steps > 0 && warp >= kSoftWarps && warp < kSoftWarps + kConvWarps) {
     // ------------------------------------------------------------------ codes to fp16
-    const int cw = warp - kSoftWarps;              // tokens 32 cw .. 32 cw + 31 of a step
+    const int cw = warp - kSoftWarps;              // runs of 8 tokens cw, cw + 3, ... of a step's 16
+    constexpr int RUNS = (kStepTokens / 8 + kConvWarps - 1) / kConvWarps;
     const uint32_t magic = *(volatile uint32_t*)&magic_word;
     const int32_t* table = a.pool.table + (int64_t)(s < 0 ? 0 : s) * a.pool.max_pages;
-    // pages of the warp's two groups of 16 tokens, -1 for those that are not there
-    auto look_up = [&](int step, int (&p)[2]) {
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const int tok = tok_lo + step * kStepTokens + 32 * cw + 16 * z;
-        p[z] = -1;
-        if (step < steps && tok < len) {
-          p[z] = __ldg(table + tok / page);
-          if (p[z] < 0 || p[z] >= a.pool.n_pages) {
-            if (lane == 0) atomicOr(a.err, ERR_PAGE);
-            p[z] = -1;
-          }
-        }
-      }
+    // lanes 0-7: the page of a group of 16 tokens, -1 where there is none
+    auto look_up = [&](int step) {
+      const int tok = tok_lo + step * kStepTokens + 16 * (lane & 7);
+      if (step >= steps || tok >= len) return -1;
+      const int p = __ldg(table + tok / page);
+      if (p >= 0 && p < a.pool.n_pages) return p;
+      if (lane < 8 && cw == 0) atomicOr(a.err, ERR_PAGE);
+      return -1;
     };
     // the largest value scale of the range
     float unit = 0.0f;
-    for (int64_t tok = tok_lo / page * page + (int64_t)(cw * 32 + lane) * page; tok < seen_hi && tok < len; tok += 128 * page) {
+    for (int64_t tok = tok_lo / page * page + (int64_t)(cw * 32 + lane) * page; tok < seen_hi && tok < len; tok += 32 * kConvWarps * page) {
       const int p = __ldg(table + tok / page);
       if (p >= 0 && p < a.pool.n_pages) unit = fmaxf(unit, __ldg(a.cache.v_absmax + (int64_t)p * a.cache.heads + hk));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, o));
     if (lane == 0) unit_parts[cw] = unit;
-    asm volatile("bar.sync 1, 128;" ::: "memory");
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kConvWarps) : "memory");
 #pragma unroll
     for (int w = 0; w < kConvWarps; ++w) unit = fmaxf(unit, unit_parts[w]);
     unit *= 1.0f / kQmax8;
@@ -238,53 +234,66 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     if (tid == 32 * kSoftWarps) unit_word = unit;
     const float inv_unit = unit > 0.0f ? __fdiv_rn(1.0f, unit) : 0.0f;
 
-    // a warp-wide access: 8 tokens x 4 chunks of 16 codes; 4 of tokens x HALVES of columns per tile
+    // a warp-wide access: 8 tokens x 4 chunks of 16 codes
     const int r8 = lane >> 2, c4 = lane & 3;
-    const uint32_t put = (uint32_t)((32 * cw + r8) * 128), flip = (uint32_t)r8;
-    auto load = [&](const int8_t* base, const int (&p)[2], int step, uint4 (&to)[4 * HALVES]) {
+    const uint32_t put = (uint32_t)(r8 * 128), flip = (uint32_t)r8;
+    // Where a lane's codes of its runs lie in both tensors.  Tokens that are not there are read from page 0: whatever the codes are, they
+    // are numbers, their scores are masked and their weights 0.
+    int in_page[RUNS];
+    int64_t place[RUNS];
 #pragma unroll
-      for (int o = 0; o < 4; ++o) {
-        const int z = o >> 1, tok = tok_lo + step * kStepTokens + 32 * cw + 8 * o;
-        const int8_t* from = base + (((int64_t)p[z] * a.cache.heads + hk) * page + (tok & (page - 1)) + r8) * D + c4 * 16;
+    for (int o = 0; o < RUNS; ++o) in_page[o] = ((hk * page + ((8 * (cw + o * kConvWarps)) & (page - 1)) + r8) * D + c4 * 16);
+    const int page_bytes = a.cache.heads * page * D;
+    auto find = [&](int pages) {
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) to[o * HALVES + h] = p[z] >= 0 ? __ldg(reinterpret_cast<const uint4*>(from + h * 64)) : make_uint4(0, 0, 0, 0);
+      for (int o = 0; o < RUNS; ++o) place[o] = (int64_t)max(__shfl_sync(0xffffffffu, pages, min((cw + o * kConvWarps) >> 1, kGroups - 1)), 0) * page_bytes + in_page[o];
+    };
+    auto load = [&](const int8_t* base, uint4 (&to)[RUNS * HALVES]) {
+#pragma unroll
+      for (int o = 0; o < RUNS; ++o) {
+        if (cw + o * kConvWarps >= kStepTokens / 8) break;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) to[o * HALVES + h] = __ldg(reinterpret_cast<const uint4*>(base + place[o] + h * 64));
       }
     };
-    auto store = [&](uint32_t tile, const uint4 (&from)[4 * HALVES]) {
+    auto store = [&](uint32_t tile, const uint4 (&from)[RUNS * HALVES]) {
 #pragma unroll
-      for (int o = 0; o < 4; ++o)
+      for (int o = 0; o < RUNS; ++o) {
+        const int run = cw + o * kConvWarps;
+        if (run >= kStepTokens / 8) break;
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
-          const uint4 v = from[o * HALVES + h];
+          uint4 v = from[o * HALVES + h];
+          asm volatile("" : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w) :: "memory");      // not in front of the wait for the stage
           const uint32_t x = v.x ^ 0x80808080u, y = v.y ^ 0x80808080u, z = v.z ^ 0x80808080u, w = v.w ^ 0x80808080u;
-          const uint32_t at = tile + put + o * 1024 + h * HALF;
+          const uint32_t at = tile + put + run * 1024 + h * HALF;
           st_shared_v4(at + (((2 * c4) ^ flip) << 4), two_codes<0x4140>(x, magic), two_codes<0x4342>(x, magic), two_codes<0x4140>(y, magic), two_codes<0x4342>(y, magic));
           st_shared_v4(at + (((2 * c4 + 1) ^ flip) << 4), two_codes<0x4140>(z, magic), two_codes<0x4342>(z, magic), two_codes<0x4140>(w, magic), two_codes<0x4342>(w, magic));
         }
-    };
-    int now[2], next[2];
-    uint4 kc[4 * HALVES], vc[4 * HALVES];
-    float k_max = 0.0f, v_max = 0.0f;
-    auto load_scales = [&](const int (&p)[2]) {       // lanes 0 and 1: the warp's two groups
-      const int mine = lane & 1 ? p[1] : p[0];
-      k_max = v_max = -1.0f;
-      if (lane < 2 && mine >= 0) {
-        k_max = __ldg(a.cache.k_absmax + (int64_t)mine * a.cache.heads + hk);
-        v_max = __ldg(a.cache.v_absmax + (int64_t)mine * a.cache.heads + hk);
       }
     };
-    look_up(0, now);
-    look_up(1, next);
-    load(a.cache.k, now, 0, kc);
-    load_scales(now);
-    load(a.cache.v, now, 0, vc);
+    uint4 kc[RUNS * HALVES], vc[RUNS * HALVES];
+    float k_max = -1.0f, v_max = -1.0f;
+    auto load_scales = [&](int pages) {            // the first warp's lanes 0-7
+      k_max = v_max = -1.0f;
+      if (cw == 0 && lane < kGroups && pages >= 0) {
+        k_max = __ldg(a.cache.k_absmax + (int64_t)pages * a.cache.heads + hk);
+        v_max = __ldg(a.cache.v_absmax + (int64_t)pages * a.cache.heads + hk);
+      }
+    };
+    int next = look_up(0);
+    find(next);
+    load(a.cache.k, kc);
+    load_scales(next);
+    load(a.cache.v, vc);
+    next = look_up(1);
     for (int j = 0; j < steps; ++j) {
       const uint32_t st = j & 1, ph = (j >> 1) & 1;
       if (j >= 2 && !mbar_wait_warp(k_empty + 8 * st, ph ^ 1, abort_flag, a.err)) break;
       store(k_sm + st * kv_tile_bytes<D>(), kc);
-      if (lane < 2) {
+      if (cw == 0 && lane < kGroups) {
         Scales& sc = scales[j % kTables];
-        const int g = 2 * cw + lane;
+        const int g = lane;
         const bool ok = k_max >= 0.0f;
         sc.key[g] = !ok ? -1.0f : k_max > 0.0f ? k_max * (1.0f / kQmax8) : 1.0f;
         // a page of zeros may have any weight
@@ -296,7 +305,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       __syncwarp();
       if (lane == 0) mbar_arrive(k_full + 8 * st);
       if (j + 1 < steps) {
-        load(a.cache.k, next, j + 1, kc);
+        find(next);
+        load(a.cache.k, kc);
         load_scales(next);
       }
       if (j >= 2 && !mbar_wait_warp(v_empty + 8 * st, ph ^ 1, abort_flag, a.err)) break;
@@ -304,8 +314,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(v_full + 8 * st);
-      if (j + 1 < steps) load(a.cache.v, next, j + 1, vc);
-      look_up(j + 2, next);
+      if (j + 1 < steps) load(a.cache.v, vc);
+      next = look_up(j + 2);
     }
   } else if (steps > 0 && warp == kSoftWarps + kConvWarps) {
     // ------------------------------------------------------------------ products
@@ -336,7 +346,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       for (int part = 0; part < (WIDE ? 2 : 1); ++part)
 #pragma unroll
         for (int k = 0; k < kStepTokens / 16; ++k)
-          mma_f16_ta((part ? l_at : o_at) + D * i, s_at + 128 * i + 64 * part + 8 * k, v0 + ((k * 2048) >> 4), kIdescO, j + k > 0);
+          mma_f16_ta((part ? l_at : o_at) + D * i, s_at + 128 * i + kPart * k + 8 * part, v0 + ((k * 2048) >> 4), kIdescO, j + k > 0);
     };
     ok = mbar_wait_warp(k_full, 0, abort_flag, a.err);
     tc_fence_after();
@@ -373,7 +383,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t s_row = s_at + 128 * i + lanes, o_row = o_at + D * i + lanes, l_row = l_at + D * i + lanes;
     float ref = -INFINITY, sum = 0.0f;
-    bool ok = true;
+    bool ok = true, fresh = true;      // fresh: no reference yet
     const int n = i == 0 || two ? steps : 0;
     for (int j = 0; j < n; ++j) {
       const int tok = tok_lo + j * kStepTokens;
@@ -381,103 +391,115 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       if (!mbar_wait_warp(s_full + 8 * i, j & 1, abort_flag, a.err)) { ok = false; break; }
       tc_fence_after();
       const Scales& sc = scales[j % kTables];
+      float f[kGroups], log_share[kGroups], inv_share[kGroups];
+#pragma unroll
+      for (int g = 0; g < kGroups; g += 4) {
+        *reinterpret_cast<float4*>(f + g) = *reinterpret_cast<const float4*>(sc.key + g);
+        *reinterpret_cast<float4*>(log_share + g) = *reinterpret_cast<const float4*>(sc.log_share + g);
+        *reinterpret_cast<float4*>(inv_share + g) = *reinterpret_cast<const float4*>(sc.inv_share + g);
+      }
       bool some = false;
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) some |= sc.key[g] < 0.0f;
+      for (int g = 0; g < kGroups; ++g) {
+        some |= f[g] < 0.0f;
+        f[g] = fmaxf(row_f * f[g], 1.2e-38f);
+      }
       const bool masked = __any_sync(0xffffffffu, some || from > 0 || to < kStepTokens);
-      // scores of 16 tokens that are not seen
-      auto mask = [&](uint32_t (&v)[16], int g) {
-        const bool none = sc.key[g] < 0.0f;
+      // scores of 32 tokens that are not seen
+      auto mask = [&](uint32_t (&v)[32], int c) {
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const int t = 16 * g + k;
-          if (t < from || t >= to || none) v[k] = 0xff800000u;
+        for (int k = 0; k < 32; ++k) {
+          const int t = 32 * c + k;
+          if (t < from || t >= to || sc.key[2 * c + (k >> 4)] < 0.0f) v[k] = 0xff800000u;
         }
       };
-      // Weights of the step against a reference, in registers; `part` their sum (of the unscaled exponentials).  False: some sum of 16 is so
-      // large that a weight may not fit fp16.  The scores of the next 16 tokens are on their way while 16 are worked on.
-      uint32_t p[64], l[WIDE ? 64 : 1];
-      float part;
-      auto weigh = [&]() {
-        const float shift = weight_bias<WIDE>() - (ref == -INFINITY ? 0.0f : ref);
-        bool fits = true;
-        part = 0.0f;
-        uint32_t v[2][16];
-        tmem_ld16(s_row, v[0]);
+      // Weights of 32 tokens at a time, over scores that have been read: group g of 16 in columns kPart * g on.  The next 32 scores are on
+      // their way meanwhile.  The reference is a whole number, and moves only when a row has none yet or a sum of 16 weights no longer
+      // fits fp16: what has been written and summed up is then scaled by a power of two.  So a score is read once, and no
+      // maximum is taken of most.
+      float part = 0.0f;             // of the step's unscaled exponentials
+      uint32_t v[2][32];
+      tmem_ld32_issue(s_row, v[0]);
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          const float f1 = fmaxf(row_f * sc.key[g], 1.2e-38f), at1 = shift + sc.log_share[g];
-          const float2 fg = make_float2(f1, f1), at = make_float2(at1, at1);
-          tmem_ld_wait();
-          if (g + 1 < kGroups) tmem_ld16(s_row + 16 * (g + 1), v[(g + 1) & 1]);
-          uint32_t (&x16)[16] = v[g & 1];
-          if (masked) mask(x16, g);
-          float2 acc = make_float2(0.0f, 0.0f);
+      for (int c = 0; c < 4; ++c) {
+        uint32_t (&x32)[32] = v[c & 1];
+        tmem_ld_wait();
+        if (c < 3) tmem_ld32_issue(s_row + 32 * (c + 1), v[(c + 1) & 1]);
+        if (masked) mask(x32, c);
+        uint32_t p[2][8], l[WIDE ? 2 : 1][WIDE ? 8 : 1];
+        float of16[2];
+        auto take = [&]() {
+          const float shift = weight_bias<WIDE>() - (ref == -INFINITY ? 0.0f : ref);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float2 x = __ffma2_rn(make_float2(__uint_as_float(x16[2 * k]), __uint_as_float(x16[2 * k + 1])), fg, at);
-            const float2 e = make_float2(ex2(x.x), ex2(x.y));
-            acc = __fadd2_rn(acc, e);
-            const __half2 h = __floats2half2_rn(e.x, e.y);
-            p[8 * g + k] = h2_bits(h);
-            if (WIDE) l[8 * g + k] = pack_h2(e.x - __low2float(h), e.y - __high2float(h));
+          for (int z = 0; z < 2; ++z) {
+            const float f1 = f[2 * c + z], at1 = shift + log_share[2 * c + z];
+            const float2 fg = make_float2(f1, f1), at = make_float2(at1, at1);
+            float2 acc[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float2 x = __ffma2_rn(make_float2(__uint_as_float(x32[16 * z + 2 * k]), __uint_as_float(x32[16 * z + 2 * k + 1])), fg, at);
+              const float2 e = make_float2(ex2(x.x), ex2(x.y));
+              acc[k & 1] = __fadd2_rn(acc[k & 1], e);
+              const __half2 h = __floats2half2_rn(e.x, e.y);
+              p[z][k] = h2_bits(h);
+              if (WIDE) l[z][k] = pack_h2(e.x - __low2float(h), e.y - __high2float(h));
+            }
+            acc[0] = __fadd2_rn(acc[0], acc[1]);
+            of16[z] = acc[0].x + acc[0].y;
           }
-          const float of16 = acc.x + acc.y;
-          fits = fits && of16 <= 65504.0f;
-          part = fmaf(of16, sc.inv_share[g], part);
-        }
-        return fits;
-      };
-      // The reference is found anew only where the one in use does not do: at the first step, and when scores outgrow it.
-      if (__any_sync(0xffffffffu, ref == -INFINITY) || !__all_sync(0xffffffffu, weigh())) {
-        float most = ref;
-#pragma unroll 1
-        for (int g = 0; g < kGroups; ++g) {
-          uint32_t v[16];
-          tmem_ld16(s_row + 16 * g, v);
-          tmem_ld_wait();
-          if (masked) mask(v, g);
-          float m = __uint_as_float(v[0]);
+        };
+        take();
+        // (a NaN counts as too large; it stays one)
+        const bool large = !(of16[0] <= 65504.0f) || !(of16[1] <= 65504.0f);
+        if (__any_sync(0xffffffffu, fresh || large)) {
+          float most = -INFINITY;
 #pragma unroll
-          for (int k = 1; k < 16; ++k) m = fmaxf(m, __uint_as_float(v[k]));
-          most = fmaxf(most, m * fmaxf(row_f * sc.key[g], 1.2e-38f));
-        }
-        const float keep = ex2(ref - (most == -INFINITY ? 0.0f : most));
-        ref = most;
-        sum *= keep;
-        if (j > 0) {      // the products so far have been completed in front of these scores
-#pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t v[32];
-            tmem_ld32_issue(o_row + 32 * c, v);
-            tmem_ld_wait();
+          for (int z = 0; z < 2; ++z) {
+            float m = __uint_as_float(x32[16 * z]);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * keep);
-            tmem_st32(o_row + 32 * c, v);
-            if constexpr (WIDE) {
-              tmem_ld32_issue(l_row + 32 * c, v);
+            for (int k = 1; k < 16; ++k) m = fmaxf(m, __uint_as_float(x32[16 * z + k]));
+            most = fmaxf(most, m * f[2 * c + z]);
+          }
+          const float was = ref;
+          if (fresh || large) ref = fmaxf(ref, ceilf(most));
+          fresh = ref == -INFINITY;
+          const float keep = ex2(was - (fresh ? 0.0f : ref));
+          if (__any_sync(0xffffffffu, keep != 1.0f)) {
+            sum *= keep;
+            part *= keep;
+            const __half2 keep2 = __floats2half2_rn(keep, keep);
+#pragma unroll 1
+            for (int h = 0; h < (WIDE ? 4 * c : 2 * c); ++h) {
+              uint32_t w[8];
+              tmem_ld8(s_row + 8 * h, w);
               tmem_ld_wait();
 #pragma unroll
-              for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * keep);
-              tmem_st32(l_row + 32 * c, v);
+              for (int k = 0; k < 8; ++k) w[k] = h2_bits(__hmul2(*reinterpret_cast<const __half2*>(&w[k]), keep2));
+              tmem_st8(s_row + 8 * h, w);
             }
+            // the products so far have been completed in front of these scores
+#pragma unroll 1
+            for (int h = 0; j > 0 && h < (WIDE ? 2 : 1) * D / 16; ++h) {
+              const uint32_t at = h < D / 16 ? o_row + 16 * h : l_row + 16 * (h - D / 16);
+              uint32_t w[16];
+              tmem_ld16(at, w);
+              tmem_ld_wait();
+#pragma unroll
+              for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * keep);
+              tmem_st16(at, w);
+            }
+            tmem_st_wait();
           }
+          take();
         }
-        weigh();
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          part = fmaf(of16[z], inv_share[2 * c + z], part);
+          tmem_st8(s_row + kPart * (2 * c + z), p[z]);
+          if constexpr (WIDE) tmem_st8(s_row + kPart * (2 * c + z) + 8, l[z]);
+        }
       }
       sum += part;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {        // over the scores, all of which have been read
-        uint32_t x[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) x[k] = p[16 * c + k];
-        tmem_st16(s_row + 16 * c, x);
-        if constexpr (WIDE) {
-#pragma unroll
-          for (int k = 0; k < 16; ++k) x[k] = l[16 * c + k];
-          tmem_st16(s_row + 64 + 16 * c, x);
-        }
-      }
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
