@@ -80,33 +80,54 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
   constexpr int HALVES = D / 64, HALF = kTileRows * 128;              // bytes of 64 columns of a tile
   constexpr uint32_t kCols = 512, kPart = WIDE ? 16 : 8;             // columns of the weights of 16 tokens (fp32: two fp16 numbers each)
   extern __shared__ uint8_t raw_smem[];
-  __shared__ uint64_t bars[14];
+  __shared__ uint64_t bars[15];
   __shared__ uint32_t tmem_at, magic_word;
-  __shared__ int abort_word, seen_lo, seen_hi;
+  __shared__ int abort_word;
+  __shared__ struct { int64_t row0; int rows, nth, seq, len, claim; } mine;
   __shared__ float unit_word, unit_parts[kConvWarps];
   __shared__ Scales scales[kTables];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group = a.q_heads / a.cache.heads, page = a.pool.page, item = blockIdx.x / a.cache.heads, hk = blockIdx.x - item * a.cache.heads;
   const int per_tile = kTileRows / group, per_block = 2 * per_tile;    // query tokens
 
-  // ---- which rows: entries own rows / per_block + 1 blocks each and head, the last tokens (the longest rows) first
-  int64_t first;
-  const int entry = entry_of_item(a.batch, item, per_block, 1, first);
-  if (entry < 0 || entry >= a.batch.n) return;
-  int64_t row0, row1;
-  entry_rows(a.batch, entry, row0, row1);
-  const int rows = (int)(row1 - row0), tiles = (rows + per_block - 1) / per_block;
-  const int64_t nth = item - first;
-  if (nth >= tiles) return;
-  const int t_first = (tiles - 1 - (int)nth) * per_block;              // first query token
-  const int s = entry_seq(a.batch, a.pool, entry, a.err);
-  const int len = s < 0 ? 0 : seq_len(a.pool, s);
+  // ---- which rows: entry i owns the blocks starts[i] / per_block + i .. of each head, the last tokens (the longest rows) first.  A thread
+  // looks at an entry, so that all that has to be known is fetched at once.
+  if (tid == 0) mine.claim = -1;
+  __syncthreads();
+  for (int i0 = 0; i0 < a.batch.n; i0 += kPromptThreads) {
+    const int i = i0 + tid;
+    if (i < a.batch.n) {
+      int64_t r0, r1;
+      entry_rows(a.batch, i, r0, r1);
+      const int q = entry_seq(a.batch, a.pool, i, a.err), held = q < 0 ? 0 : seq_len(a.pool, q);
+      const int64_t nth = item - (a.batch.starts ? (int64_t)a.batch.starts[i] / per_block + i : 2 * (int64_t)i);
+      if (nth >= 0 && nth < (r1 - r0 + per_block - 1) / per_block && atomicCAS(&mine.claim, -1, i) == -1) {      // one at most, where starts ascend
+        mine.row0 = r0;
+        mine.rows = (int)(r1 - r0);
+        mine.nth = (int)nth;
+        mine.seq = q;
+        mine.len = held;
+      }
+    }
+  }
+  __syncthreads();
+  if (mine.claim < 0) return;
+  const int64_t row0 = mine.row0;
+  const int rows = mine.rows, s = mine.seq, len = mine.len;
+  const int t_first = ((rows + per_block - 1) / per_block - 1 - mine.nth) * per_block;              // first query token
+  const int t_last = min(t_first + per_block, rows) - 1;
   const bool two = t_first + per_tile < rows;                          // the second tile has rows
+  // the tokens seen: both ends ascend with the position
+  int seen_lo, seen_hi, unused;
+  seen_range(a, (int64_t)len - rows + t_last, len, unused, seen_hi);
+  seen_range(a, max((int64_t)len - rows + t_first, (int64_t)0), len, seen_lo, unused);
+  const int tok_lo = seen_hi > 0 ? seen_lo / kStepTokens * kStepTokens : 0;
+  const int steps = seen_hi > tok_lo ? (seen_hi - tok_lo + kStepTokens - 1) / kStepTokens : 0;
 
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
   const uint32_t q_sm = smem_u32(smem), k_sm = q_sm + 2 * q_tile_bytes<D, WIDE>(), v_sm = k_sm + 2 * kv_tile_bytes<D>();
   const uint32_t bar = smem_u32(bars);
-  const uint32_t k_full = bar, k_empty = bar + 16, v_full = bar + 32, v_empty = bar + 48, s_full = bar + 64, p_ready = bar + 80, o_done = bar + 96;
+  const uint32_t k_full = bar, k_empty = bar + 16, v_full = bar + 32, v_empty = bar + 48, s_full = bar + 64, p_ready = bar + 80, o_done = bar + 96, q_full = bar + 112;
   volatile int* abort_flag = &abort_word;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -118,9 +139,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       mbar_init(p_ready + 8 * i, 4);
       mbar_init(o_done + 8 * i, 1);
     }
+    mbar_init(q_full, kSoftWarps);
     abort_word = 0;
-    seen_lo = 0x7fffffff;
-    seen_hi = 0;
     magic_word = 0x64646464u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -128,79 +148,15 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_at)), "r"(kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  __syncthreads();
-  // The next kernel may begin only now: it could take the TMEM of an SM in front of this block, and then wait for it.
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
-  // ---- queries: a thread a row
-  int lo = 0, hi = 0x7fffffff, out_row = -1, out_head = 0;
-  float row_f = 0.0f;
-  if (warp < kSoftWarps) {
-    const int tile = warp >> 2, r = tid & 127;
-    const int tok = t_first + tile * per_tile + r / group;
-    const bool real = r < per_tile * group && tok < rows;
-    const T* q = nullptr;
-    if (real) {
-      out_row = tok;
-      out_head = hk * group + r % group;
-      q = reinterpret_cast<const T*>(a.q) + (row0 + tok) * a.q_row + out_head * a.q_head;
-      seen_range(a, (int64_t)len - rows + tok, len, lo, hi);
-      if (hi > lo) {
-        atomicMin(&seen_lo, lo);
-        atomicMax(&seen_hi, hi);
-      }
-    }
-    constexpr int V = Vec<T>::N;
-    unsigned top = 0;
-#pragma unroll 4
-    for (int c = 0; c < D / V; ++c) {
-      float f[V];
-      if (real) {
-        load_vec<T>(q + c * V, f);
-#pragma unroll
-        for (int j = 0; j < V; ++j) top = max(top, abs_bits(f[j]));
-      }
-    }
-    const int shift = row_shift(top);
-    const float up = exp2_of(shift);
-    row_f = a.scale * exp2_of(-shift);
-    const uint32_t base = q_sm + tile * q_tile_bytes<D, WIDE>() + r * 128;
-#pragma unroll 4
-    for (int c = 0; c < D / 8; ++c) {
-      float f[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = 0.0f;
-      if (real) {
-        if constexpr (WIDE) {
-          load_vec<T>(q + c * 8, reinterpret_cast<float(&)[Vec<T>::N]>(f[0]));
-          load_vec<T>(q + c * 8 + 4, reinterpret_cast<float(&)[Vec<T>::N]>(f[4]));
-        } else {
-          load_vec<T>(q + c * 8, reinterpret_cast<float(&)[Vec<T>::N]>(f[0]));
-        }
-      }
-      uint32_t w[4], l[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float x = f[2 * j] * up, y = f[2 * j + 1] * up;
-        const __half2 h = __floats2half2_rn(x, y);
-        w[j] = h2_bits(h);
-        if (WIDE) l[j] = pack_h2(x - __low2float(h), y - __high2float(h));
-      }
-      const uint32_t to = base + (c >> 3) * HALF + (((c & 7) ^ (r & 7)) << 4);
-      st_shared_v4(to, w[0], w[1], w[2], w[3]);
-      if (WIDE) st_shared_v4(to + kTileRows * D * 2, l[0], l[1], l[2], l[3]);
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_at;
-  const int tok_lo = seen_hi > 0 ? seen_lo / kStepTokens * kStepTokens : 0;
-  const int steps = seen_hi > tok_lo ? (seen_hi - tok_lo + kStepTokens - 1) / kStepTokens : 0;
   // TMEM columns: scores (then weights) of the tiles, accumulators, and for fp32 those of the second
   // halves: an MMA's sum is not rounded but cut, so small products are not added to large sums one by one
   const uint32_t s_at = tmem, o_at = tmem + 256, l_at = tmem + 384;
+  // The next kernel may begin only now: it could take the TMEM of an SM in front of this block, and then wait for it.
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   if (steps > 0 && warp >= kSoftWarps && warp < kSoftWarps + kConvWarps) {
     // ------------------------------------------------------------------ codes to fp16
@@ -217,23 +173,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       if (lane < 8 && cw == 0) atomicOr(a.err, ERR_PAGE);
       return -1;
     };
-    // the largest value scale of the range
-    float unit = 0.0f;
-    for (int64_t tok = tok_lo / page * page + (int64_t)(cw * 32 + lane) * page; tok < seen_hi && tok < len; tok += 32 * kConvWarps * page) {
-      const int p = __ldg(table + tok / page);
-      if (p >= 0 && p < a.pool.n_pages) unit = fmaxf(unit, __ldg(a.cache.v_absmax + (int64_t)p * a.cache.heads + hk));
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, o));
-    if (lane == 0) unit_parts[cw] = unit;
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * kConvWarps) : "memory");
-#pragma unroll
-    for (int w = 0; w < kConvWarps; ++w) unit = fmaxf(unit, unit_parts[w]);
-    unit *= 1.0f / kQmax8;
-    if (unit > 0.0f) unit = fmaxf(unit, 1.2e-38f);
-    if (tid == 32 * kSoftWarps) unit_word = unit;
-    const float inv_unit = unit > 0.0f ? __fdiv_rn(1.0f, unit) : 0.0f;
-
     // a warp-wide access: 8 tokens x 4 chunks of 16 codes
     const int r8 = lane >> 2, c4 = lane & 3;
     const uint32_t put = (uint32_t)(r8 * 128), flip = (uint32_t)r8;
@@ -287,6 +226,23 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     load_scales(next);
     load(a.cache.v, vc);
     next = look_up(1);
+    // the largest value scale of the range
+    float unit = 0.0f;
+    for (int64_t tok = tok_lo / page * page + (int64_t)(cw * 32 + lane) * page; tok < seen_hi && tok < len; tok += 32 * kConvWarps * page) {
+      const int p = __ldg(table + tok / page);
+      if (p >= 0 && p < a.pool.n_pages) unit = fmaxf(unit, __ldg(a.cache.v_absmax + (int64_t)p * a.cache.heads + hk));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, o));
+    if (lane == 0) unit_parts[cw] = unit;
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kConvWarps) : "memory");
+#pragma unroll
+    for (int w = 0; w < kConvWarps; ++w) unit = fmaxf(unit, unit_parts[w]);
+    unit *= 1.0f / kQmax8;
+    if (unit > 0.0f) unit = fmaxf(unit, 1.2e-38f);
+    if (tid == 32 * kSoftWarps) unit_word = unit;
+    const float inv_unit = unit > 0.0f ? __fdiv_rn(1.0f, unit) : 0.0f;
+
     for (int j = 0; j < steps; ++j) {
       const uint32_t st = j & 1, ph = (j >> 1) & 1;
       if (j >= 2 && !mbar_wait_warp(k_empty + 8 * st, ph ^ 1, abort_flag, a.err)) break;
@@ -348,7 +304,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
         for (int k = 0; k < kStepTokens / 16; ++k)
           mma_f16_ta((part ? l_at : o_at) + D * i, s_at + 128 * i + kPart * k + 8 * part, v0 + ((k * 2048) >> 4), kIdescO, j + k > 0);
     };
-    ok = mbar_wait_warp(k_full, 0, abort_flag, a.err);
+    ok = mbar_wait_warp(q_full, 0, abort_flag, a.err) && mbar_wait_warp(k_full, 0, abort_flag, a.err);
     tc_fence_after();
     if (ok) {
       for (int i = 0; i < n_tiles; ++i) product_s(i, 0);
@@ -378,6 +334,52 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     }
     __syncwarp();
   } else if (warp < kSoftWarps) {
+    // ------------------------------------------------------------------ queries: a thread a row
+    int lo = 0, hi = 0x7fffffff, out_row = -1, out_head = 0;
+    float row_f = 0.0f;
+    {
+      constexpr int V = Vec<T>::N, PIECES = D / V;
+      const int tile = warp >> 2, r = tid & 127;
+      const int tok = t_first + tile * per_tile + r / group;
+      union Piece { uint4 u; T t[V]; } held[PIECES];
+#pragma unroll
+      for (int c = 0; c < PIECES; ++c) held[c].u = make_uint4(0, 0, 0, 0);
+      if (r < per_tile * group && tok < rows) {
+        out_row = tok;
+        out_head = hk * group + r % group;
+        const T* q = reinterpret_cast<const T*>(a.q) + (row0 + tok) * a.q_row + out_head * a.q_head;
+        seen_range(a, (int64_t)len - rows + tok, len, lo, hi);
+#pragma unroll
+        for (int c = 0; c < PIECES; ++c) held[c].u = __ldg(reinterpret_cast<const uint4*>(q) + c);
+      }
+      unsigned top = 0;
+#pragma unroll
+      for (int c = 0; c < PIECES; ++c)
+#pragma unroll
+        for (int j = 0; j < V; ++j) top = max(top, abs_bits(to_float<T>(held[c].t[j])));
+      const int shift = row_shift(top);
+      const float up = exp2_of(shift);
+      row_f = a.scale * exp2_of(-shift);
+      const uint32_t base = q_sm + tile * q_tile_bytes<D, WIDE>() + r * 128;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        uint32_t w[4], l[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int e = 8 * c + 2 * j;
+          const float x = to_float<T>(held[e / V].t[e % V]) * up, y = to_float<T>(held[(e + 1) / V].t[(e + 1) % V]) * up;
+          const __half2 h = __floats2half2_rn(x, y);
+          w[j] = h2_bits(h);
+          if (WIDE) l[j] = pack_h2(x - __low2float(h), y - __high2float(h));
+        }
+        const uint32_t to = base + (c >> 3) * HALF + (((c & 7) ^ (r & 7)) << 4);
+        st_shared_v4(to, w[0], w[1], w[2], w[3]);
+        if (WIDE) st_shared_v4(to + kTileRows * D * 2, l[0], l[1], l[2], l[3]);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+    }
     // ------------------------------------------------------------------ weights
     const int i = warp >> 2;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
@@ -512,7 +514,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : (sum == 0.0f ? 0.0f : sum);
       if (n > 0) inv *= unit_word;
       T* out = reinterpret_cast<T*>(a.out) + (row0 + out_row) * a.o_row + out_head * a.o_head;
-#pragma unroll 1
+#pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         uint32_t v[32];
         if (n > 0) {
