@@ -337,45 +337,60 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     // ------------------------------------------------------------------ queries: a thread a row
     int lo = 0, hi = 0x7fffffff, out_row = -1, out_head = 0;
     float row_f = 0.0f;
+    // Rows are read and written whole, LPR lanes each: a lane for each row would touch 32 rows with every access.
+    constexpr int V = Vec<T>::N, LPR = D / V, RPA = 32 / LPR;          // elements a lane, lanes a row, rows an access
+    const int my_chunk = lane % LPR;
     {
-      constexpr int V = Vec<T>::N, PIECES = D / V;
       const int tile = warp >> 2, r = tid & 127;
       const int tok = t_first + tile * per_tile + r / group;
-      union Piece { uint4 u; T t[V]; } held[PIECES];
-#pragma unroll
-      for (int c = 0; c < PIECES; ++c) held[c].u = make_uint4(0, 0, 0, 0);
+      const T* q = nullptr;
       if (r < per_tile * group && tok < rows) {
         out_row = tok;
         out_head = hk * group + r % group;
-        const T* q = reinterpret_cast<const T*>(a.q) + (row0 + tok) * a.q_row + out_head * a.q_head;
+        q = reinterpret_cast<const T*>(a.q) + (row0 + tok) * a.q_row + out_head * a.q_head;
         seen_range(a, (int64_t)len - rows + tok, len, lo, hi);
-#pragma unroll
-        for (int c = 0; c < PIECES; ++c) held[c].u = __ldg(reinterpret_cast<const uint4*>(q) + c);
       }
-      unsigned top = 0;
+      union Piece { uint4 u; T t[V]; } held[LPR];
 #pragma unroll
-      for (int c = 0; c < PIECES; ++c)
+      for (int c = 0; c < LPR; ++c) {
+        const T* from = reinterpret_cast<const T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(q), c * RPA + lane / LPR));
+        held[c].u = from ? __ldg(reinterpret_cast<const uint4*>(from) + my_chunk) : make_uint4(0, 0, 0, 0);
+      }
+      int shift = 0;
+#pragma unroll
+      for (int c = 0; c < LPR; ++c) {
+        unsigned top = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) top = max(top, abs_bits(to_float<T>(held[c].t[j])));
-      const int shift = row_shift(top);
-      const float up = exp2_of(shift);
-      row_f = a.scale * exp2_of(-shift);
-      const uint32_t base = q_sm + tile * q_tile_bytes<D, WIDE>() + r * 128;
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        uint32_t w[4], l[4];
+        for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const int row = c * RPA + lane / LPR, up_by = row_shift(top);
+        // the row's own thread needs it too
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int e = 8 * c + 2 * j;
-          const float x = to_float<T>(held[e / V].t[e % V]) * up, y = to_float<T>(held[(e + 1) / V].t[(e + 1) % V]) * up;
+        for (int k = 0; k < RPA; ++k) {
+          const int other = __shfl_sync(0xffffffffu, up_by, k * LPR);
+          if (lane == c * RPA + k) shift = other;
+        }
+        const float up = exp2_of(up_by);
+        uint32_t w[V / 2], l[V / 2];
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+          const float x = to_float<T>(held[c].t[2 * j]) * up, y = to_float<T>(held[c].t[2 * j + 1]) * up;
           const __half2 h = __floats2half2_rn(x, y);
           w[j] = h2_bits(h);
-          if (WIDE) l[j] = pack_h2(x - __low2float(h), y - __high2float(h));
+          l[j] = pack_h2(x - __low2float(h), y - __high2float(h));
         }
-        const uint32_t to = base + (c >> 3) * HALF + (((c & 7) ^ (r & 7)) << 4);
-        st_shared_v4(to, w[0], w[1], w[2], w[3]);
-        if (WIDE) st_shared_v4(to + kTileRows * D * 2, l[0], l[1], l[2], l[3]);
+        const int at8 = my_chunk * V / 8, r128 = 32 * (warp & 3) + row;       // 16 bytes of fp16
+        const uint32_t to = q_sm + tile * q_tile_bytes<D, WIDE>() + r128 * 128 + (at8 >> 3) * HALF + (((at8 & 7) ^ (r128 & 7)) << 4);
+        if constexpr (WIDE) {
+          const uint32_t half = (my_chunk & 1) * 8;
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + half), "r"(w[0]), "r"(w[1]) : "memory");
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + half + kTileRows * D * 2), "r"(l[0]), "r"(l[1]) : "memory");
+        } else {
+          st_shared_v4(to, w[0], w[1], w[2], w[3]);
+        }
       }
+      row_f = a.scale * exp2_of(-shift);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
@@ -513,7 +528,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       tc_fence_after();
       float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : (sum == 0.0f ? 0.0f : sum);
       if (n > 0) inv *= unit_word;
-      T* out = reinterpret_cast<T*>(a.out) + (row0 + out_row) * a.o_row + out_head * a.o_head;
+      // through the tile's queries, which nobody reads any more: a warp's 32 rows of D elements
+      const uint32_t stage = q_sm + i * q_tile_bytes<D, WIDE>() + (warp & 3) * 32 * D * (int)sizeof(T);
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         uint32_t v[32];
@@ -531,15 +547,25 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
 #pragma unroll
           for (int k = 0; k < 32; ++k) v[k] = 0u;
         }
-        if (out_row < 0) continue;
-        constexpr int V = Vec<T>::N;
 #pragma unroll
         for (int k = 0; k < 32; k += V) {
           union { uint4 u; T t[V]; } w;
 #pragma unroll
           for (int e = 0; e < V; ++e) w.t[e] = from_float<T>(sum == 0.0f ? 0.0f : __uint_as_float(v[k + e]) * inv);
-          *reinterpret_cast<uint4*>(out + 32 * c + k) = w.u;
+          const int chunk = (32 * c + k) / V;
+          st_shared_v4(stage + lane * D * (int)sizeof(T) + ((chunk ^ (lane & (LPR - 1))) << 4), w.u.x, w.u.y, w.u.z, w.u.w);
         }
+      }
+      __syncwarp();
+      T* out = out_row < 0 ? nullptr : reinterpret_cast<T*>(a.out) + (row0 + out_row) * a.o_row + out_head * a.o_head;
+#pragma unroll
+      for (int c = 0; c < LPR; ++c) {
+        const int row = c * RPA + lane / LPR;
+        T* to = reinterpret_cast<T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(out), row));
+        uint4 w;
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                     : "r"(stage + row * D * (int)sizeof(T) + ((my_chunk ^ (row & (LPR - 1))) << 4)));
+        if (to) reinterpret_cast<uint4*>(to)[my_chunk] = w;
       }
     }
   }
