@@ -430,52 +430,64 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
           if (t < from || t >= to || sc.key[2 * c + (k >> 4)] < 0.0f) v[k] = 0xff800000u;
         }
       };
-      // Weights of 32 tokens at a time, over scores that have been read: group g of 16 in columns kPart * g on.  The next 32 scores are on
-      // their way meanwhile.  The reference is a whole number, and moves only when a row has none yet or a sum of 16 weights no longer
-      // fits fp16: what has been written and summed up is then scaled by a power of two.  So a score is read once, and no
-      // maximum is taken of most.
+      // Weights of BLOCK x 32 tokens at a time (all of them; fp32, with twice as many to hold, 32), over scores that have been read: group
+      // g of 16 in columns kPart * g on.  The next 32 scores are on their way meanwhile.  The reference is a whole number, and moves only
+      // when a row has none yet or a sum of 16 weights no longer fits fp16: what has been written and summed up is then scaled by a
+      // power of two.  So no maximum is taken of most scores.
+      constexpr int BLOCK = WIDE ? 1 : 4;
       float part = 0.0f;             // of the step's unscaled exponentials
-      uint32_t v[2][32];
-      tmem_ld32_issue(s_row, v[0]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t (&x32)[32] = v[c & 1];
-        tmem_ld_wait();
-        if (c < 3) tmem_ld32_issue(s_row + 32 * (c + 1), v[(c + 1) & 1]);
-        if (masked) mask(x32, c);
-        uint32_t p[2][8], l[WIDE ? 2 : 1][WIDE ? 8 : 1];
-        float of16[2];
+      for (int b = 0; b < 4; b += BLOCK) {
+        uint32_t p[2 * BLOCK][8], l[WIDE ? 2 : 1][WIDE ? 8 : 1];
+        float block_part;
+        bool large;
         auto take = [&]() {
           const float shift = weight_bias<WIDE>() - (ref == -INFINITY ? 0.0f : ref);
+          block_part = 0.0f;
+          large = false;
+          uint32_t v[2][32];
+          tmem_ld32_issue(s_row + 32 * b, v[0]);
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const float f1 = f[2 * c + z], at1 = shift + log_share[2 * c + z];
-            const float2 fg = make_float2(f1, f1), at = make_float2(at1, at1);
-            float2 acc[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+          for (int c = b; c < b + BLOCK; ++c) {
+            uint32_t (&x32)[32] = v[(c - b) & 1];
+            tmem_ld_wait();
+            if (c + 1 < b + BLOCK) tmem_ld32_issue(s_row + 32 * (c + 1), v[(c + 1 - b) & 1]);
+            if (masked) mask(x32, c);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float2 x = __ffma2_rn(make_float2(__uint_as_float(x32[16 * z + 2 * k]), __uint_as_float(x32[16 * z + 2 * k + 1])), fg, at);
-              const float2 e = make_float2(ex2(x.x), ex2(x.y));
-              acc[k & 1] = __fadd2_rn(acc[k & 1], e);
-              const __half2 h = __floats2half2_rn(e.x, e.y);
-              p[z][k] = h2_bits(h);
-              if (WIDE) l[z][k] = pack_h2(e.x - __low2float(h), e.y - __high2float(h));
+            for (int z = 0; z < 2; ++z) {
+              const float f1 = f[2 * c + z], at1 = shift + log_share[2 * c + z];
+              const float2 fg = make_float2(f1, f1), at = make_float2(at1, at1);
+              float2 acc[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float2 x = __ffma2_rn(make_float2(__uint_as_float(x32[16 * z + 2 * k]), __uint_as_float(x32[16 * z + 2 * k + 1])), fg, at);
+                const float2 e = make_float2(ex2(x.x), ex2(x.y));
+                acc[k & 1] = __fadd2_rn(acc[k & 1], e);
+                const __half2 h = __floats2half2_rn(e.x, e.y);
+                p[2 * (c - b) + z][k] = h2_bits(h);
+                if constexpr (WIDE) l[z][k] = pack_h2(e.x - __low2float(h), e.y - __high2float(h));
+              }
+              acc[0] = __fadd2_rn(acc[0], acc[1]);
+              const float of16 = acc[0].x + acc[0].y;
+              large |= !(of16 <= 65504.0f);              // (a NaN counts; it stays one)
+              block_part = fmaf(of16, inv_share[2 * c + z], block_part);
             }
-            acc[0] = __fadd2_rn(acc[0], acc[1]);
-            of16[z] = acc[0].x + acc[0].y;
           }
         };
         take();
-        // (a NaN counts as too large; it stays one)
-        const bool large = !(of16[0] <= 65504.0f) || !(of16[1] <= 65504.0f);
         if (__any_sync(0xffffffffu, fresh || large)) {
           float most = -INFINITY;
+#pragma unroll 1
+          for (int g = 2 * b; g < 2 * (b + BLOCK); ++g) {
+            uint32_t x[16];
+            tmem_ld16(s_row + 16 * g, x);
+            tmem_ld_wait();
+            const float key = sc.key[g];
+            float m = -INFINITY;
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            float m = __uint_as_float(x32[16 * z]);
-#pragma unroll
-            for (int k = 1; k < 16; ++k) m = fmaxf(m, __uint_as_float(x32[16 * z + k]));
-            most = fmaxf(most, m * f[2 * c + z]);
+            for (int k = 0; k < 16; ++k)
+              if (!masked || (16 * g + k >= from && 16 * g + k < to && key >= 0.0f)) m = fmaxf(m, __uint_as_float(x[k]));
+            most = fmaxf(most, m * fmaxf(row_f * key, 1.2e-38f));
           }
           const float was = ref;
           if (fresh || large) ref = fmaxf(ref, ceilf(most));
@@ -486,7 +498,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
             part *= keep;
             const __half2 keep2 = __floats2half2_rn(keep, keep);
 #pragma unroll 1
-            for (int h = 0; h < (WIDE ? 4 * c : 2 * c); ++h) {
+            for (int h = 0; h < (int)kPart / 8 * 2 * b; ++h) {
               uint32_t w[8];
               tmem_ld8(s_row + 8 * h, w);
               tmem_ld_wait();
@@ -509,11 +521,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
           }
           take();
         }
+        part += block_part;
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          part = fmaf(of16[z], inv_share[2 * c + z], part);
-          tmem_st8(s_row + kPart * (2 * c + z), p[z]);
-          if constexpr (WIDE) tmem_st8(s_row + kPart * (2 * c + z) + 8, l[z]);
+        for (int g = 0; g < 2 * BLOCK; ++g) {
+          tmem_st8(s_row + kPart * (2 * b + g), p[g]);
+          if constexpr (WIDE) tmem_st8(s_row + kPart * (2 * b + g) + 8, l[g]);
         }
       }
       sum += part;
