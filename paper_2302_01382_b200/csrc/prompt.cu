@@ -496,14 +496,17 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
           if (__any_sync(0xffffffffu, keep != 1.0f)) {
             sum *= keep;
             part *= keep;
-            const __half2 keep2 = __floats2half2_rn(keep, keep);
+            if (b > 0) tmem_st_wait();       // loads are not ordered behind stores that have not been waited for
 #pragma unroll 1
             for (int h = 0; h < (int)kPart / 8 * 2 * b; ++h) {
               uint32_t w[8];
               tmem_ld8(s_row + 8 * h, w);
               tmem_ld_wait();
 #pragma unroll
-              for (int k = 0; k < 8; ++k) w[k] = h2_bits(__hmul2(*reinterpret_cast<const __half2*>(&w[k]), keep2));
+              for (int k = 0; k < 8; ++k) {      // (the factor itself may be too small for fp16)
+                const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+                w[k] = pack_h2(e.x * keep, e.y * keep);
+              }
               tmem_st8(s_row + 8 * h, w);
             }
             // the products so far have been completed in front of these scores
@@ -544,20 +547,16 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       const uint32_t stage = q_sm + i * q_tile_bytes<D, WIDE>() + (warp & 3) * 32 * D * (int)sizeof(T);
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
+        if (n == 0) break;               // nothing is seen (and the queries may still be on their way to shared memory)
         uint32_t v[32];
-        if (n > 0) {
-          tmem_ld32_issue(o_row + 32 * c, v);
+        tmem_ld32_issue(o_row + 32 * c, v);
+        tmem_ld_wait();
+        if constexpr (WIDE) {
+          uint32_t u[32];
+          tmem_ld32_issue(l_row + 32 * c, u);
           tmem_ld_wait();
-          if constexpr (WIDE) {
-            uint32_t u[32];
-            tmem_ld32_issue(l_row + 32 * c, u);
-            tmem_ld_wait();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + __uint_as_float(u[k]));
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 32; ++k) v[k] = 0u;
+          for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + __uint_as_float(u[k]));
         }
 #pragma unroll
         for (int k = 0; k < 32; k += V) {
@@ -577,7 +576,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
         uint4 w;
         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
                      : "r"(stage + row * D * (int)sizeof(T) + ((my_chunk ^ (row & (LPR - 1))) << 4)));
-        if (to) reinterpret_cast<uint4*>(to)[my_chunk] = w;
+        if (to) reinterpret_cast<uint4*>(to)[my_chunk] = n > 0 ? w : make_uint4(0, 0, 0, 0);
       }
     }
   }
@@ -604,10 +603,18 @@ int prompt_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
 
 }  // namespace
 
+// Whether a call goes this way or streams the cache, by the rows of the longest entry as far as known.  A block takes 256 rows through the
+// whole context, so there have to be blocks for a good part of the SMs; streaming cuts the context instead, and repeats the
+// conversion of the codes for every 32 rows.  us, this way / streaming, entries x new tokens behind a context, heads x group, dim:
+//   8 heads x 4, 128   8 x 8, 1000 35.0 / 35.5    8 x 16, 1000 35.8 / 39.5    8 x 64, 1000 43 / 70    32 x 8, 1000 67 / 60    32 x 16, 1000 65 / 85
+//                      64 x 8, 4000 219 / 193     64 x 16, 4000 206 / 253     1 x 64, 1000 43 / 37    1 x 64, 30000 481 / 170
+//                      1 x 512, 1000 50 / 113     1 x 512, 30000 503 / 1122
+//   12 heads x 1, 64   8 x 64, 1000 39 / 28       8 x 128, 1000 39 / 39       32 x 64, 300 75 / 35    1 x 384, 0 35 / 19    32 x 384, 0 (fp32) 99 / 177
 bool prompt_pays(Ctx* ctx, const AttnArgs& a, int dtype, int64_t rows) {
   const int group = a.q_heads / a.cache.heads;
   if (group > kTileRows || (a.cache.dim != 64 && a.cache.dim != 128) || (dtype == QCFG_FP32 && a.cache.dim != 64)) return false;
-  return rows * group >= 64 && (a.batch.rows * group + 255) / 256 * a.cache.heads >= sm_count(ctx) / 4;
+  const int64_t blocks = std::max<int64_t>(a.batch.n, (a.batch.rows * group + 255) / 256) * a.cache.heads;
+  return rows * group >= (a.cache.dim == 128 ? 64 : 192) && 3 * blocks >= sm_count(ctx);
 }
 
 int launch_prompt(Ctx* ctx, const AttnArgs& a, int dtype, cudaStream_t st) {

@@ -475,15 +475,39 @@ def test_attention_of_prompts(ctx, page, q_heads, heads, dim, dtype):
     check_attention(ctx, cache, co, [0], [300], q_heads, dtype, rng, window=1)
 
 
+MANY = [(16, 12, 12, 64, [torch.float32, torch.bfloat16, torch.float16]), (128, 16, 8, 64, DTYPES), (64, 32, 8, 128, DTYPES[1:]), (32, 56, 8, 128, DTYPES[1:]),
+        (16, 8, 8, 128, DTYPES[1:]), (64, 130, 5, 128, DTYPES[1:])]
+
+
+@pytest.mark.parametrize("page,q_heads,heads,dim,dtypes", MANY)
+def test_attention_of_many_rows(ctx, page, q_heads, heads, dim, dtypes):
+    """Enough rows for the kernel that takes 256 at a time: ragged entries, rows that see nothing, windows, contexts that end anywhere."""
+    group = q_heads // heads
+    lens = [530, 129, 5, 700, 0, 257, 1, 384, 40, 256]
+    rows = [400, 129, 9, 128, 3, 257, 1, 300, 0, 255]
+    for dtype in dtypes:
+        rng = np.random.default_rng(page + group)
+        pool, cache, po, co = make(ctx, 2600 // page + 30, page, len(lens), 704 // page + 1, heads, dim)
+        steps(ctx, pool, cache, po, co, list(range(len(lens))), lens, dtype, rng, spread=2.0)
+        order = [3, 0, -1, 1, 2, 4, 5, 6, 7, 8, 9]
+        counts = [rows[s] if s >= 0 else 2 for s in order]
+        for kw in ({}, {"behind": 5, "layout": "packed", "max_new": 400}, {"layout": "heads", "window": 100}, {"causal": False}, {"window": 3, "sm_scale": 1.0}):
+            before = ctx.launch_count()
+            check_attention(ctx, cache, co, order, counts, q_heads, dtype, rng, **kw)
+            # max_new unknown: the mean decides, 135 rows here
+            assert ctx.launch_count() - before == (1 if "max_new" in kw or 135 * group >= (192 if dim == 64 else 64) else 2)
+
+
 def test_attention_of_uneven_scales(ctx):
     """Pages whose maxima differ by ten orders of magnitude, values of zero pages, scores up to hundreds."""
     for dtype in DTYPES:
         rng = np.random.default_rng(7)
-        pool, cache, po, co = make(ctx, 40, 16, 2, 40, 2, 64)
+        pool, cache, po, co = make(ctx, 40, 16, 2, 40, 25, 64)
         for t in range(12):
             steps(ctx, pool, cache, po, co, [0], [16], torch.float32, rng, spread=0.0 if t % 5 == 4 else 10.0 ** (t - 8))
-        check_attention(ctx, cache, co, [0], [1], 4, dtype, rng, sm_scale=0.02)
-        check_attention(ctx, cache, co, [0], [150], 4, dtype, rng, sm_scale=0.02)
+        check_attention(ctx, cache, co, [0], [1], 50, dtype, rng, sm_scale=0.02)
+        check_attention(ctx, cache, co, [0], [20], 50, dtype, rng, sm_scale=0.02)
+        check_attention(ctx, cache, co, [0, 0], [150, 100], 50, dtype, rng, sm_scale=0.02, max_new=150)
 
 
 def test_attention_of_a_long_context(ctx):
@@ -530,11 +554,11 @@ def test_attention_of_nonfinite_queries_and_bad_pages(ctx):
     """A query with NaN spoils its own rows only; tokens on pages that do not exist are left out and reported."""
     import paper_2302_01382_b200 as q
     for dtype in DTYPES:
-        for rows in (1, 40):
+        for rows, heads in ((1, 2), (40, 2), (100, 26)):
             rng = np.random.default_rng(13)
-            pool, cache, po, co = make(ctx, 30, 16, 3, 8, 2, 64)
+            pool, cache, po, co = make(ctx, 30, 16, 3, 8, heads, 64)
             steps(ctx, pool, cache, po, co, [0, 1], [100, 50], torch.float32, rng)
-            x = dev(rng.standard_normal((2 * rows, 4, 64)).astype(np.float32), dtype)
+            x = dev(rng.standard_normal((2 * rows, 2 * heads, 64)).astype(np.float32), dtype)
             clean = cache.attention(x, ints([0, 1]), ints([0, rows, 2 * rows]))
             y = x.clone()
             y[0, 1, 3] = float("nan")
@@ -557,22 +581,23 @@ def test_garbage_behind_the_end_is_not_seen(ctx):
     """Codes behind the last token and the maxima of pages nobody holds do not matter, whatever they are."""
     for dtype in DTYPES:
         rng = np.random.default_rng(17)
-        pool, cache, po, co = make(ctx, 30, 64, 3, 8, 2, 128)
+        pool, cache, po, co = make(ctx, 30, 64, 3, 8, 26, 64)
         cache.k.fill_(-128)
         cache.v.fill_(-128)
         cache.k_absmax.fill_(float("nan"))
         cache.v_absmax.fill_(float("inf"))
         steps(ctx, pool, cache, po, co, [0, 1], [70, 3], torch.float32, rng)
-        check_attention(ctx, cache, co, [0, 1], [1, 1], 8, dtype, rng)
-        check_attention(ctx, cache, co, [0, 1], [70, 3], 8, dtype, rng, max_new=70)
-        check_attention(ctx, cache, co, [0, 1], [65, 2], 8, dtype, rng, causal=False)
+        check_attention(ctx, cache, co, [0, 1], [1, 1], 104, dtype, rng)
+        check_attention(ctx, cache, co, [0, 1], [70, 3], 104, dtype, rng, max_new=70)
+        check_attention(ctx, cache, co, [0, 1], [10, 2], 104, dtype, rng, causal=False)
+        check_attention(ctx, cache, co, [0, 1], [65, 2], 104, dtype, rng, causal=False, max_new=65)
 
 
 def test_repeats_give_the_same_bits(ctx):
     rng = np.random.default_rng(19)
     pool, cache, po, co = make(ctx, 400, 16, 8, 320, 2, 128)
     steps(ctx, pool, cache, po, co, list(range(4)), [4000, 17, 900, 1], torch.bfloat16, rng)
-    for rows in ([1, 1, 1, 1], [150, 3, 70, 1]):
+    for rows in ([1, 1, 1, 1], [5, 3, 7, 1], [3000, 17, 900, 1]):
         q = dev(rng.standard_normal((sum(rows), 16, 128)).astype(np.float32), torch.bfloat16)
         first = cache.attention(q, ints(range(4)), ints(starts_of(rows)))
         for _ in range(5):
