@@ -304,141 +304,257 @@ __global__ void __launch_bounds__(kCopyThreads) kv_copy_kernel(CacheView c, int 
   }
 }
 
-// New keys or values of one page and head.
-constexpr int kAppendThreads = 128;
-template <typename T>
-__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(PoolView p, CacheView c, BatchView b, const T* k, const T* v,
-                                                                   int64_t row_stride, int64_t head_stride, unsigned* err) {
-  pdl_entry();
-  constexpr int V = Vec<T>::N;
-  int64_t first;
-  const int i = entry_of_item(b, blockIdx.x, p.page, b.starts ? 2 : 0, first);
-  if (i < 0 || i >= b.n) return;
-  int64_t lo, hi;
-  entry_rows(b, i, lo, hi);
-  const int s = entry_seq(b, p, i, err);
-  if (s < 0 || hi == lo) return;
-  const int len = seq_len(p, s);
-  const int64_t old = len - (hi - lo);             // tokens before this call
-  if (old < 0) {
-    if (threadIdx.x == 0) atomicOr(err, ERR_PAGE);
-    return;
-  }
-  const int64_t j = old / p.page + (blockIdx.x - first);
-  if (j * p.page >= len) return;
-  int twice = 0;
-  for (int e = threadIdx.x; e < b.n; e += kAppendThreads) twice |= e != i && b.seqs[e] == s;
-  const int number = p.table[(int64_t)s * p.max_pages + j];
-  const bool valid = number >= 0 && number < p.n_pages && p.refs[number] == 1;
-  if (__syncthreads_or(twice || !valid)) {
-    if (threadIdx.x == 0) atomicOr(err, ERR_PAGE);
-    return;
-  }
-  const int h = blockIdx.y;
-  const T* x = blockIdx.z ? v : k;
-  int8_t* codes = (blockIdx.z ? c.v : c.k) + ((int64_t)number * c.heads + h) * p.page * c.dim;
-  float* absmax = (blockIdx.z ? c.v_absmax : c.k_absmax) + (int64_t)number * c.heads + h;
-  const int t0 = (int)(max(old, j * p.page) - j * p.page);           // new tokens of the page: [t0, t1)
-  const int t1 = (int)(min((int64_t)len, (j + 1) * p.page) - j * p.page);
-  x += (lo + j * p.page + t0 - old) * row_stride + h * head_stride;
-  const int per_row = c.dim / V, n_vec = (t1 - t0) * per_row;
-  unsigned top = 0, odd = 0;
-  for (int e = threadIdx.x; e < n_vec; e += kAppendThreads) {
-    const int t = e / per_row, d = (e - t * per_row) * V;
-    float f[V];
-    load_vec<T>(x + t * row_stride + d, f);
-#pragma unroll
-    for (int q = 0; q < V; ++q) {
-      const unsigned a = abs_bits(f[q]);
-      if (a < 0x7f800000u) top = a > top ? a : top; else odd = 1;
+// What a block of a ragged batch works on.  Entry i owns the items starts[i] / unit + 2 i, ...; a thread looks at an entry, so that
+// everything that has to be known of the block's own is fetched at once.
+struct Claim {
+  int64_t row0;
+  int entry, rows, nth, seq, len, twice;
+};
+// twice: whether the sequence is listed by another entry too (only where asked for).  Whole block; false: nothing to do.
+__device__ __forceinline__ bool claim_item(const PoolView& p, const BatchView& b, int64_t item, int unit, bool want_twice, Claim* c, unsigned* err) {
+  if (threadIdx.x == 0) { c->entry = -1; c->twice = 0; }
+  __syncthreads();
+  for (int i0 = 0; i0 < b.n; i0 += blockDim.x) {
+    const int i = i0 + threadIdx.x;
+    if (i >= b.n) break;
+    int64_t lo, hi;
+    entry_rows(b, i, lo, hi);
+    const int64_t first = b.starts ? (int64_t)b.starts[i] / unit + 2 * (int64_t)i : i;
+    const int64_t nth = item - first;
+    const int s = b.seqs[i], len = s >= 0 && s < p.max_seqs ? seq_len(p, s) : 0;
+    // the bound of a run of items: those of the next entry begin behind rows / unit + 2 of this one's
+    if (nth >= 0 && nth < (b.starts ? (hi - lo) / unit + 2 : 1) && hi > lo && atomicCAS(&c->entry, -1, i) == -1) {
+      c->row0 = lo;
+      c->rows = (int)(hi - lo);
+      c->nth = (int)nth;
+      c->seq = s;
+      c->len = len;
     }
   }
-  __shared__ unsigned tops[kAppendThreads / 32];
-  top = warp_max_u(top);
-  if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
-  const float held = t0 > 0 ? *absmax : 0.0f;
-  if (__syncthreads_or(odd) && threadIdx.x == 0) atomicOr(err, ERR_NONFINITE);
-#pragma unroll
-  for (int w = 0; w < kAppendThreads / 32; ++w) top = tops[w] > top ? tops[w] : top;
-  const float fresh = __uint_as_float(top), now = held > fresh ? held : fresh;
-  const float inv = inv_scale_of(now);
-  for (int e = threadIdx.x; e < n_vec; e += kAppendThreads) {
-    const int t = e / per_row, d = (e - t * per_row) * V;
-    float f[V];
-    load_vec<T>(x + t * row_stride + d, f);
-    union { uint32_t w[V / 4]; int8_t b[V]; } q;
-#pragma unroll
-    for (int g = 0; g < V; ++g) q.b[g] = (int8_t)(finite_bits(f[g]) ? code_of(f[g], inv) : 0);
-    uint32_t* to = reinterpret_cast<uint32_t*>(codes + (t0 + t) * c.dim + d);
-#pragma unroll
-    for (int g = 0; g < V / 4; ++g) to[g] = q.w[g];
+  __syncthreads();
+  if (c->entry < 0) return false;
+  if (c->seq >= p.max_seqs && threadIdx.x == 0) atomicOr(err, ERR_PAGE);
+  if (want_twice) {
+    for (int i = threadIdx.x; i < b.n; i += blockDim.x)
+      if (i != c->entry && b.seqs[i] == c->seq) c->twice = 1;
+    __syncthreads();
   }
-  if (t0 > 0 && now > held && held > 0.0f) {       // the earlier codes on the new grid
-    const float ratio = __fdiv_rn(held, now);
-    for (int e = threadIdx.x; e < t0 * c.dim / 4; e += kAppendThreads) {
-      char4* at = reinterpret_cast<char4*>(codes) + e;
-      const char4 q = *at;
-      *at = make_char4((signed char)__float2int_rn(q.x * ratio), (signed char)__float2int_rn(q.y * ratio),
-                       (signed char)__float2int_rn(q.z * ratio), (signed char)__float2int_rn(q.w * ratio));
-    }
-  }
-  if (threadIdx.x == 0) *absmax = now;
+  return true;
 }
 
-// Values of cached tokens, a warp for each row.
-constexpr int kReadWarps = 8;
-template <typename T>
-__global__ void __launch_bounds__(32 * kReadWarps) kv_read_kernel(PoolView p, CacheView c, BatchView b, const int32_t* first_tok, T* k,
-                                                                  T* v, unsigned* err) {
+// New keys and values of a run of pages: a block takes 8 / W heads, W warps a head (1, 2, 4 or 8: as many as it takes to keep a page of
+// a head in registers, kAppendHeld pieces of 16 bytes a lane, so that it is read once; what does not fit is read twice).  To find a
+// page takes five loads one behind the other, longer than to write it: a block writes both tensors and, of 16 tokens, two pages.
+constexpr int kAppendThreads = 256, kAppendHeld = 8;
+template <typename T, int W>
+__global__ void __launch_bounds__(kAppendThreads, 3) kv_append_kernel(PoolView p, CacheView c, BatchView b, const T* k, const T* v, int64_t row_stride,
+                                                                      int64_t head_stride, int run, unsigned* err) {
   pdl_entry();
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * kReadWarps + (threadIdx.x >> 5);
-  if (row >= b.rows) return;
-  int i = (int)row;
-  if (b.starts) {
-    int count = 0;
-    for (int e = lane; e < b.n; e += 32) count += b.starts[e] <= row;
-    i = __reduce_add_sync(0xffffffffu, count) - 1;
+  constexpr int V = Vec<T>::N, N = 32 * W;
+  __shared__ Claim own;
+  __shared__ unsigned tops[8];
+  if (!claim_item(p, b, blockIdx.x, run * p.page, true, &own, err)) return;
+  const int s = own.seq, len = own.len;
+  if (s < 0 || s >= p.max_seqs) return;
+  const int64_t old = (int64_t)len - own.rows;     // tokens before this call
+  if (old < 0 || own.twice) {
+    if (threadIdx.x == 0) atomicOr(err, ERR_PAGE);
+    return;
   }
-  if (i < 0 || i >= b.n) return;
-  int64_t lo, hi;
-  entry_rows(b, i, lo, hi);
-  if (row >= hi) return;
-  const int s = entry_seq(b, p, i, err);
-  int number = -1;
-  int64_t pos = 0;
-  if (s >= 0) {
-    pos = first_tok[i] + (row - lo);
-    if (pos >= 0 && pos < seq_len(p, s)) {
-      number = p.table[(int64_t)s * p.max_pages + pos / p.page];
-      if (number < 0 || number >= p.n_pages) {
-        if (lane == 0) atomicOr(err, ERR_PAGE);
-        number = -1;
+  const int warp = threadIdx.x >> 5, h = blockIdx.y * (8 / W) + warp / W, t = threadIdx.x & (N - 1);
+  const bool here = h < c.heads;                   // (W > 1: a block's warps meet)
+  if (W == 1 && !here) return;
+  const int per_row = c.dim / V;
+  // the own.nth run of pages, counted from the one the first new token lies in
+  const int64_t j_first = (old / (run * p.page) + own.nth) * run;
+  for (int64_t j = max(j_first, old / p.page); j < j_first + run && j * p.page < len; ++j) {
+    const int number = p.table[(int64_t)s * p.max_pages + j];
+    if (number < 0 || number >= p.n_pages || p.refs[number] != 1) {
+      if (threadIdx.x == 0) atomicOr(err, ERR_PAGE);
+      continue;
+    }
+    const int64_t block = (int64_t)number * c.heads + (here ? h : 0);
+    const int t0 = (int)(max(old, j * p.page) - j * p.page);           // new tokens of the page: [t0, t1)
+    const int t1 = (int)(min((int64_t)len, (j + 1) * p.page) - j * p.page);
+    const int n_vec = here ? (t1 - t0) * per_row : 0;
+    const int z_last = gridDim.z == 2 ? blockIdx.z : 1;
+#pragma unroll 1
+    for (int z = gridDim.z == 2 ? blockIdx.z : 0; z <= z_last; ++z) {
+      int8_t* codes = (z ? c.v : c.k) + block * p.page * c.dim;
+      float* absmax = (z ? c.v_absmax : c.k_absmax) + block;
+      const T* x = (z ? v : k) + (own.row0 + j * p.page + t0 - old) * row_stride + h * head_stride;
+      const float before = t0 > 0 && here ? *absmax : 0.0f;
+      union Piece { uint4 u; T t[V]; } held[kAppendHeld];
+      // piece t + i N of the page's new tokens, i ascending: a division once, then steps
+      const int row_step = N / per_row, col_step = N - row_step * per_row;
+      int row = t / per_row, col = t - row * per_row;
+      const int row_first = row, col_first = col;
+      auto next = [&]() {
+        const T* from = x + row * row_stride + col * V;
+        row += row_step;
+        col += col_step;
+        if (col >= per_row) { col -= per_row; ++row; }
+        return from;
+      };
+      unsigned top = 0;
+      auto see = [&](const Piece& f) {                 // a NaN or Inf orders above all others
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          const unsigned a = abs_bits(to_float<T>(f.t[q]));
+          top = a > top ? a : top;
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < kAppendHeld; ++i)
+        if (t + i * N < n_vec) held[i].u = __ldg(reinterpret_cast<const uint4*>(next()));
+#pragma unroll
+      for (int i = 0; i < kAppendHeld; ++i)
+        if (t + i * N < n_vec) see(held[i]);
+      Piece f;
+      const int row_held = row, col_held = col;          // of the first piece not held
+      for (int e = t + kAppendHeld * N; e < n_vec; e += N) {
+        f.u = __ldg(reinterpret_cast<const uint4*>(next()));
+        see(f);
       }
+      auto over_head = [&](unsigned m) {
+        m = __reduce_max_sync(0xffffffffu, m);
+        if (W > 1) {
+          __syncthreads();
+          if ((threadIdx.x & 31) == 0) tops[warp] = m;
+          __syncthreads();
+#pragma unroll
+          for (int w = 0; w < W; ++w) m = max(m, tops[warp / W * W + w]);
+        }
+        return m;
+      };
+      top = over_head(top);
+      const bool odd = top >= 0x7f800000u;
+      if (W > 1 ? __syncthreads_or(odd) : odd) {       // the largest of the others
+        if (odd && t == 0) atomicOr(err, ERR_NONFINITE);
+        unsigned other = 0;
+        row = row_first;
+        col = col_first;
+        for (int e = t; e < n_vec; e += N) {
+          f.u = __ldg(reinterpret_cast<const uint4*>(next()));
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            const unsigned a = abs_bits(to_float<T>(f.t[q]));
+            if (a < 0x7f800000u && a > other) other = a;
+          }
+        }
+        top = over_head(other);
+      }
+      if (!here) continue;
+      const float fresh = __uint_as_float(top), now = before > fresh ? before : fresh;
+      const float inv = inv_scale_of(now);
+      const bool plain = !odd && finite_bits(inv);
+      auto put = [&](int e, const Piece& f) {
+        union { uint32_t w[V / 4]; int8_t b[V]; } q;
+        if (plain) {
+#pragma unroll
+          for (int g = 0; g < V / 4; ++g) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {              // clamp, then round by a magic number: the low byte is the code
+              float y;
+              asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(y) : "f"(__fmul_rn(to_float<T>(f.t[4 * g + i]), inv)), "f"(kQmax8));
+              w[i] = __float_as_uint(__fadd_rn(y, 12582912.0f));
+            }
+            q.w[g] = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
+          }
+        } else {
+#pragma unroll
+          for (int g = 0; g < V; ++g) {
+            const float y = to_float<T>(f.t[g]);
+            q.b[g] = (int8_t)(finite_bits(y) ? code_of(y, inv) : 0);
+          }
+        }
+        uint32_t* to = reinterpret_cast<uint32_t*>(codes + t0 * c.dim + e * V);
+        if (V == 8) *reinterpret_cast<uint2*>(to) = make_uint2(q.w[0], q.w[V / 4 - 1]);
+        else to[0] = q.w[0];
+      };
+#pragma unroll
+      for (int i = 0; i < kAppendHeld; ++i)
+        if (t + i * N < n_vec) put(t + i * N, held[i]);
+      row = row_held;
+      col = col_held;
+      for (int e = t + kAppendHeld * N; e < n_vec; e += N) {
+        f.u = __ldg(reinterpret_cast<const uint4*>(next()));
+        put(e, f);
+      }
+      if (t0 > 0 && now > before && before > 0.0f) {   // the earlier codes on the new grid
+        const float ratio = __fdiv_rn(before, now);
+        for (int e = t; e < t0 * c.dim / 4; e += N) {
+          char4* to = reinterpret_cast<char4*>(codes) + e;
+          const char4 q = *to;
+          *to = make_char4((signed char)__float2int_rn(q.x * ratio), (signed char)__float2int_rn(q.y * ratio),
+                           (signed char)__float2int_rn(q.z * ratio), (signed char)__float2int_rn(q.w * ratio));
+        }
+      }
+      if (t == 0) *absmax = now;
     }
   }
-  const int per_head = c.dim / 4, n_vec = c.heads * per_head;
-  for (int e = lane; e < n_vec; e += 32) {
-    const int h = e / per_head, d = (e - h * per_head) * 4;
+}
+
+// Values of cached tokens: a block takes 4 tokens (of one page, as positions count), a warp a row of keys or of values, written whole.
+// Small blocks: what bounds a block is the four loads one behind the other that lead to its codes, so many of them have to be under way.
+constexpr int kReadTokens = 4, kReadThreads = 64 * kReadTokens;
+template <typename T>
+__global__ void __launch_bounds__(kReadThreads, 5) kv_read_kernel(PoolView p, CacheView c, BatchView b, const int32_t* first_tok, T* k, T* v, unsigned* err) {
+  pdl_entry();
+  __shared__ Claim own;
+  if (!claim_item(p, b, blockIdx.x, kReadTokens, false, &own, err)) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, z = warp & 1;
+  const int64_t from = first_tok[own.entry];
+  // positions of this block: the own.nth run of 4 from the one `from` lies in (floor, for negative ones too)
+  const int64_t run = (from >= 0 ? from / kReadTokens : -((-from + kReadTokens - 1) / kReadTokens)) + own.nth;
+  const int64_t pos = run * kReadTokens + (warp >> 1);
+  T* out = z ? v : k;
+  if (!out || pos < from || pos >= from + own.rows) return;
+  out += (own.row0 + pos - from) * c.heads * c.dim;
+  int number = -1;
+  if (own.seq >= 0 && own.seq < p.max_seqs && pos >= 0 && pos < own.len) {
+    number = p.table[(int64_t)own.seq * p.max_pages + pos / p.page];
+    if (number < 0 || number >= p.n_pages) {
+      if (lane == 0) atomicOr(err, ERR_PAGE);
+      number = -1;
+    }
+  }
+  const int quads = c.dim / 4, head_bytes = p.page * c.dim;
+  const int step_h = 32 / quads, step_d = 4 * (32 - step_h * quads);
+  const int64_t block = (int64_t)max(number, 0) * c.heads;
+  const int8_t* codes = (z ? c.v : c.k) + (block * p.page + (number < 0 ? 0 : pos % p.page)) * c.dim;
+  const float* absmax = (z ? c.v_absmax : c.k_absmax) + block;
+  // 32 heads at a time: lane i holds the scale of the i-th, element lane + 32 e of [heads][quads] is the lane's e-th
+  for (int h0 = 0; h0 < c.heads; h0 += 32) {
+    const int nh = min(32, c.heads - h0), n = nh * quads;
+    const float mine = number < 0 ? 0.0f : lane < nh ? scale_of(absmax[h0 + lane]) : 1.0f;
+    int h = lane / quads, d = 4 * (lane - h * quads);
+    T* to = out + h0 * c.dim + 4 * lane;
+    constexpr int kBatch = 8;
+    for (int e0 = 0; e0 < n; e0 += 32 * kBatch, to += 128 * kBatch) {
+      char4 q[kBatch];
+      float f[kBatch];
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      T* out = z ? v : k;
-      if (!out) continue;
-      union { T t[4]; uint4 w4; uint2 w2; } o;
-      char4 q = make_char4(0, 0, 0, 0);
-      float scale = 0.0f;
-      if (number >= 0) {
-        const int64_t at = (int64_t)number * c.heads + h;
-        q = *reinterpret_cast<const char4*>((z ? c.v : c.k) + (at * p.page + pos % p.page) * c.dim + d);
-        scale = scale_of((z ? c.v_absmax : c.k_absmax)[at]);
+      for (int i = 0; i < kBatch; ++i) {
+        q[i] = make_char4(0, 0, 0, 0);
+        if (number >= 0 && e0 + 32 * i + lane < n) q[i] = *reinterpret_cast<const char4*>(codes + (int64_t)(h0 + h) * head_bytes + d);
+        f[i] = __shfl_sync(0xffffffffu, mine, h & 31);
+        h += step_h;
+        d += step_d;
+        if (d >= c.dim) { d -= c.dim; ++h; }
       }
-      o.t[0] = from_float<T>(q.x * scale);
-      o.t[1] = from_float<T>(q.y * scale);
-      o.t[2] = from_float<T>(q.z * scale);
-      o.t[3] = from_float<T>(q.w * scale);
-      T* to = out + (row * c.heads + h) * c.dim + d;
-      if (sizeof(T) == 4) *reinterpret_cast<uint4*>(to) = o.w4;
-      else *reinterpret_cast<uint2*>(to) = o.w2;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (e0 + 32 * i + lane >= n) continue;
+        union { T t[4]; uint4 w4; uint2 w2; } o;
+        o.t[0] = from_float<T>(q[i].x * f[i]);
+        o.t[1] = from_float<T>(q[i].y * f[i]);
+        o.t[2] = from_float<T>(q[i].z * f[i]);
+        o.t[3] = from_float<T>(q[i].w * f[i]);
+        if (sizeof(T) == 4) *reinterpret_cast<uint4*>(to + 128 * i) = o.w4;
+        else *reinterpret_cast<uint2*>(to + 128 * i) = o.w2;
+      }
     }
   }
 }
@@ -490,9 +606,19 @@ int launch_kv_copy(Ctx* ctx, const PoolView& p, const CacheView& c, const int32_
 template <typename T>
 static void append_as(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const void* k, const void* v, int64_t row_stride,
                       int64_t head_stride, cudaStream_t st) {
-  const int64_t items = b.starts ? b.rows / p.page + 2 * (int64_t)b.n : b.n;
-  launch_pdl(kv_append_kernel<T>, dim3((unsigned)items, c.heads, 2), dim3(kAppendThreads), 0, st, p, c, b, (const T*)k, (const T*)v, row_stride,
-             head_stride, err_word(ctx));
+  // a row each: one page of an entry, few bytes of it, and both tensors at once; else runs of 32 tokens or a page
+  const bool single = b.rows <= b.n;
+  const int run = single || p.page > 16 ? 1 : 2;
+  const int64_t items = b.starts ? b.rows / (run * p.page) + 2 * (int64_t)b.n : b.n;
+  const int64_t pieces = (single ? 1 : p.page) * c.dim / Vec<T>::N, warps = (pieces + 32 * kAppendHeld - 1) / (32 * kAppendHeld);
+  const auto go = [&](auto kernel, int w) {
+    launch_pdl(kernel, dim3((unsigned)items, (c.heads * w + 7) / 8, single ? 2 : 1), dim3(kAppendThreads), 0, st, p, c, b, (const T*)k, (const T*)v, row_stride,
+               head_stride, run, err_word(ctx));
+  };
+  if (warps <= 1) go(kv_append_kernel<T, 1>, 1);
+  else if (warps <= 2) go(kv_append_kernel<T, 2>, 2);
+  else if (warps <= 4) go(kv_append_kernel<T, 4>, 4);
+  else go(kv_append_kernel<T, 8>, 8);
 }
 int launch_kv_append(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const void* k, const void* v, int dtype,
                      int64_t row_stride, int64_t head_stride, cudaStream_t st) {
@@ -505,7 +631,7 @@ int launch_kv_append(Ctx* ctx, const PoolView& p, const CacheView& c, const Batc
 }
 template <typename T>
 static void read_as(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const int32_t* first, void* k, void* v, cudaStream_t st) {
-  launch_pdl(kv_read_kernel<T>, dim3((unsigned)((b.rows + kReadWarps - 1) / kReadWarps)), dim3(32 * kReadWarps), 0, st, p, c, b, first, (T*)k, (T*)v,
+  launch_pdl(kv_read_kernel<T>, dim3((unsigned)(b.starts ? b.rows / kReadTokens + 2 * (int64_t)b.n : b.n)), dim3(kReadThreads), 0, st, p, c, b, first, (T*)k, (T*)v,
              err_word(ctx));
 }
 int launch_kv_read(Ctx* ctx, const PoolView& p, const CacheView& c, const BatchView& b, const int32_t* first, void* k, void* v, int dtype,
