@@ -377,6 +377,17 @@ int qcfg_model_create(qcfg_ctx* ctx, const qcfg_layer* layers, int32_t n_layers,
                       qcfg_model** out);
 int qcfg_model_destroy(qcfg_model* model);
 
+/* Puts an attention in front of a linear layer: its input is no longer its source's output but the
+ * attention of it (the queries, q_heads heads of k_in / q_heads) over the outputs of k_layer and
+ * v_layer (kv_heads heads each, earlier layers with as many rows).  Rows come in runs of seq_len tokens, each run a sequence
+ * of its own; the last may be shorter.  Keys and values pass through a cache at 8 bits with pages
+ * of page_tokens (qcfg_kv_append) and are read by qcfg_kv_attention with sm_scale, causal and window, as
+ * when the model serves: a configuration is judged on what it will be served with.  Every forward of the
+ * model includes it, the calibration's too.  Once for a layer (QCFG_ESTATE); the model has to be calibrated
+ * again.  The scale adjustment does not cover models with attention (QCFG_ESHAPE).                */
+int qcfg_model_set_attention(qcfg_ctx* ctx, qcfg_model* model, int32_t layer, int32_t k_layer, int32_t v_layer, int32_t q_heads,
+                             int32_t kv_heads, int32_t seq_len, int32_t page_tokens, float sm_scale, int causal, int32_t window);
+
 /* Max calibration of every activation tensor (Section 3.1): a forward of x_dev ([m x k] fp32,
  * or NHWC images with m = batch) with every layer at 16 bit -- the float model the searches
  * start from -- recording max|input| of every layer.  Synchronises the stream and keeps the

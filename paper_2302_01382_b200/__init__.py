@@ -29,7 +29,7 @@ EXPORTS = ["qcfg_create", "qcfg_destroy", "qcfg_sync_status", "qcfg_selftest_wai
            "qcfg_set_fusion", "qcfg_set_pair_tiles", "qcfg_set_grouping", "qcfg_set_prefix_reuse", "qcfg_set_implicit_conv", "qcfg_set_gemm_chains", "qcfg_profile_enable", "qcfg_profile_read", "qcfg_calibrate", "qcfg_scales_from_absmax", "qcfg_quantize",
            "qcfg_quant_error_sweep", "qcfg_quant_error_sweep_static", "qcfg_gemm_i8", "qcfg_gemm_i8_requant", "qcfg_gemm_bf16",
            "qcfg_quantize_tokens", "qcfg_gemm_i8_token", "qcfg_linear_i8_work", "qcfg_linear_i8", "qcfg_kv_extend", "qcfg_kv_free", "qcfg_kv_fork",
-           "qcfg_kv_compact", "qcfg_kv_copy_pages", "qcfg_kv_append", "qcfg_kv_read", "qcfg_kv_attention_work", "qcfg_kv_attention", "qcfg_model_create",
+           "qcfg_kv_compact", "qcfg_kv_copy_pages", "qcfg_kv_append", "qcfg_kv_read", "qcfg_kv_attention_work", "qcfg_kv_attention", "qcfg_model_create", "qcfg_model_set_attention",
            "qcfg_model_destroy", "qcfg_calibrate_model", "qcfg_model_act_absmax",
            "qcfg_model_weight_absmax", "qcfg_eval_config", "qcfg_latency_table", "qcfg_config_cost", "qcfg_noise_sensitivity", "qcfg_search", "qcfg_adjust_scales", "qcfg_scale_gradients", "qcfg_model_scales",
            "qcfg_model_reset_scales", "qcfg_debug_dump", "qcfg_debug_launch_forms"]
@@ -110,6 +110,7 @@ def load_library() -> C.CDLL:
         "qcfg_kv_read": [vp, pool, cache, batch, vp, vp, vp, ci, vp],
         "qcfg_kv_attention": [vp, pool, cache, batch, vp, i64, i64, i32, vp, i64, i64, ci, i32, i32, f32, ci, i32, vp, i64, vp],
         "qcfg_model_create": [vp, C.POINTER(LayerStruct), i32, C.POINTER(vp)],
+        "qcfg_model_set_attention": [vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, ci, i32],
         "qcfg_model_destroy": [vp],
         "qcfg_calibrate_model": [vp, vp, vp, i64, vp],
         "qcfg_model_act_absmax": [vp, C.POINTER(f32)],
@@ -597,6 +598,15 @@ class Model:
             self.close()
         except Exception:
             pass
+
+    def set_attention(self, layer: int, k_layer: int, v_layer: int, q_heads: int, kv_heads: int, seq_len: int, page_tokens: int = 64,
+                      sm_scale: Optional[float] = None, causal: bool = True, window: int = 0):
+        """Layer `layer` reads the attention of its source's rows over k_layer's and v_layer's, keys and values held at 8 bits.
+        sm_scale None: 1 / sqrt(head_dim)."""
+        if sm_scale is None:
+            sm_scale = (q_heads / max(self.layers[layer].k_in, 1)) ** 0.5 if 0 <= layer < len(self.layers) and q_heads > 0 else 1.0
+        self.ctx._check(self.ctx.lib.qcfg_model_set_attention(self.ctx.h, self.h, layer, k_layer, v_layer, q_heads, kv_heads, seq_len,
+                                                              page_tokens, sm_scale, int(causal), window))
 
     def calibrate_model(self, x: torch.Tensor, m: int, stream=None):
         self.ctx._check(self.ctx.lib.qcfg_calibrate_model(self.ctx.h, self.h, _ptr(x), m, _stream(stream)))

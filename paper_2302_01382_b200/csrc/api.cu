@@ -208,8 +208,18 @@ struct WeightCodes {
   bool adjusted = false;  // the scales no longer come from the calibrated maxima (scale adjustment)
 };
 
+// A layer whose input is the attention of its source's rows over the outputs of two other layers.
+struct AttnInput {
+  bool on = false;
+  int k = -1, v = -1;              // the layers whose outputs are the keys and the values
+  int32_t q_heads = 0, kv_heads = 0, dim = 0, seq_len = 0, page = 0, causal = 0, window = 0;
+  float scale = 0.0f;
+  bool reads(int l) const { return on && (l == k || l == v); }
+};
+
 struct LayerState {
   qcfg_layer d;
+  AttnInput attn;
   int64_t ldk = 0;                 // padded k_in of the code matrices
   DevBuf w_absmax;                 // fp32 [n_out]
   WeightCodes wc[17];              // by bit width
@@ -226,8 +236,8 @@ struct LayerState {
   int64_t rows = 0;
   DevBuf ybuf;                     // internal fp32 output [rows x n_out]
   DevBuf abuf;                     // GEMM input codes [rows x ldk] (sized for bf16)
-  DevBuf prebuf;                   // pooled fp32 input (convolution table only)
-  const float* pre_ptr = nullptr;  // pooled input actually used (may alias another layer's prebuf)
+  DevBuf prebuf;                   // fp32 input after pooling or attention
+  const float* pre_ptr = nullptr;  // such an input actually used (a pooled one may alias another layer's prebuf)
   const void* a_ptr = nullptr;     // codes actually used (may alias another layer's abuf)
   const float* y_ptr = nullptr;    // where this layer's fp32 output went (nullptr: not materialised)
   bool a_ready = false;
@@ -248,6 +258,10 @@ struct Model {
   DevBuf search_ref, search_out, search_partial;   // buffers of the search drivers
   DevBuf noise_codes;                              // perturbed bf16 weights of one layer
   DevBuf adj_gs, adj_gt, adj_qxt, adj_qwt, adj_dx, adj_dw, adj_grads, adj_coef;   // scale adjustment temporaries
+  DevBuf attn_pool, attn_cache, attn_copy;         // the cache of attention inputs, laid out for attn_rows tokens
+  int64_t attn_rows = -1;
+  int32_t attn_len = 0, attn_page = 0;
+  bool has_attn = false;
   int64_t last_m = 0;
   // what the layers' buffers hold after the last evaluation (for prefix reuse)
   bool reuse_valid = false;
@@ -294,6 +308,9 @@ bool same_input(const qcfg_layer& a, const qcfg_layer& b) {
          a.stride == b.stride && a.pad == b.pad && a.pool_before == b.pool_before && a.in_h == b.in_h &&
          a.in_w == b.in_w && a.in_c == b.in_c && (!image || (a.src_h == b.src_h && a.src_w == b.src_w));
 }
+
+// Two layers with the same GEMM operand.  The attention in front of a layer makes its operand its own.
+bool same_operand(const LayerState& a, const LayerState& b) { return !a.attn.on && !b.attn.on && same_input(a.d, b.d); }
 
 // Weight codes and per-row scales for (layer, bits); computed once and kept.
 int ensure_weight_codes(Ctx* ctx, LayerState& S, int bits, cudaStream_t st) {
@@ -354,6 +371,64 @@ void reset_adjusted_scales(Model* M) {
   M->reuse_valid = false;
 }
 
+// The input of a layer with attention in front: keys and values go through a cache at 8 bits, every run of seq_len rows a
+// sequence of its own, and the queries read it, as they do when the model serves.  The cache lives from here to the
+// attention behind it only, so all layers use the same memory.
+int attention_input(Ctx* ctx, Model* M, int l, cudaStream_t st) {
+  LayerState& S = M->L[l];
+  const AttnInput& t = S.attn;
+  const int64_t rows = S.rows, len = std::min<int64_t>(t.seq_len, rows), n = (rows + len - 1) / len, per = (len + t.page - 1) / t.page, pages = n * per;
+  if (rows > 0x7fffffff - 4096 || pages > 0x7fffffff || n > (1 << 20)) return set_error(ctx, QCFG_ESHAPE, "layer %d: %lld sequences are too many", l, (long long)n);
+  const LayerState* in[3] = {&M->L[S.d.src], &M->L[t.k], &M->L[t.v]};
+  int64_t odd = 0;                                    // elements of outputs whose place the kernels' 16-byte loads cannot take
+  for (const LayerState* p : in) {
+    if (!p->y_ptr) return set_error(ctx, QCFG_ESTATE, "layer %d: an output its attention reads is not materialised", l);
+    if (p->rows != rows) return set_error(ctx, QCFG_ESHAPE, "layer %d: its queries, keys and values have different numbers of rows", l);
+    if ((uintptr_t)p->y_ptr % 16) odd += rows * p->d.n_out;
+  }
+  const auto up = [](int64_t bytes) { return (bytes + 255) & ~(int64_t)255; };
+  // pool: table, lengths, counts of holders, sequences, starts
+  const int64_t at_len = up(pages * 4), at_refs = at_len + up(n * 4), at_seqs = at_refs + up(pages * 4), at_starts = at_seqs + up(n * 4);
+  const void* pool_before = M->attn_pool.p;
+  int rc = M->attn_pool.ensure(ctx, (size_t)(at_starts + up((n + 1) * 4)));
+  if (rc) return rc;
+  char* pb = (char*)M->attn_pool.p;
+  const PoolView pool{(int32_t*)pb, (int32_t*)(pb + at_len), (int32_t*)(pb + at_refs), (int32_t)pages, t.page, (int32_t)n, (int32_t)per};
+  const BatchView batch{(int32_t*)(pb + at_seqs), (int32_t*)(pb + at_starts), (int32_t)n, rows};
+  if (pb != pool_before || M->attn_rows != rows || M->attn_len != t.seq_len || M->attn_page != t.page) {
+    M->attn_rows = -1;
+    rc = launch_kv_layout(ctx, pool, (int32_t*)(pb + at_seqs), (int32_t*)(pb + at_starts), (int)len, rows, st);
+    if (rc) return rc;
+    M->attn_rows = rows; M->attn_len = t.seq_len; M->attn_page = t.page;
+  }
+  const int64_t codes = up(pages * t.page * t.kv_heads * t.dim), maxima = up(pages * t.kv_heads * 4);
+  CacheView cache{nullptr, nullptr, nullptr, nullptr, t.kv_heads, t.dim};
+  const int64_t work = kv_attention_work(ctx, cache, (int)len);
+  rc = M->attn_cache.ensure(ctx, (size_t)(2 * (codes + maxima) + work));
+  if (!rc && odd) rc = M->attn_copy.ensure(ctx, (size_t)odd * 4);
+  if (!rc) rc = S.prebuf.ensure(ctx, (size_t)(rows * S.d.k_in) * 4);
+  if (rc) return rc;
+  char* cb = (char*)M->attn_cache.p;
+  cache.k = (int8_t*)cb; cache.v = (int8_t*)(cb + codes);
+  cache.k_absmax = (float*)(cb + 2 * codes); cache.v_absmax = (float*)(cb + 2 * codes + maxima);
+  const float* y[3];
+  float* copy = (float*)M->attn_copy.p;
+  for (int i = 0; i < 3; ++i) {
+    y[i] = in[i]->y_ptr;
+    if ((uintptr_t)y[i] % 16 == 0) continue;
+    rc = check_cuda(ctx, cudaMemcpyAsync(copy, y[i], (size_t)(rows * in[i]->d.n_out) * 4, cudaMemcpyDeviceToDevice, st), "attention input copy");
+    if (rc) return rc;
+    y[i] = copy;
+    copy += rows * in[i]->d.n_out;                    // heads of a multiple of 16 elements: stays aligned
+  }
+  rc = launch_kv_append(ctx, pool, cache, batch, y[1], y[2], QCFG_FP32, (int64_t)t.kv_heads * t.dim, t.dim, st);
+  if (!rc)
+    rc = launch_kv_attention(ctx, pool, cache, batch, y[0], (int64_t)t.q_heads * t.dim, t.dim, t.q_heads, S.prebuf.p, (int64_t)t.q_heads * t.dim,
+                             t.dim, QCFG_FP32, (int)len, (int)len, t.scale, t.causal, t.window, cb + 2 * (codes + maxima), st);
+  if (!rc) S.pre_ptr = (const float*)S.prebuf.p;
+  return rc;
+}
+
 // One forward pass.  calibrate = true: every layer at 16 bit, record max|input| per layer.
 int forward(Ctx* ctx, Model* M, const uint8_t* bits, const float* x_dev, int64_t x_ld, int64_t m,
             float* const* y_dev, bool calibrate, cudaStream_t st, cudaEvent_t* layer_ev = nullptr) {
@@ -380,27 +455,41 @@ int forward(Ctx* ctx, Model* M, const uint8_t* bits, const float* x_dev, int64_t
       const qcfg_layer& d = M->L[l].d;
       changed[l] = M->L[l].bits != bits[l];
       dirty[l] = changed[l] || (y_dev && y_dev[l]) || (d.src >= 0 && dirty[d.src]) ||
-                 (d.residual_from >= 0 && dirty[d.residual_from]) || (!M->reuse_force.empty() && M->reuse_force[l]);
+                 (d.residual_from >= 0 && dirty[d.residual_from]) || (!M->reuse_force.empty() && M->reuse_force[l]) ||
+                 (M->L[l].attn.on && (dirty[M->L[l].attn.k] || dirty[M->L[l].attn.v]));
     }
-    for (int l = n - 1; l >= 0; --l) {
-      if (!dirty[l]) continue;
-      LayerState& S = M->L[l];
-      const qcfg_layer& d = S.d;
-      if (d.residual_from >= 0 && !dirty[d.residual_from]) {
-        LayerState& R = M->L[d.residual_from];
-        if (!(R.y_ptr && R.y_internal)) dirty[d.residual_from] = 1;
+    // One way back settles what has to run again besides.  Where a layer turns out to be needed behind the turn of an
+    // attention that reads it, the attention needs its other inputs too: another way back.
+    std::vector<char> before;
+    do {
+      before = dirty;
+      for (int l = n - 1; l >= 0; --l) {
+        if (!dirty[l]) continue;
+        LayerState& S = M->L[l];
+        const qcfg_layer& d = S.d;
+        if (d.residual_from >= 0 && !dirty[d.residual_from]) {
+          LayerState& R = M->L[d.residual_from];
+          if (!(R.y_ptr && R.y_internal)) dirty[d.residual_from] = 1;
+        }
+        const bool codes_kept = !changed[l] && S.a_ready && S.a_ptr && S.a_ptr == S.abuf.p;
+        if (S.attn.on && (dirty[d.src] || dirty[S.attn.k] || dirty[S.attn.v] || !(codes_kept || S.pre_ptr)))
+          for (int p : {(int)d.src, S.attn.k, S.attn.v})
+            if (!(M->L[p].y_ptr && M->L[p].y_internal)) dirty[p] = 1;
+        if (d.src < 0 || dirty[d.src]) continue;
+        LayerState& P = M->L[d.src];
+        // a pooled reader goes on from its pooled input, which is there as long as its source is not run again (the stem of
+        // a convolutional table writes nothing else)
+        if (!codes_kept && !S.pre_ptr && !(P.y_ptr && P.y_internal)) dirty[d.src] = 1;
       }
-      if (d.src < 0 || dirty[d.src]) continue;
-      LayerState& P = M->L[d.src];
-      const bool codes_kept = !changed[l] && S.a_ready && S.a_ptr && S.a_ptr == S.abuf.p;
-      // a pooled reader goes on from its pooled input, which is there as long as its source is not run again (the stem of
-      // a convolutional table writes nothing else)
-      if (!codes_kept && !S.pre_ptr && !(P.y_ptr && P.y_internal)) dirty[d.src] = 1;
-    }
+    } while (M->has_attn && dirty != before);
   }
+  auto source_runs = [&](int l) {
+    const LayerState& S = M->L[l];
+    return (S.d.src >= 0 && dirty[S.d.src]) || (S.attn.on && (dirty[S.attn.k] || dirty[S.attn.v]));
+  };
   auto codes_kept = [&](int l) {                     // a recomputed layer whose operand is still in its own buffer
     const LayerState& S = M->L[l];
-    return reuse && S.bits == bits[l] && S.a_ready && S.a_ptr && S.a_ptr == S.abuf.p && (S.d.src < 0 || !dirty[S.d.src]);
+    return reuse && S.bits == bits[l] && S.a_ready && S.a_ptr && S.a_ptr == S.abuf.p && !source_runs(l);
   };
   // A skipped layer may read its codes out of the buffer of a layer that is about to put others there (layers on one
   // input, of which one changes its width).  It takes that buffer over, with the codes in it, so that they stay what the
@@ -427,7 +516,7 @@ int forward(Ctx* ctx, Model* M, const uint8_t* bits, const float* x_dev, int64_t
     S.implicit = ctx->implicit && !calibrate && implicit_capable(S.d);
     if (!codes_kept(l)) { S.a_ready = false; S.a_ptr = nullptr; }
     S.y_ptr = nullptr; S.y_internal = false;
-    if (!reuse || S.d.src < 0 || dirty[S.d.src]) S.pre_ptr = nullptr;
+    if (!reuse || S.d.src < 0 || source_runs(l)) S.pre_ptr = nullptr;
     S.bits = calibrate ? 16 : bits[l];
   }
   M->reuse_valid = false;                            // until this evaluation has been enqueued completely
@@ -455,7 +544,7 @@ int forward(Ctx* ctx, Model* M, const uint8_t* bits, const float* x_dev, int64_t
     const int b = S.bits;
     if (!dirty[l]) continue;
     for (int pl : pending_layers)
-      if (d.src == pl || d.residual_from == pl) {
+      if (d.src == pl || d.residual_from == pl || S.attn.reads(pl)) {
         // With chained launches the order of independent GEMMs is a free choice, and the best
         // one keeps a GEMM away from the one it reads: only the layers this one reads go out
         // now, with half of the others behind them as a buffer; the rest wait and are launched
@@ -464,10 +553,10 @@ int forward(Ctx* ctx, Model* M, const uint8_t* bits, const float* x_dev, int64_t
           std::vector<GemmArgs> now, later;
           std::vector<int> now_l, later_l;
           for (size_t i = 0; i < pending.size(); ++i)
-            if (d.src == pending_layers[i] || d.residual_from == pending_layers[i]) { now.push_back(pending[i]); now_l.push_back(pending_layers[i]); }
+            if (d.src == pending_layers[i] || d.residual_from == pending_layers[i] || S.attn.reads(pending_layers[i])) { now.push_back(pending[i]); now_l.push_back(pending_layers[i]); }
           size_t others = pending.size() - now.size(), taken = 0;
           for (size_t i = 0; i < pending.size(); ++i) {
-            if (d.src == pending_layers[i] || d.residual_from == pending_layers[i]) continue;
+            if (d.src == pending_layers[i] || d.residual_from == pending_layers[i] || S.attn.reads(pending_layers[i])) continue;
             if (taken < (others + 1) / 2) { now.push_back(pending[i]); now_l.push_back(pending_layers[i]); ++taken; }
             else { later.push_back(pending[i]); later_l.push_back(pending_layers[i]); }
           }
@@ -526,6 +615,10 @@ int forward(Ctx* ctx, Model* M, const uint8_t* bits, const float* x_dev, int64_t
           S.pre_ptr = (const float*)S.prebuf.p;
         }
         sp = S.pre_ptr; srows = prows;
+      }
+      if (S.attn.on) {
+        if (!S.pre_ptr) { rc = attention_input(ctx, M, l, st); if (rc) return rc; }
+        sp = S.pre_ptr;
       }
       if (!sp) return set_error(ctx, QCFG_ESTATE, "layer %d: producer %d output not materialised", l, d.src);
       const bool direct = d.kh == 0 || (d.kh == 1 && d.kw == 1 && d.stride == 1 && d.pad == 0);
@@ -611,7 +704,7 @@ int forward(Ctx* ctx, Model* M, const uint8_t* bits, const float* x_dev, int64_t
       int share = -1;
       for (int j = 0; j < l && share < 0; ++j) {
         LayerState& T = M->L[j];
-        if (same_input(T.d, d) && T.bits == b && T.a_ptr && (b == 16 || act_inv(T, b) == act_inv(S, b)) &&
+        if (same_operand(T, S) && T.bits == b && T.a_ptr && (b == 16 || act_inv(T, b) == act_inv(S, b)) &&
             (dirty[j] || T.a_ptr == T.abuf.p))       // a skipped layer's codes are trusted only in its own buffer
           share = j;
       }
@@ -640,7 +733,7 @@ int forward(Ctx* ctx, Model* M, const uint8_t* bits, const float* x_dev, int64_t
           grids[count++] = CodeSlot{S.abuf.p, S.ldk, inv, b == 16 ? 0.0f : qmax_of(b), b == 16 ? 2 : 1, b};
           for (int j = l + 1; j < n && count < kMaxSlots; ++j) {
             LayerState& T = M->L[j];
-            if (!dirty[j] || T.a_ready || T.rows != S.rows || !same_input(T.d, d)) continue;
+            if (!dirty[j] || T.a_ready || T.rows != S.rows || !same_operand(T, S)) continue;
             float tsc = 1.0f, tinv = 1.0f;
             if (T.bits != 16) act_scales(T, T.bits, &tsc, &tinv);
             bool known = false;
@@ -692,7 +785,7 @@ int forward(Ctx* ctx, Model* M, const uint8_t* bits, const float* x_dev, int64_t
       // a consumer whose operand is this whole output: a plain row read, or a convolution the GEMM gathers for
       const bool c_implicit = ctx->implicit && !calibrate && implicit_capable(C.d) && C.d.pool_before == QCFG_POOL_NONE;
       // (in the calibration forward the epilogue also takes the range of what the consumer reads)
-      const bool fusable = ctx->fuse && C.d.src_col0 == 0 &&
+      const bool fusable = ctx->fuse && !C.attn.on && C.d.src_col0 == 0 &&
                            ((reads_rows_directly(C.d) && C.d.k_in == S.d.n_out) || (!calibrate && c_implicit && C.d.in_c == S.d.n_out));
       if (!fusable) { all_fused = false; continue; }
       const int64_t c_ld = c_implicit ? C.d.in_c : C.ldk;
@@ -1336,6 +1429,43 @@ int qcfg_model_create(qcfg_ctx* ctx, const qcfg_layer* layers, int32_t n_layers,
   return QCFG_OK;
 }
 
+int qcfg_model_set_attention(qcfg_ctx* ctx, qcfg_model* model, int32_t layer, int32_t k_layer, int32_t v_layer, int32_t q_heads, int32_t kv_heads,
+                             int32_t seq_len, int32_t page_tokens, float sm_scale, int causal, int32_t window) {
+  if (!ctx || !model) return QCFG_EINVAL;
+  Ctx* c = &ctx->c;
+  Model* M = &model->m;
+  const int n = (int)M->L.size();
+  if (layer < 0 || layer >= n || k_layer < 0 || k_layer >= layer || v_layer < 0 || v_layer >= layer)
+    return set_error(c, QCFG_EINVAL, "set_attention: keys and values must come from earlier layers");
+  LayerState& S = M->L[layer];
+  const qcfg_layer& d = S.d;
+  if (S.attn.on) return set_error(c, QCFG_ESTATE, "set_attention: layer %d has an attention already", layer);
+  if (d.kh > 0 || d.pool_before != QCFG_POOL_NONE || d.src < 0 || d.src_col0 != 0 || M->L[d.src].d.n_out != d.k_in)
+    return set_error(c, QCFG_ESHAPE, "set_attention: layer %d must be linear and read the whole output of another one", layer);
+  if (q_heads < 1 || q_heads > 65535 || kv_heads < 1 || kv_heads > 4096 || q_heads % kv_heads || d.k_in % q_heads)
+    return set_error(c, QCFG_ESHAPE, "set_attention: the heads do not divide layer %d's input", layer);
+  const int64_t dim = d.k_in / q_heads;
+  if (dim < 16 || dim > 256 || dim % 16) return set_error(c, QCFG_ESHAPE, "set_attention: head_dim must be a multiple of 16 up to 256");
+  if (M->L[k_layer].d.n_out != kv_heads * dim || M->L[v_layer].d.n_out != kv_heads * dim)
+    return set_error(c, QCFG_ESHAPE, "set_attention: keys and values must be kv_heads x %lld wide", (long long)dim);
+  if (page_tokens != 16 && page_tokens != 32 && page_tokens != 64 && page_tokens != 128)
+    return set_error(c, QCFG_ESHAPE, "set_attention: page_tokens must be 16, 32, 64 or 128, got %d", page_tokens);
+  if (seq_len < 1 || seq_len > 0x7fffffff - 4096) return set_error(c, QCFG_ESHAPE, "set_attention: bad seq_len");
+  if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return set_error(c, QCFG_EINVAL, "set_attention: sm_scale must be positive and finite");
+  if (window < 0 || (window > 0 && !causal)) return set_error(c, QCFG_EINVAL, "set_attention: a window needs causal attention");
+  AttnInput t;
+  t.on = true; t.k = k_layer; t.v = v_layer; t.q_heads = q_heads; t.kv_heads = kv_heads; t.dim = (int32_t)dim; t.seq_len = seq_len;
+  t.page = page_tokens; t.causal = causal ? 1 : 0; t.window = window; t.scale = sm_scale;
+  for (int p : {k_layer, v_layer}) {                // an output with a reader that takes no codes stays in fp32
+    auto& readers = M->L[p].consumers;
+    if (std::find(readers.begin(), readers.end(), layer) == readers.end()) readers.push_back(layer);
+  }
+  S.attn = t;
+  M->has_attn = true;
+  M->calibrated = M->evaluated = M->reuse_valid = false;     // the layers behind see other inputs
+  return QCFG_OK;
+}
+
 int qcfg_model_destroy(qcfg_model* model) {
   if (!model) return QCFG_EINVAL;
   cudaDeviceSynchronize();
@@ -1346,6 +1476,7 @@ int qcfg_model_destroy(qcfg_model* model) {
     for (auto& W : S.wc) { W.codes.release(); W.scale.release(); W.inv.release(); }
   }
   M->act_absmax_dev.release();
+  M->attn_pool.release(); M->attn_cache.release(); M->attn_copy.release();
   M->search_ref.release(); M->search_out.release(); M->search_partial.release();
   M->noise_codes.release();
   M->adj_gs.release(); M->adj_gt.release(); M->adj_qxt.release(); M->adj_qwt.release();
@@ -1665,7 +1796,8 @@ int qcfg_noise_sensitivity(qcfg_ctx* ctx, qcfg_model* model, const float* x_dev,
     reach[i][i] = 1;
     for (int l = i + 1; l < n; ++l) {
       const qcfg_layer& d = M->L[l].d;
-      reach[i][l] = (d.src >= 0 && reach[i][d.src]) || (d.residual_from >= 0 && reach[i][d.residual_from]);
+      const AttnInput& t = M->L[l].attn;
+      reach[i][l] = (d.src >= 0 && reach[i][d.src]) || (d.residual_from >= 0 && reach[i][d.residual_from]) || (t.on && (reach[i][t.k] || reach[i][t.v]));
     }
   }
   // The noise-free model, every layer at 16 bit, then one perturbed layer at a time, last layer first: the
@@ -1936,8 +2068,8 @@ int adjust_reference(qcfg_ctx* h, Model* M, const float* x_dev, int64_t m, cudaS
   Ctx* c = &h->c;
   const int n = (int)M->L.size();
   for (int l = 0; l < n; ++l)
-    if (M->L[l].d.kh > 0 || M->L[l].d.pool_before != QCFG_POOL_NONE)
-      return set_error(c, QCFG_ESHAPE, "scale adjustment covers linear layers only (layer %d is a convolution or pooled)", l);
+    if (M->L[l].d.kh > 0 || M->L[l].d.pool_before != QCFG_POOL_NONE || M->L[l].attn.on)
+      return set_error(c, QCFG_ESHAPE, "scale adjustment covers linear layers only (layer %d is a convolution, pooled or behind an attention)", l);
   std::vector<uint8_t> b16((size_t)n, 16);
   std::vector<float*> ys((size_t)n, nullptr);
   int rc = M->search_ref.ensure(c, (size_t)(m * M->L[n - 1].d.n_out) * 4);

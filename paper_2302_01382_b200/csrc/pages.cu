@@ -4,6 +4,8 @@
 // A page of a head is quantized with one maximum (Eq. 1 at b = 8 over page_tokens x head_dim values).
 #include <cooperative_groups.h>
 
+#include <algorithm>
+
 #include "serve.cuh"
 
 namespace cg = cooperative_groups;
@@ -559,8 +561,33 @@ __global__ void __launch_bounds__(kReadThreads, 5) kv_read_kernel(PoolView p, Ca
   }
 }
 
+// A pool whose sequences all have the same length: sequence i holds the pages i * max_pages and on.
+__global__ void __launch_bounds__(256) kv_layout_kernel(PoolView p, int32_t* seqs, int32_t* starts, int seq_len, int64_t rows) {
+  pdl_entry();
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i <= p.max_seqs) {
+    const int64_t lo = min(i * seq_len, rows);
+    starts[i] = (int32_t)lo;
+    if (i < p.max_seqs) {
+      seqs[i] = (int32_t)i;
+      p.len[i] = (int32_t)min((int64_t)seq_len, rows - lo);
+    }
+  }
+  if (i < p.n_pages) {
+    const int64_t lo = i / p.max_pages * seq_len + i % p.max_pages * p.page;      // its first token's row
+    const bool held = lo < rows;
+    p.table[i] = held ? (int32_t)i : -1;
+    p.refs[i] = held ? 1 : 0;
+  }
+}
+
 }  // namespace
 
+int launch_kv_layout(Ctx* ctx, const PoolView& p, int32_t* seqs, int32_t* starts, int seq_len, int64_t rows, cudaStream_t st) {
+  launch_pdl(kv_layout_kernel, dim3((unsigned)((std::max(p.n_pages, p.max_seqs + 1) + 255) / 256)), dim3(256), 0, st, p, seqs, starts, seq_len, rows);
+  count_launch(ctx);
+  return check_cuda(ctx, cudaGetLastError(), "kv_layout");
+}
 int launch_kv_extend(Ctx* ctx, const PoolView& p, const BatchView& b, cudaStream_t st) {
   if (b.n == 0) return QCFG_OK;
   const size_t smem = (size_t)b.n * 8;

@@ -42,6 +42,9 @@ struct BatchView {
 
 // ----- pages.cu -------------------------------------------------------------------------
 int launch_kv_extend(Ctx* ctx, const PoolView& p, const BatchView& b, cudaStream_t st);
+// Lays the pool out for n_seqs sequences of seq_len tokens (the last may be shorter), rows in all: fills table, len and
+// refs of the pool and the batch over it.
+int launch_kv_layout(Ctx* ctx, const PoolView& p, int32_t* seqs, int32_t* starts, int seq_len, int64_t rows, cudaStream_t st);
 int launch_kv_free(Ctx* ctx, const PoolView& p, const int32_t* seqs, int n, cudaStream_t st);
 int launch_kv_fork(Ctx* ctx, const PoolView& p, const int32_t* parents, const int32_t* children, int n, int32_t* src, int32_t* dst, cudaStream_t st);
 int launch_kv_compact(Ctx* ctx, const PoolView& p, int32_t* map, cudaStream_t st);
