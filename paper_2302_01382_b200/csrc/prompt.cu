@@ -422,13 +422,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
         f[g] = fmaxf(row_f * f[g], 1.2e-38f);
       }
       const bool masked = __any_sync(0xffffffffu, some || from > 0 || to < kStepTokens);
-      // scores of 32 tokens that are not seen
-      auto mask = [&](uint32_t (&v)[32], int c) {
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          const int t = 32 * c + k;
-          if (t < from || t >= to || sc.key[2 * c + (k >> 4)] < 0.0f) v[k] = 0xff800000u;
-        }
+      // which of 32 tokens are seen, a bit each (a comparison and a look at the scale for each token made such steps 5 times as long)
+      auto seen_bits = [&](int c) {
+        const int first = from - 32 * c, end = to - 32 * c;
+        const uint32_t below = end <= 0 ? 0u : end >= 32 ? 0xffffffffu : (1u << end) - 1u;
+        const uint32_t above = first <= 0 ? 0xffffffffu : first >= 32 ? 0u : 0xffffffffu << first;
+        return below & above & (sc.key[2 * c] < 0.0f ? 0xffff0000u : 0xffffffffu) & (sc.key[2 * c + 1] < 0.0f ? 0xffffu : 0xffffffffu);
       };
       // Weights of BLOCK x 32 tokens at a time (all of them; fp32, with twice as many to hold, 32), over scores that have been read: group
       // g of 16 in columns kPart * g on.  The next 32 scores are on their way meanwhile.  The reference is a whole number, and moves only
@@ -452,7 +451,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
             uint32_t (&x32)[32] = v[(c - b) & 1];
             tmem_ld_wait();
             if (c + 1 < b + BLOCK) tmem_ld32_issue(s_row + 32 * (c + 1), v[(c + 1 - b) & 1]);
-            if (masked) mask(x32, c);
+            if (masked) {
+              const uint32_t seen = seen_bits(c);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) x32[k] = seen & 1u << k ? x32[k] : 0xff800000u;
+            }
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
               const float f1 = f[2 * c + z], at1 = shift + log_share[2 * c + z];
@@ -474,55 +477,59 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
             }
           }
         };
-        take();
-        if (__any_sync(0xffffffffu, fresh || large)) {
-          float most = -INFINITY;
+        bool move = fresh;                 // of the row's reference; written once, so that a step's code stays in the instruction cache and in registers
 #pragma unroll 1
-          for (int g = 2 * b; g < 2 * (b + BLOCK); ++g) {
-            uint32_t x[16];
-            tmem_ld16(s_row + 16 * g, x);
-            tmem_ld_wait();
-            const float key = sc.key[g];
-            float m = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < 16; ++k)
-              if (!masked || (16 * g + k >= from && 16 * g + k < to && key >= 0.0f)) m = fmaxf(m, __uint_as_float(x[k]));
-            most = fmaxf(most, m * fmaxf(row_f * key, 1.2e-38f));
-          }
-          const float was = ref;
-          if (fresh || large) ref = fmaxf(ref, ceilf(most));
-          fresh = ref == -INFINITY;
-          const float keep = ex2(was - (fresh ? 0.0f : ref));
-          if (__any_sync(0xffffffffu, keep != 1.0f)) {
-            sum *= keep;
-            part *= keep;
-            if (b > 0) tmem_st_wait();       // loads are not ordered behind stores that have not been waited for
+        for (int go = 0; go < 2; ++go) {
+          if (__any_sync(0xffffffffu, move)) {
+            float most = -INFINITY;
 #pragma unroll 1
-            for (int h = 0; h < (int)kPart / 8 * 2 * b; ++h) {
-              uint32_t w[8];
-              tmem_ld8(s_row + 8 * h, w);
+            for (int g = 2 * b; g < 2 * (b + BLOCK); ++g) {
+              uint32_t x[16];
+              tmem_ld16(s_row + 16 * g, x);
               tmem_ld_wait();
+              const uint32_t seen = masked ? seen_bits(g >> 1) >> (16 * (g & 1)) : 0xffffu;
+              float m = -INFINITY;
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {      // (the factor itself may be too small for fp16)
-                const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
-                w[k] = pack_h2(e.x * keep, e.y * keep);
+              for (int k = 0; k < 16; ++k) m = fmaxf(m, seen & 1u << k ? __uint_as_float(x[k]) : -INFINITY);
+              most = fmaxf(most, m * fmaxf(row_f * sc.key[g], 1.2e-38f));
+            }
+            const float was = ref;
+            if (move) ref = fmaxf(ref, ceilf(most));
+            fresh = ref == -INFINITY;
+            const float keep = ex2(was - (fresh ? 0.0f : ref));
+            if (__any_sync(0xffffffffu, keep != 1.0f)) {
+              sum *= keep;
+              part *= keep;
+              if (b > 0) tmem_st_wait();       // loads are not ordered behind stores that have not been waited for
+#pragma unroll 1
+              for (int h = 0; h < (int)kPart / 8 * 2 * b; ++h) {
+                uint32_t w[8];
+                tmem_ld8(s_row + 8 * h, w);
+                tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {      // (the factor itself may be too small for fp16)
+                  const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+                  w[k] = pack_h2(e.x * keep, e.y * keep);
+                }
+                tmem_st8(s_row + 8 * h, w);
               }
-              tmem_st8(s_row + 8 * h, w);
-            }
-            // the products so far have been completed in front of these scores
+              // the products so far have been completed in front of these scores
 #pragma unroll 1
-            for (int h = 0; j > 0 && h < (WIDE ? 2 : 1) * D / 16; ++h) {
-              const uint32_t at = h < D / 16 ? o_row + 16 * h : l_row + 16 * (h - D / 16);
-              uint32_t w[16];
-              tmem_ld16(at, w);
-              tmem_ld_wait();
+              for (int h = 0; j > 0 && h < (WIDE ? 2 : 1) * D / 16; ++h) {
+                const uint32_t at = h < D / 16 ? o_row + 16 * h : l_row + 16 * (h - D / 16);
+                uint32_t w[16];
+                tmem_ld16(at, w);
+                tmem_ld_wait();
 #pragma unroll
-              for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * keep);
-              tmem_st16(at, w);
+                for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * keep);
+                tmem_st16(at, w);
+              }
+              tmem_st_wait();
             }
-            tmem_st_wait();
           }
           take();
+          move = large;
+          if (!__any_sync(0xffffffffu, move)) break;
         }
         part += block_part;
 #pragma unroll
