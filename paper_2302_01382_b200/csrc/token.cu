@@ -8,7 +8,8 @@ namespace qcfg {
 namespace {
 
 // WPR warps (1 or 8) for each row, which they read once and keep in registers, as it came, while it fits: HELD pieces of 16 bytes a
-// thread (2, 4 or 8: the fewer, the more rows are on their way), or with VEC false (rows not on 16-byte boundaries) single elements.  What does not fit is read twice, the second time from L2.
+// thread (2, 4 or 8: the fewer, the more rows are on their way).  What does not fit is read twice, the second time from L2.  With VEC
+// false (rows not on 16-byte boundaries) a piece is cut out of the two aligned ones it lies in, at the row's ends element by element.
 // HBM bounds it once an element costs no more than its share: clamp and round in two operations (magic number, low byte), the
 // test for NaN, Inf and an infinite inverse once a row.  12288 x 768 bf16 21.3 -> 8.1 us against the first form, which held floats.
 constexpr int kTokenThreads = 256, kHeldMost = 8;
@@ -27,7 +28,7 @@ __global__ void __launch_bounds__(kTokenThreads, HELD == 2 ? 6 : HELD == 4 ? 5 :
   // late: the next kernel may begin only once everything in front of this one has completed (see few_tokens_kernel)
   if (late) asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");
   else pdl_entry();
-  constexpr int V = VEC ? Vec<T>::N : 1, N = 32 * WPR;
+  constexpr int V = Vec<T>::N, N = 32 * WPR;
   union Piece { uint4 u; T t[Vec<T>::N]; };
   __shared__ unsigned tops[8];
   const int64_t row = WPR == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -38,9 +39,26 @@ __global__ void __launch_bounds__(kTokenThreads, HELD == 2 ? 6 : HELD == 4 ? 5 :
   const int pieces = (int)(cols / V);
   Piece held[HELD];
   unsigned top = 0;
+  const int off = VEC ? 0 : (int)(reinterpret_cast<uintptr_t>(x) & 15);                  // bytes behind a boundary
+  const int whole = VEC ? 0 : (int)((cols * (int64_t)sizeof(T) + off) / 16) - 1;       // pieces 1 .. whole - 1 lie in two aligned ones of the row
   auto get = [&](int p, Piece& f) {
-    if (VEC) f.u = __ldg(reinterpret_cast<const uint4*>(x) + p);
-    else f.t[0] = x[p];
+    if (VEC || off == 0) {
+      f.u = __ldg(reinterpret_cast<const uint4*>(x) + p);
+    } else if (p >= 1 && p < whole) {
+      const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(x) - off) + p;
+      const uint4 a = __ldg(from), b = __ldg(from + 1);
+      const uint32_t c[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      uint32_t d[6], e[5];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) d[i] = off & 8 ? c[i + 2] : c[i];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) e[i] = off & 4 ? d[i + 1] : d[i];
+      const uint32_t bits = 8 * (off & 3);
+      f.u = make_uint4(__funnelshift_r(e[0], e[1], bits), __funnelshift_r(e[1], e[2], bits), __funnelshift_r(e[2], e[3], bits), __funnelshift_r(e[3], e[4], bits));
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) f.t[j] = x[(int64_t)p * V + j];
+    }
   };
   auto largest = [&](const Piece& f) {        // a NaN or Inf orders above all others
 #pragma unroll
@@ -104,9 +122,8 @@ __global__ void __launch_bounds__(kTokenThreads, HELD == 2 ? 6 : HELD == 4 ? 5 :
 #pragma unroll
       for (int j = 0; j < V; ++j) b[j] = code_bits(to_float<T>(f.t[j]), inv, qmax);
       int8_t* to = q + (int64_t)p * V;
-      if constexpr (VEC && Vec<T>::N == 8) *reinterpret_cast<uint2*>(to) = make_uint2(low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
-      else if constexpr (VEC) *reinterpret_cast<uint32_t*>(to) = low_bytes(b[0], b[1], b[2], b[3]);
-      else *to = (int8_t)b[0];
+      if constexpr (V == 8) *reinterpret_cast<uint2*>(to) = make_uint2(low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
+      else *reinterpret_cast<uint32_t*>(to) = low_bytes(b[0], b[1], b[2], b[3]);
     };
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
@@ -353,7 +370,7 @@ template <typename T>
 static void quantize_as(Ctx* ctx, const T* x, int64_t rows, int64_t cols, int64_t ld, float qmax, int8_t* q, int64_t ldq, float* scale, int late, cudaStream_t st) {
   const bool vec = (uintptr_t)x % 16 == 0 && (rows == 1 || ld * (int64_t)sizeof(T) % 16 == 0);
   // a warp a row where a row fits its registers and there are rows enough to fill the GPU
-  const int64_t pieces = vec ? (cols + Vec<T>::N - 1) / Vec<T>::N : cols;
+  const int64_t pieces = (cols + Vec<T>::N - 1) / Vec<T>::N;
   const bool narrow = rows >= 8 * sm_count(ctx) && pieces <= 32 * kHeldMost;
   const int64_t each = (pieces + (narrow ? 31 : 255)) / (narrow ? 32 : 256);      // of a thread
   const dim3 grid((unsigned)(narrow ? (rows + 7) / 8 : rows)), block(kTokenThreads);
