@@ -889,7 +889,7 @@ int check_pool(Ctx* c, const char* who, const qcfg_kv_pool* p) {
   if (!p || !p->table_dev || !p->len_dev || !p->refs_dev) return set_error(c, QCFG_EINVAL, "%s: null pool", who);
   if (p->page_tokens != 16 && p->page_tokens != 32 && p->page_tokens != 64 && p->page_tokens != 128)
     return set_error(c, QCFG_ESHAPE, "%s: page_tokens must be 16, 32, 64 or 128, got %d", who, p->page_tokens);
-  if (p->n_pages < 1 || p->max_seqs < 1 || p->max_pages < 1 || (int64_t)p->max_pages * p->page_tokens > 0x7fffffff - 256)
+  if (p->n_pages < 1 || p->n_pages > 0x7fffffff - 8192 || p->max_seqs < 1 || p->max_seqs > 0x7fffffff - 8192 || p->max_pages < 1 || (int64_t)p->max_pages * p->page_tokens > 0x7fffffff - 256)
     return set_error(c, QCFG_ESHAPE, "%s: bad pool sizes", who);
   if ((uintptr_t)p->table_dev % 4 || (uintptr_t)p->len_dev % 4 || (uintptr_t)p->refs_dev % 4)
     return set_error(c, QCFG_EALIGN, "%s: pool arrays must be 4-byte aligned", who);
@@ -1366,6 +1366,7 @@ int qcfg_kv_attention(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cac
   if (rc) return rc;
   if (!dtype_ok(dtype)) return set_error(c, QCFG_EINVAL, "kv_attention: bad element type");
   if (batch->n_rows > 0 && batch->n > 0 && (!q_dev || !out_dev)) return set_error(c, QCFG_EINVAL, "kv_attention: null pointer");
+  if (batch->n_rows > 0 && q_dev == out_dev) return set_error(c, QCFG_EINVAL, "kv_attention: out_dev must not overlap q_dev");
   if (q_heads < 1 || q_heads % cache->kv_heads) return set_error(c, QCFG_ESHAPE, "kv_attention: q_heads must be a multiple of kv_heads");
   if (q_heads > 65535) return set_error(c, QCFG_ESHAPE, "kv_attention: too many heads");
   if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return set_error(c, QCFG_EINVAL, "kv_attention: sm_scale must be positive and finite");

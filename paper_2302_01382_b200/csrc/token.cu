@@ -12,7 +12,7 @@ namespace {
 // false (rows not on 16-byte boundaries) a piece is cut out of the two aligned ones it lies in, at the row's ends element by element.
 // HBM bounds it once an element costs no more than its share: clamp and round in two operations (magic number, low byte), the
 // test for NaN, Inf and an infinite inverse once a row.  12288 x 768 bf16 21.3 -> 8.6 us against the first form, which held floats; fp32
-// 10.5 us (4.5 TB/s).  1037 x 4001 fp16, rows off 16-byte boundaries: 11.7 us element by element, 8.9 this way.
+// 10.5 us (4.5 TB/s).  1037 x 4001 fp16, rows off 16-byte boundaries: 11.7 us element by element, 8.0 this way.
 constexpr int kTokenThreads = 256, kHeldMost = 8;
 // Bytes of the codes of elements that are all finite, with a finite inverse
 __device__ __forceinline__ uint32_t code_bits(float x, float inv, float qmax) {

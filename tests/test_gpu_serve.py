@@ -627,6 +627,25 @@ def test_attention_refusals(ctx):
     assert cache.attention(x[:0], s[:0]).shape == (0, 4, 64)
 
 
+def test_refusals_of_pools_beyond_32_bits_and_of_outputs_in_place(ctx):
+    import paper_2302_01382_b200 as q
+    pool, cache, _, _ = make(ctx, 8, 16, 3, 4, 2, 64)
+    x = torch.ones((2, 4, 64), device="cuda")
+    with pytest.raises(q.QcfgError) as e:
+        cache.attention(x, ints([0, 1]), out=x)
+    assert e.value.status == q.EINVAL
+    for field, value in (("n_pages", 0x7fffffff), ("max_seqs", 0x7fffffff), ("max_pages", 0x7fffffff // 16)):
+        before = getattr(pool._c, field)
+        setattr(pool._c, field, value)
+        for call in (lambda: pool.extend(ints([0])), lambda: pool.free(ints([0])), lambda: cache.attention(x, ints([0, 1]))):
+            with pytest.raises(q.QcfgError) as e:
+                call()
+            assert e.value.status == q.ESHAPE
+        setattr(pool._c, field, before)
+    assert not cache.attention(x, ints([0, 1])).any()
+    ctx.check_sync()
+
+
 # ----------------------------------------------------------------------------- together
 
 def block(ctx, cache, weights, x, seqs, starts, heads, group, dim):
