@@ -498,6 +498,35 @@ def test_attention_of_many_rows(ctx, page, q_heads, heads, dim, dtypes):
             assert ctx.launch_count() - before == (1 if "max_new" in kw or 135 * group >= (192 if dim == 64 else 64) else 2)
 
 
+def test_many_entries_and_heads(ctx):
+    """More entries than a block has threads, in every kernel that looks for its own; more heads than a warp has lanes."""
+    rng = np.random.default_rng(41)
+    n, heads = 500, 40
+    lens = [int(v) for v in rng.integers(0, 21, n)]
+    pool, cache, po, co = make(ctx, 2 * n, 16, n, 3, heads, 16)
+    order = [int(v) for v in rng.permutation(n)]
+    steps(ctx, pool, cache, po, co, order, [lens[s] for s in order], torch.bfloat16, rng)
+    steps(ctx, pool, cache, po, co, order[::-1], [1] * n, torch.bfloat16, rng, spread=2.0)
+    same_pool(pool, po)
+    same_cache(cache, co)
+    counts = [po.lens[s] for s in order]
+    k, v = cache.read(ints(order), ints([0] * n), ints(starts_of(counts)), sum(counts))
+    for z, got in enumerate((host(k), host(v))):
+        want = np.concatenate([co.values(s)[z] for s in order])
+        assert (np.abs(got - want) <= (U + half_step(torch.float32)) * np.abs(want) + 2.0 ** -25).all()
+    check_attention(ctx, cache, co, order, [min(2, po.lens[s]) for s in order], heads, torch.bfloat16, rng)
+    check_attention(ctx, cache, co, order, [min(2, po.lens[s]) for s in order], 2 * heads, torch.bfloat16, rng, max_len=22)
+    # the kernel for many rows: the hint says so
+    n = 420
+    lens = [int(v) for v in rng.integers(0, 6, n)]
+    lens[399] = 230
+    pool, cache, po, co = make(ctx, n + 20, 64, n, 4, 1, 64)
+    steps(ctx, pool, cache, po, co, list(range(n)), lens, torch.float16, rng)
+    before = ctx.launch_count()
+    check_attention(ctx, cache, co, list(range(n)), [min(v, 200) for v in lens], 2, torch.float16, rng, max_new=200)
+    assert ctx.launch_count() - before == 1
+
+
 def test_attention_of_uneven_scales(ctx):
     """Pages whose maxima differ by ten orders of magnitude, values of zero pages, scores up to hundreds."""
     for dtype in DTYPES:
