@@ -290,7 +290,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     const int n_tiles = two ? 2 : 1;
     bool ok = true;
     auto product_s = [&](int i, int j) {
-      if (!elected) return;
       const uint64_t k0 = tile_desc(k_sm + (j & 1) * kv_tile_bytes<D>(), 16);
 #pragma unroll
       for (int part = 0; part < (WIDE ? 2 : 1); ++part) {       // the queries' second halves first: they are added up while the sum is small
@@ -304,7 +303,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       tc_commit(s_full + 8 * i);
     };
     auto product_o = [&](int i, int j) {
-      if (!elected) return;
       const uint64_t v0 = tile_desc(v_sm + (j & 1) * kv_tile_bytes<D>(), HALF);
 #pragma unroll
       for (int part = 0; part < (WIDE ? 2 : 1); ++part)
@@ -315,29 +313,30 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     ok = mbar_wait_warp(q_full, 0, abort_flag, a.err) && mbar_wait_warp(k_full, 0, abort_flag, a.err);
     tc_fence_after();
     if (ok) {
-      for (int i = 0; i < n_tiles; ++i) product_s(i, 0);
-      if (elected) tc_commit(k_empty);
+      if (elected) {
+        for (int i = 0; i < n_tiles; ++i) product_s(i, 0);
+        tc_commit(k_empty);
+      }
+      __syncwarp();
     }
     for (int j = 0; j < steps && ok; ++j) {
       const uint32_t st = j & 1, ph = (j >> 1) & 1, st1 = st ^ 1, ph1 = ((j + 1) >> 1) & 1;
-      ok = mbar_wait_warp(v_full + 8 * st, ph, abort_flag, a.err);
+      const bool more = j + 1 < steps;
+      ok = mbar_wait_warp(v_full + 8 * st, ph, abort_flag, a.err) && (!more || mbar_wait_warp(k_full + 8 * st1, ph1, abort_flag, a.err));
       for (int i = 0; i < n_tiles && ok; ++i) {
         ok = mbar_wait_warp(p_ready + 8 * i, j & 1, abort_flag, a.err);
         if (!ok) break;
         tc_fence_after();
-        product_o(i, j);
-        if (elected && i == n_tiles - 1) tc_commit(v_empty + 8 * st);
-        if (j + 1 < steps) {
-          if (i == 0) {
-            ok = mbar_wait_warp(k_full + 8 * st1, ph1, abort_flag, a.err);
-            if (!ok) break;
-            tc_fence_after();
+        if (elected) {
+          product_o(i, j);
+          if (more) product_s(i, j + 1);
+          else tc_commit(o_done + 8 * i);
+          if (i == n_tiles - 1) {
+            tc_commit(v_empty + 8 * st);
+            if (more) tc_commit(k_empty + 8 * st1);
           }
-          product_s(i, j + 1);
-          if (elected && i == n_tiles - 1) tc_commit(k_empty + 8 * st1);
-        } else if (elected) {
-          tc_commit(o_done + 8 * i);
         }
+        __syncwarp();
       }
     }
     __syncwarp();
