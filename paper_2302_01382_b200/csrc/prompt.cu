@@ -14,7 +14,7 @@
 // What bounds it is neither but the chain of one tile: a step takes 4300 cycles, 2450 for a warp's 32 rows of weights (also where it
 // has its scheduler to itself), 350 until the tensor core knows of them, 1500 for the two products and the way back.  A block
 // costs 14000 cycles besides its steps (who it is, the queries, the first codes, the output).  4 entries of up to 2048 bf16 tokens behind up
-// to 4000, 32 heads on 8 of 128: 370 us, 828 TFLOP/s, 51% of the measured bf16 rate; 32 entries of up to 384 fp32 tokens, 12 heads of 64: 72 us.
+// to 4000, 32 heads on 8 of 128: 366 us, 838 TFLOP/s, 52% of the measured bf16 rate; 32 entries of up to 384 fp32 tokens, 12 heads of 64: 72 us.
 // Tried against 370 us: scores, weights and products in halves of 64 tokens, so that a tile never waits (403: 48 MMAs a step in
 // place of 32, at 54 cycles each whatever their width), weights in halves only (398), a warp that issues for each tile (448: registers),
 // queries fetched before the TMEM is there (383: registers).
@@ -35,6 +35,9 @@ constexpr int kGroups = kStepTokens / 16;        // scales are looked up for eac
 constexpr int kSoftWarps = 8, kConvWarps = 3;      // and one that issues: three warps a scheduler, 168 registers a thread
 constexpr int kPromptThreads = 32 * (kSoftWarps + kConvWarps + 1);
 constexpr int kTables = 4;
+// fp32: the second half of a weight, at most 2^-12 of it (2^4), is held times this, so that the many small weights of a long context
+// keep their digits: as it is it would end at 2^-25, next to a largest weight of 1 (100 tokens, values up to 9.5: off by 1.3e-6).
+constexpr float kRest = 1024.0f;
 
 template <int D, bool WIDE> __host__ __device__ constexpr int q_tile_bytes() { return kTileRows * D * 2 * (WIDE ? 2 : 1); }
 template <int D> __host__ __device__ constexpr int kv_tile_bytes() { return kStepTokens * D * 2; }
@@ -475,7 +478,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
                 acc[k & 1] = __fadd2_rn(acc[k & 1], e);
                 const __half2 h = __floats2half2_rn(e.x, e.y);
                 p[2 * (c - b) + z][k] = h2_bits(h);
-                if constexpr (WIDE) l[z][k] = pack_h2(e.x - __low2float(h), e.y - __high2float(h));
+                if constexpr (WIDE) {
+                  const float2 rest = __fmul2_rn(__fadd2_rn(e, make_float2(-__low2float(h), -__high2float(h))), make_float2(kRest, kRest));
+                  l[z][k] = pack_h2(rest.x, rest.y);
+                }
               }
               acc[0] = __fadd2_rn(acc[0], acc[1]);
               const float of16 = acc[0].x + acc[0].y;
@@ -570,7 +576,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
           tmem_ld32_issue(l_row + 32 * c, u);
           tmem_ld_wait();
 #pragma unroll
-          for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + __uint_as_float(u[k]));
+          for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(fmaf(__uint_as_float(u[k]), 1.0f / kRest, __uint_as_float(v[k])));
         }
 #pragma unroll
         for (int k = 0; k < 32; k += V) {
@@ -620,15 +626,16 @@ int prompt_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
 // Whether a call goes this way or streams the cache, by the rows of the longest entry as far as known.  A block takes 256 rows through the
 // whole context, so there have to be blocks for a good part of the SMs; streaming cuts the context instead, and repeats the
 // conversion of the codes for every 32 rows.  us, this way / streaming, entries x new tokens behind a context, heads x group, dim:
-//   8 heads x 4, 128   8 x 8, 1000 35.0 / 35.5    8 x 16, 1000 35.8 / 39.5    8 x 64, 1000 43 / 70    32 x 8, 1000 67 / 60    32 x 16, 1000 65 / 85
-//                      64 x 8, 4000 219 / 193     64 x 16, 4000 206 / 253     1 x 64, 1000 43 / 37    1 x 64, 30000 481 / 170
-//                      1 x 512, 1000 50 / 113     1 x 512, 30000 503 / 1122
-//   12 heads x 1, 64   8 x 64, 1000 39 / 28       8 x 128, 1000 39 / 39       32 x 64, 300 75 / 35    1 x 384, 0 35 / 19    32 x 384, 0 (fp32) 99 / 177
+//   8 heads x 4, 128   8 x 8, 1000 27 / 36      8 x 64, 1000 32 / 71     32 x 4, 1000 42 / 32     32 x 8, 1000 47 / 60    32 x 16, 1000 46 / 87
+//                      64 x 4, 4000 201 / 105   64 x 8, 4000 189 / 192   64 x 16, 4000 180 / 253
+//                      1 x 64, 1000 31 / 37     1 x 64, 30000 488 / 171  1 x 512, 1000 38 / 113   1 x 512, 30000 502 / 1127
+//   12 heads x 1, 64   8 x 32, 1000 24 / 26     8 x 64, 1000 25 / 28     8 x 128, 1000 24 / 39    32 x 32, 300 32 / 25    32 x 64, 300 34 / 35
+//          (fp32)      32 x 32, 300 38 / 28     32 x 64, 300 41 / 39     4 x 128, 300 20 / 18     32 x 384, 0 72 / 177
 bool prompt_pays(Ctx* ctx, const AttnArgs& a, int dtype, int64_t rows) {
   const int group = a.q_heads / a.cache.heads;
   if (group > kTileRows || (a.cache.dim != 64 && a.cache.dim != 128) || (dtype == QCFG_FP32 && a.cache.dim != 64)) return false;
   const int64_t blocks = std::max<int64_t>(a.batch.n, (a.batch.rows * group + 255) / 256) * a.cache.heads;
-  return rows * group >= (a.cache.dim == 128 ? 64 : 192) && 3 * blocks >= sm_count(ctx);
+  return rows * group >= (a.cache.dim == 128 ? 32 : 64) && 3 * blocks >= sm_count(ctx);
 }
 
 int launch_prompt(Ctx* ctx, const AttnArgs& a, int dtype, cudaStream_t st) {
