@@ -14,8 +14,8 @@
 // What bounds it is neither but the chain of one tile: a step takes 4300 cycles, 2450 for a warp's 32 rows of weights (also where it
 // has its scheduler to itself), 350 until the tensor core knows of them, 1500 for the two products and the way back.  A block
 // costs 14000 cycles besides its steps (who it is, the queries, the first codes, the output).  4 entries of up to 2048 bf16 tokens behind up
-// to 4000, 32 heads on 8 of 128: 366 us, 838 TFLOP/s, 52% of the measured bf16 rate; 32 entries of up to 384 fp32 tokens, 12 heads of 64: 72 us.
-// Tried against 370 us: scores, weights and products in halves of 64 tokens, so that a tile never waits (403: 48 MMAs a step in
+// to 4000, 32 heads on 8 of 128: 361 us, 849 TFLOP/s, 52% of the measured bf16 rate; 32 entries of up to 384 fp32 tokens, 12 heads of 64: 71 us.
+// Tried against 370 us then: scores, weights and products in halves of 64 tokens, so that a tile never waits (403: 48 MMAs a step in
 // place of 32, at 54 cycles each whatever their width), weights in halves only (398), a warp that issues for each tile (448: registers),
 // queries fetched before the TMEM is there (383: registers).
 // Numbers as in the streaming kernel: codes are exact in fp16, a page's key scale multiplies the scores' factor, its value scale the
@@ -630,7 +630,7 @@ int prompt_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
 //                      64 x 4, 4000 201 / 105   64 x 8, 4000 189 / 192   64 x 16, 4000 180 / 253
 //                      1 x 64, 1000 31 / 37     1 x 64, 30000 488 / 171  1 x 512, 1000 38 / 113   1 x 512, 30000 502 / 1127
 //   12 heads x 1, 64   8 x 32, 1000 24 / 26     8 x 64, 1000 25 / 28     8 x 128, 1000 24 / 39    32 x 32, 300 32 / 25    32 x 64, 300 34 / 35
-//          (fp32)      32 x 32, 300 38 / 28     32 x 64, 300 41 / 39     4 x 128, 300 20 / 18     32 x 384, 0 72 / 177
+//          (fp32)      32 x 32, 300 38 / 28     32 x 64, 300 41 / 39     4 x 128, 300 20 / 18     32 x 384, 0 71 / 177
 bool prompt_pays(Ctx* ctx, const AttnArgs& a, int dtype, int64_t rows) {
   const int group = a.q_heads / a.cache.heads;
   if (group > kTileRows || (a.cache.dim != 64 && a.cache.dim != 128) || (dtype == QCFG_FP32 && a.cache.dim != 64)) return false;
