@@ -4,8 +4,9 @@
 // The codes go to the tensor cores as fp16, which holds them exactly, and never exist as numbers of 16 bits in memory: a page's
 // scale multiplies the finished scores (keys) or the weights (values).  Queries are fp16 after a power of two has brought
 // their row's largest element to 2^12 .. 2^13, so bf16 and fp16 ones lose nothing above 2^-38 of the row; fp32 ones are the sum
-// of two fp16 numbers.  Weights are e = 2^(14 + x - max) times the page's share of the largest value scale seen, in fp16
-// (fp32 calls: the sum of two), which leaves 28 binary orders below the largest weight before the fp16 grid coarsens.
+// of two fp16 numbers.  Weights are e = 2^(7 + x - ref) times the page's share of the largest value scale seen, in fp16, with ref
+// at most 8 below the running maximum (fp32 calls: 2^(x - ref), the sum of two): 21 binary orders and more below the largest weight
+// before the fp16 grid coarsens.
 #include <algorithm>
 
 #include "attention.cuh"
