@@ -113,6 +113,13 @@ def test_linear(ctx, m, k, n, dtype, act, with_bias):
     ctx.check_sync()
 
 
+@pytest.mark.parametrize("m,k,n", [(1280, 300, 3136), (1280, 300, 2240), (1100, 130, 2311), (2000, 64, 2250), (257, 64, 16000)])
+@pytest.mark.parametrize("dtype,act,with_bias", [(torch.float32, "relu", True), (torch.float16, "none", False)])
+def test_linear_in_tiles_of_any_width(ctx, m, k, n, dtype, act, with_bias):
+    """Sizes whose tiles are 224, 160, 192 and other numbers of columns wide on 148 SMs."""
+    test_linear(ctx, m, k, n, dtype, act, with_bias)
+
+
 @pytest.mark.parametrize("m", [1, 7, 40, 260])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_linear_strided_rows_in_and_out(ctx, m, dtype):
