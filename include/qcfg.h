@@ -382,7 +382,7 @@ int qcfg_model_destroy(qcfg_model* model);
  * v_layer (kv_heads heads each, earlier layers with as many rows).  Rows come in runs of seq_len tokens, each run a sequence
  * of its own; the last may be shorter.  Keys and values pass through a cache at 8 bits with pages
  * of page_tokens (qcfg_kv_append) and are read by qcfg_kv_attention with sm_scale, causal and window, as
- * when the model serves: a configuration is judged on what it will be served with.  Every forward of the
+ * when the model serves: a configuration is evaluated with what it will be served with.  Every forward of the
  * model includes it, the calibration's too.  Once for a layer (QCFG_ESTATE); the model has to be calibrated
  * again.  The scale adjustment does not cover models with attention (QCFG_ESHAPE).                */
 int qcfg_model_set_attention(qcfg_ctx* ctx, qcfg_model* model, int32_t layer, int32_t k_layer, int32_t v_layer, int32_t q_heads,
