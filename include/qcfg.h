@@ -357,7 +357,7 @@ int qcfg_kv_read(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* c
  * empty sequence, an entry without one) gives zeros.  q_dev, out_dev: [n_rows] rows of
  * `dtype` with q_heads heads of head_dim elements, strides in elements, 16-byte aligned pointers and
  * strides (QCFG_EALIGN); head h reads cache head h / (q_heads / kv_heads).  out_dev must not
- * overlap q_dev.  Sums, maxima and accumulators are fp32.
+ * overlap q_dev.  A query with a NaN or Inf gives NaN where it sees something.  Sums, maxima and accumulators are fp32.
  * max_rows, max_len: the longest entry's rows and the longest sequence's tokens as far as the caller
  * knows them (0: unknown).  They only choose how the work is spread; the results hold for any value.
  * work_dev: qcfg_kv_attention_work bytes (of the same n_rows and max_len; 0: may be NULL) on a 256-byte

@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
           top = b > top ? b : top;
         }
         const int shift = row_shift(top);
-        const float up = exp2_of(shift);
+        const float up = top < 0x7f800000u ? exp2_of(shift) : __int_as_float(0x7fffffff);      // an Inf makes the row NaN, like a NaN
 #pragma unroll
         for (int c = 0; c < DP / 8 / V; ++c)
 #pragma unroll

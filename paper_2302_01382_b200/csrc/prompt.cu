@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
           const int other = __shfl_sync(0xffffffffu, up_by, k * LPR);
           if (lane == c * RPA + k) shift = other;
         }
-        const float up = exp2_of(up_by);
+        const float up = top < 0x7f800000u ? exp2_of(up_by) : __int_as_float(0x7fffffff);      // an Inf makes the row NaN, like a NaN
         uint32_t w[V / 2], l[V / 2];
 #pragma unroll
         for (int j = 0; j < V / 2; ++j) {

@@ -613,6 +613,43 @@ def test_attention_of_nonfinite_queries_and_bad_pages(ctx):
             assert torch.equal(got[rows:], clean[rows:]) and not got[:rows].any()
 
 
+@pytest.mark.parametrize("dim,dtype", [(64, torch.float32), (64, torch.bfloat16), (128, torch.float16)])
+def test_many_rows_with_nonfinite_queries_and_bad_pages(ctx, dim, dtype):
+    """In the kernel for many rows a NaN or Inf stays with its row, and a page that is not there with its sequence."""
+    import paper_2302_01382_b200 as q
+    rng = np.random.default_rng(dim)
+    pool, cache, po, co = make(ctx, 80, 16, 3, 24, 16, dim)
+    lens = [300, 257, 384]
+    steps(ctx, pool, cache, po, co, [0, 1, 2], lens, dtype, rng)
+    x = dev(rng.standard_normal((sum(lens), 16, dim)).astype(np.float32), dtype)
+    seqs, starts = ints([0, 1, 2]), ints(starts_of(lens))
+    run = lambda x: cache.attention(x, seqs, starts, max_new=384)
+    before = ctx.launch_count()
+    clean = run(x)
+    assert ctx.launch_count() - before == 1
+    bad = x.clone()
+    bad[5, 3, 0], bad[299, 3, 7], bad[301, 11, dim - 1] = float("nan"), float("inf"), -float("inf")
+    got = run(bad)
+    ctx.check_sync()
+    hit = torch.zeros(got.shape[:2], dtype=torch.bool, device="cuda")
+    hit[5, 3] = hit[299, 3] = hit[301, 11] = True
+    assert torch.isnan(got[hit].float()).all() and torch.equal(got[~hit], clean[~hit])
+    streamed = cache.attention(bad, seqs, starts, max_new=1)
+    assert torch.isnan(streamed[hit].float()).all() and torch.isfinite(streamed[~hit].float()).all()
+    pool.table[1, 3] = 1 << 20
+    pool.table[2, 0] = -1
+    got = run(x)
+    with pytest.raises(q.QcfgError) as e:
+        ctx.check_sync()
+    assert e.value.status == q.EPAGE
+    assert torch.equal(got[:300], clean[:300]) and torch.isfinite(got.float()).all()
+    # the rows in front of the page; the sequence's largest value scale may be that page's, so to the bits of the bound only
+    k, v = (t[:48] for t in co.values(1))
+    want, tol = attention_bound(host(x)[300:348], k, v, dim ** -0.5, True, 0, dtype)
+    assert (np.abs(host(got)[300:348] - want) <= tol).all()
+    assert not got[557:557 + 16].any()                               # these rows see that page only
+
+
 def test_garbage_behind_the_end_is_not_seen(ctx):
     """Codes behind the last token and the maxima of pages nobody holds do not matter, whatever they are."""
     for dtype in DTYPES:
