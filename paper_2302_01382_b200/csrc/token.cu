@@ -357,6 +357,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) few_tokens_kernel(const Few
     if (pass_lo >= tile_hi) return;
     count = min(RT, tile_hi - pass_lo);
     load_run = load_tile = 0;
+    fill = drain = 0;                  // (the empty fetches behind a pass's last step have moved one and not the other)
     __syncthreads();                   // the sums have been read
 #pragma unroll
     for (int i = 0; i < kAhead - 1; ++i) fetch();
