@@ -74,8 +74,9 @@ typedef struct qcfg_layer {
 int qcfg_create(qcfg_ctx** out, int device);
 int qcfg_destroy(qcfg_ctx* ctx);
 
-/* Synchronises `stream`, then returns and clears the device error word:
- * QCFG_OK, QCFG_ETIMEOUT, QCFG_ENONFINITE, QCFG_EPAGE or QCFG_ECUDA.                      */
+/* Synchronises `stream`, then returns what the device error word holds and clears it: QCFG_OK,
+ * QCFG_ETIMEOUT, QCFG_EPAGE, QCFG_ENONFINITE or QCFG_ECUDA.  Where several causes came up, the
+ * first of these is returned and cleared; the next call returns the next.                  */
 int qcfg_sync_status(qcfg_ctx* ctx, void* stream);
 /* Self-test of the failure path of the kernels' bounded waits (every device-side wait, on a
  * barrier or on a counter in shared or global memory, gives up after a time limit instead of

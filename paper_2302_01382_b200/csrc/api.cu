@@ -114,6 +114,7 @@ void prof_end(Ctx* ctx, int cls, double ops, cudaStream_t st) {
 void count_launch(Ctx* ctx, int n) { ctx->launches += n; }
 void count_form(Ctx* ctx, int form) { ctx->forms[form] += 1; }
 unsigned* err_word(Ctx* ctx) { return ctx->err_dev; }
+static __global__ void clear_error_kernel(unsigned* word, unsigned bits) { atomicAnd(word, ~bits); }
 int sm_count(Ctx* ctx) { return ctx->sms; }
 bool ctx_pair_enabled(Ctx* ctx) { return ctx->pair != 0; }
 int* pair_cluster_cache(Ctx* ctx) { return ctx->pair_clusters; }
@@ -980,11 +981,19 @@ int qcfg_sync_status(qcfg_ctx* ctx, void* stream) {
   if (e != cudaSuccess) return check_cuda(c, e, "stream synchronize");
   const unsigned w = *reinterpret_cast<volatile unsigned*>(c->pin_buf);
   if (w) {
-    cudaMemset(c->err_dev, 0, sizeof(w));
-    gemm_chain_reset(c);
-    if (w & ERR_TIMEOUT) return set_error(c, QCFG_ETIMEOUT, "a bounded device-side wait gave up");
-    if (w & ERR_NONFINITE) return set_error(c, QCFG_ENONFINITE, "non-finite value found on the device");
-    if (w & ERR_PAGE) return set_error(c, QCFG_EPAGE, "cache: a number out of range, too few free pages, or a sequence listed twice");
+    // one cause a call, work left out ahead of values replaced; the others, and what other streams set meanwhile, stay for the next
+    const unsigned cause = w & ERR_TIMEOUT ? ERR_TIMEOUT : w & ERR_PAGE ? ERR_PAGE : w;
+    DeviceScope dev(c);
+    if (!dev.ok) return set_error(c, QCFG_ECUDA, "sync_status: device not available");
+    clear_error_kernel<<<1, 1, 0, (cudaStream_t)stream>>>(c->err_dev, cause);
+    count_launch(c);
+    e = cudaGetLastError();
+    if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+    if (e != cudaSuccess) return check_cuda(c, e, "stream synchronize");
+    if (cause != ERR_PAGE) gemm_chain_reset(c);        // (the cache's calls are no part of a chain)
+    if (cause == ERR_TIMEOUT) return set_error(c, QCFG_ETIMEOUT, "a bounded device-side wait gave up");
+    if (cause == ERR_PAGE) return set_error(c, QCFG_EPAGE, "cache: a number out of range, too few free pages, or a sequence listed twice");
+    return set_error(c, QCFG_ENONFINITE, "non-finite value found on the device");
   }
   return QCFG_OK;
 }

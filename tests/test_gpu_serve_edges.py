@@ -36,3 +36,27 @@ def test_linear_of_few_tokens_into_many_strided_columns(ctx):
     room[1:m + 1, 3:3 + n] = 7
     assert (room == 7).all()
     ctx.check_sync()
+
+
+# ----------------------------------------------------------------------------- what surfaces
+
+def test_every_cause_surfaces(ctx):
+    """A value that is not finite does not hide pages that ran out, and the other way round: one cause a call, the gravest first."""
+    import paper_2302_01382_b200 as q
+    pool, cache, po, co = make(ctx, 4, 16, 2, 4)
+    x = torch.full((3, 8), float("nan"), device="cuda")
+    for order in (0, 1):
+        if order:
+            ctx.quantize_tokens(x)
+        pool.extend(ints([0]), ints([0, 65]))          # longer than a row of the table
+        ctx.quantize_tokens(x)
+        assert [ctx.sync_status() for _ in range(4)] == [q.EPAGE, q.ENONFINITE, q.OK, q.OK]
+    ctx.quantize_tokens(x)
+    ctx.selftest_wait_timeout(1000)
+    pool.free(ints([2]))
+    assert [ctx.sync_status() for _ in range(4)] == [q.ETIMEOUT, q.EPAGE, q.ENONFINITE, q.OK]
+    side = torch.cuda.Stream()
+    pool.free(ints([2]), stream=side)
+    assert ctx.sync_status(side) == q.EPAGE
+    ctx.check_sync()
+    same_pool(pool, po)
