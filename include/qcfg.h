@@ -281,7 +281,7 @@ int qcfg_linear_i8(qcfg_ctx* ctx, const void* x_dev, int x_dtype, int64_t ldx, i
                    int y_dtype, int64_t ldy, void* work_dev, int64_t work_bytes, void* stream);
 
 /* Pages and the sequences that hold them; one pool serves the caches of all layers.  Device memory
- * of the caller, filled with -1 / 0 / 0 at first and then kept by the calls below.  A sequence of
+ * of the caller, filled with -1 / 0 / 0 / 0 at first and then kept by the calls below.  A sequence of
  * len tokens holds ceil(len / page_tokens) pages, in order.                                    */
 typedef struct qcfg_kv_pool {
   int32_t* table_dev;    /* [max_seqs][max_pages] page numbers, -1 behind the last             */
@@ -290,6 +290,7 @@ typedef struct qcfg_kv_pool {
   int32_t n_pages;
   int32_t page_tokens;   /* 16, 32, 64 or 128                                                  */
   int32_t max_seqs, max_pages;
+  int32_t* refused_dev;  /* [max_seqs] 1 where the last qcfg_kv_extend with the sequence was refused */
 } qcfg_kv_pool;
 /* One layer's keys and values: int8 codes on the 8-bit grid of Eq. 1, one maximum for each page and
  * head from which the scales follow as in qcfg_scales_from_absmax.  16-byte aligned.           */
@@ -313,7 +314,8 @@ typedef struct qcfg_kv_batch {
 /* Makes every sequence of the batch longer by its rows: pages are taken where the last one is full,
  * lowest free numbers first, in the order of the entries, and len grows.  All or nothing: with too
  * few free pages, a row of the table too short or a sequence listed twice nothing changes
- * (QCFG_EPAGE from qcfg_sync_status).  At most 8192 entries (QCFG_ESHAPE).                       */
+ * (QCFG_EPAGE from qcfg_sync_status), and qcfg_kv_append leaves the sequences of the batch out until a later
+ * call makes room for them: there is nothing to be seen to between the two.  At most 8192 entries (QCFG_ESHAPE). */
 int qcfg_kv_extend(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_batch* batch, void* stream);
 /* Gives back every page of the n sequences (a page held by others too stays theirs); their length is 0 then.
  * Entries of -1 and empty sequences are passed over.                                           */
@@ -341,8 +343,8 @@ int qcfg_kv_copy_pages(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_ca
  * (one fp32 division, one product); a page that begins with a new token forgets what it held.
  * NaN and Inf are held as 0, do not count for the maximum and surface as QCFG_ENONFINITE.  k_dev, v_dev: [n_rows] rows of
  * `dtype`, row and head strides in elements, 16-byte aligned pointers and strides (QCFG_EALIGN).
- * Pages that several sequences hold are not written, nor is a sequence listed twice (QCFG_EPAGE from
- * qcfg_sync_status).                                                                           */
+ * Pages that several sequences hold are not written, nor is a sequence listed twice or one whose last
+ * qcfg_kv_extend was refused (QCFG_EPAGE from qcfg_sync_status).                               */
 int qcfg_kv_append(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch, const void* k_dev,
                    const void* v_dev, int dtype, int64_t row_stride, int64_t head_stride, void* stream);
 /* Values of cached tokens: row r of entry i is the token first_dev[i] + r of its sequence, code * scale, rounded once to

@@ -52,7 +52,7 @@ class LayerStruct(C.Structure):
 
 class PoolStruct(C.Structure):
     _fields_ = [("table_dev", C.c_void_p), ("len_dev", C.c_void_p), ("refs_dev", C.c_void_p), ("n_pages", C.c_int32),
-                ("page_tokens", C.c_int32), ("max_seqs", C.c_int32), ("max_pages", C.c_int32)]
+                ("page_tokens", C.c_int32), ("max_seqs", C.c_int32), ("max_pages", C.c_int32), ("refused_dev", C.c_void_p)]
 
 
 class CacheStruct(C.Structure):
@@ -437,20 +437,23 @@ def _int32(x: Optional[torch.Tensor], n: Optional[int] = None):
 
 class KvPool:
     """Pages and the sequences that hold them (qcfg_kv_pool).  table [max_seqs, max_pages], lens [max_seqs] and refs [n_pages]
-    are int32 tensors on the context's device, made here unless given."""
+    are int32 tensors on the context's device, made here unless given.  refused [max_seqs]: 1 where the last extend with the sequence
+    was refused; append leaves such sequences out."""
 
     def __init__(self, ctx: Context, n_pages: int, page_tokens: int, max_seqs: int, max_pages: int, table: Optional[torch.Tensor] = None,
-                 lens: Optional[torch.Tensor] = None, refs: Optional[torch.Tensor] = None):
+                 lens: Optional[torch.Tensor] = None, refs: Optional[torch.Tensor] = None, refused: Optional[torch.Tensor] = None):
         dev = torch.device("cuda", ctx.device)
         self.ctx = ctx
         self.table = torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=dev) if table is None else table
         self.lens = torch.zeros(max_seqs, dtype=torch.int32, device=dev) if lens is None else lens
         self.refs = torch.zeros(n_pages, dtype=torch.int32, device=dev) if refs is None else refs
-        ctx._on_device(self.table, self.lens, self.refs)
-        for t, n in ((self.table, max_seqs * max_pages), (self.lens, max_seqs), (self.refs, n_pages)):
+        self.refused = torch.zeros(max_seqs, dtype=torch.int32, device=dev) if refused is None else refused
+        ctx._on_device(self.table, self.lens, self.refs, self.refused)
+        for t, n in ((self.table, max_seqs * max_pages), (self.lens, max_seqs), (self.refs, n_pages), (self.refused, max_seqs)):
             _int32(t, n)
         self.n_pages, self.page_tokens, self.max_seqs, self.max_pages = n_pages, page_tokens, max_seqs, max_pages
-        self._c = PoolStruct(self.table.data_ptr(), self.lens.data_ptr(), self.refs.data_ptr(), n_pages, page_tokens, max_seqs, max_pages)
+        self._c = PoolStruct(self.table.data_ptr(), self.lens.data_ptr(), self.refs.data_ptr(), n_pages, page_tokens, max_seqs, max_pages,
+                             self.refused.data_ptr())
         self._ref = C.byref(self._c)
 
     def _batch(self, seqs: torch.Tensor, starts: Optional[torch.Tensor], rows: int):
@@ -463,7 +466,8 @@ class KvPool:
         return C.byref(BatchStruct(seqs.data_ptr(), starts.data_ptr(), n, rows))
 
     def extend(self, seqs: torch.Tensor, starts: Optional[torch.Tensor] = None, rows: Optional[int] = None, stream=None):
-        """Every sequence of `seqs` gets room for its rows (starts[i+1] - starts[i]; one each without starts)."""
+        """Every sequence of `seqs` gets room for its rows (starts[i+1] - starts[i]; one each without starts).  All or nothing: without
+        room nothing changes, append leaves these sequences out, and EPAGE surfaces from sync_status."""
         ctx = self.ctx
         ctx._check(ctx.lib.qcfg_kv_extend(ctx.h, self._ref, self._batch(seqs, starts, 0x7fffffff - 4096 if rows is None else rows),
                                           ctx._here(stream)))

@@ -887,12 +887,12 @@ bool dtype_ok(int t) { return t >= QCFG_FP32 && t <= QCFG_FP16; }
 int dtype_size(int t) { return t == QCFG_FP32 ? 4 : 2; }
 
 int check_pool(Ctx* c, const char* who, const qcfg_kv_pool* p) {
-  if (!p || !p->table_dev || !p->len_dev || !p->refs_dev) return set_error(c, QCFG_EINVAL, "%s: null pool", who);
+  if (!p || !p->table_dev || !p->len_dev || !p->refs_dev || !p->refused_dev) return set_error(c, QCFG_EINVAL, "%s: null pool", who);
   if (p->page_tokens != 16 && p->page_tokens != 32 && p->page_tokens != 64 && p->page_tokens != 128)
     return set_error(c, QCFG_ESHAPE, "%s: page_tokens must be 16, 32, 64 or 128, got %d", who, p->page_tokens);
   if (p->n_pages < 1 || p->n_pages > 0x7fffffff - 8192 || p->max_seqs < 1 || p->max_seqs > 0x7fffffff - 8192 || p->max_pages < 1 || (int64_t)p->max_pages * p->page_tokens > 0x7fffffff - 256)
     return set_error(c, QCFG_ESHAPE, "%s: bad pool sizes", who);
-  if ((uintptr_t)p->table_dev % 4 || (uintptr_t)p->len_dev % 4 || (uintptr_t)p->refs_dev % 4)
+  if ((uintptr_t)p->table_dev % 4 || (uintptr_t)p->len_dev % 4 || (uintptr_t)p->refs_dev % 4 || (uintptr_t)p->refused_dev % 4)
     return set_error(c, QCFG_EALIGN, "%s: pool arrays must be 4-byte aligned", who);
   return QCFG_OK;
 }
@@ -911,7 +911,7 @@ int check_batch(Ctx* c, const char* who, const qcfg_kv_batch* b) {
   if ((uintptr_t)b->seqs_dev % 4 || (uintptr_t)b->starts_dev % 4) return set_error(c, QCFG_EALIGN, "%s: batch arrays must be 4-byte aligned", who);
   return QCFG_OK;
 }
-PoolView view(const qcfg_kv_pool* p) { return {p->table_dev, p->len_dev, p->refs_dev, p->n_pages, p->page_tokens, p->max_seqs, p->max_pages}; }
+PoolView view(const qcfg_kv_pool* p) { return {p->table_dev, p->len_dev, p->refs_dev, p->n_pages, p->page_tokens, p->max_seqs, p->max_pages, p->refused_dev}; }
 CacheView view(const qcfg_kv_cache* k) { return {k->k_dev, k->v_dev, k->k_absmax_dev, k->v_absmax_dev, k->kv_heads, k->head_dim}; }
 BatchView view(const qcfg_kv_batch* b) { return {b->seqs_dev, b->starts_dev, b->n, b->n_rows}; }
 

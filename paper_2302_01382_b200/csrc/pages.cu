@@ -105,9 +105,12 @@ __global__ void __launch_bounds__(kPlanThreads) kv_extend_kernel(PoolView p, Bat
       p.refs[page] = 1;
     });
   __syncthreads();
+  // an append behind a refused call must not take the last tokens for the ones that got no room
   for (int i = threadIdx.x; i < b.n; i += kPlanThreads) {
+    const int s = b.seqs[i];
+    if (p.refused && s >= 0 && s < p.max_seqs) p.refused[s] = !ok;
     if (grown[i] < 0) continue;
-    int* len = p.len + b.seqs[i];
+    int* len = p.len + s;
     *len = ok ? grown[i] : (int)((unsigned)*len & ~kMark);
   }
   if (!ok && threadIdx.x == 0) atomicOr(err, ERR_PAGE);
@@ -126,7 +129,10 @@ __global__ void __launch_bounds__(128) kv_free_kernel(PoolView p, const int32_t*
     if (page >= 0 && page < p.n_pages) atomicSub(p.refs + page, 1);
     else if (page != -1) atomicOr(err, ERR_PAGE);
   }
-  if (threadIdx.x == 0) p.len[s] = 0;
+  if (threadIdx.x == 0) {
+    p.len[s] = 0;
+    if (p.refused) p.refused[s] = 0;
+  }
 }
 
 // One cluster: its first block checks the forks and takes their pages, then all blocks copy the table rows, a warp each.
@@ -189,7 +195,10 @@ kv_fork_kernel(PoolView p, const int32_t* parents, const int32_t* children, int 
         if (page >= 0 && page < p.n_pages) atomicAdd(p.refs + page, 1);
         else atomicOr(err, ERR_PAGE);
       }
-    if (lane == 0) p.len[children[f]] = failed ? 0 : len;
+    if (lane == 0) {
+      p.len[children[f]] = failed ? 0 : len;
+      if (p.refused && !failed) p.refused[children[f]] = 0;
+    }
   }
   cluster.sync();                  // the first block's shared memory has been read
 }
@@ -311,9 +320,10 @@ __global__ void __launch_bounds__(kCopyThreads) kv_copy_kernel(CacheView c, int 
 // everything that has to be known of the block's own is fetched at once.
 struct Claim {
   int64_t row0;
-  int entry, rows, nth, seq, len, twice;
+  int entry, rows, nth, seq, len, twice, refused;
 };
-// twice: whether the sequence is listed by another entry too (only where asked for).  Whole block; false: nothing to do.
+// twice: whether the sequence is listed by another entry too, refused: whether it got no room (both only where asked for).
+// Whole block; false: nothing to do.
 __device__ __forceinline__ bool claim_item(const PoolView& p, const BatchView& b, int64_t item, int unit, bool want_twice, Claim* c, unsigned* err) {
   if (threadIdx.x == 0) { c->entry = -1; c->twice = 0; }
   __syncthreads();
@@ -324,7 +334,9 @@ __device__ __forceinline__ bool claim_item(const PoolView& p, const BatchView& b
     entry_rows(b, i, lo, hi);
     const int64_t first = b.starts ? (int64_t)b.starts[i] / unit + 2 * (int64_t)i : i;
     const int64_t nth = item - first;
-    const int s = b.seqs[i], len = s >= 0 && s < p.max_seqs ? seq_len(p, s) : 0;
+    const int s = b.seqs[i];
+    const bool known = s >= 0 && s < p.max_seqs;
+    const int len = known ? seq_len(p, s) : 0, refused = want_twice && known && p.refused ? p.refused[s] : 0;
     // the bound of a run of items: those of the next entry begin behind rows / unit + 2 of this one's
     if (nth >= 0 && nth < (b.starts ? (hi - lo) / unit + 2 : 1) && hi > lo && atomicCAS(&c->entry, -1, i) == -1) {
       c->row0 = lo;
@@ -332,6 +344,7 @@ __device__ __forceinline__ bool claim_item(const PoolView& p, const BatchView& b
       c->nth = (int)nth;
       c->seq = s;
       c->len = len;
+      c->refused = refused;
     }
   }
   __syncthreads();
@@ -362,7 +375,7 @@ __global__ void __launch_bounds__(kAppendThreads, 3) kv_append_kernel(PoolView p
   const int s = own.seq, len = own.len;
   if (s < 0 || s >= p.max_seqs) return;
   const int64_t old = (int64_t)len - own.rows;     // tokens before this call
-  if (old < 0 || own.twice) {
+  if (old < 0 || own.twice || own.refused) {
     if (threadIdx.x == 0) atomicOr(err, ERR_PAGE);
     return;
   }

@@ -26,6 +26,7 @@ struct PoolView {
   int32_t* len;
   int32_t* refs;
   int32_t n_pages, page, max_seqs, max_pages;
+  int32_t* refused = nullptr;      // null: nothing is ever refused
 };
 struct CacheView {
   int8_t *k, *v;       // [n_pages][heads][page][dim]

@@ -60,3 +60,101 @@ def test_every_cause_surfaces(ctx):
     assert ctx.sync_status(side) == q.EPAGE
     ctx.check_sync()
     same_pool(pool, po)
+
+
+# ----------------------------------------------------------------------------- no room
+
+def contents(cache):
+    return [t.clone() for t in (cache.k, cache.v, cache.k_absmax, cache.v_absmax)]
+
+
+def unchanged(before, cache):
+    return all(torch.equal(a, b) for a, b in zip(before, contents(cache)))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_append_behind_a_refused_extend_writes_nothing(ctx, captured):
+    """extend, append without a look at the status in between: with too few pages the last tokens stay, and the step can be repeated."""
+    import paper_2302_01382_b200 as q
+    rng = np.random.default_rng(31)
+    pool, cache, po, co = make(ctx, 6, 16, 4, 4)
+    steps(ctx, pool, cache, po, co, [0, 1, 2], [32, 20, 16], torch.float32, rng)       # 5 of 6 pages
+    before = contents(cache)
+    seqs, shape = [0, 1, 2], (3, 2, 64)
+    k, v = (dev(50 * rng.standard_normal(shape).astype(np.float32)) for _ in range(2))
+    sd = ints(seqs)
+
+    def step():
+        pool.extend(sd)                            # two more pages: one too many
+        cache.append(k, v, sd)
+
+    if captured:
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        step = graph.replay
+    for _ in range(2):
+        step()
+        assert ctx.sync_status() == q.EPAGE and ctx.sync_status() == q.OK
+        assert unchanged(before, cache)
+        same_pool(pool, po)
+    # others go on meanwhile; a refused one stays out until it gets its room
+    pool.extend(ints([1]))
+    cache.append(k[1:2], v[1:2], ints([1]))
+    ctx.check_sync()
+    assert po.extend([1], [1])
+    co.append(host(k)[1:2], host(v)[1:2], [1], [0, 1])
+    same_cache(cache, co)
+    cache.append(k[:1], v[:1], ints([0]))
+    assert ctx.sync_status() == q.EPAGE
+    same_cache(cache, co)
+    pool.free(ints([1]))
+    po.free([1])
+    step()
+    ctx.check_sync()
+    assert po.extend(seqs, [1, 1, 1])
+    co.append(host(k), host(v), seqs, [0, 1, 2, 3])
+    same_pool(pool, po)
+    same_cache(cache, co)
+
+
+def test_room_of_other_calls_and_of_sequences_that_begin_again(ctx):
+    """A refused call keeps its own sequences out and no others; two calls may make the room of one append; a sequence that was given
+    back or forked begins anew."""
+    import paper_2302_01382_b200 as q
+    rng = np.random.default_rng(37)
+    pool, cache, po, co = make(ctx, 8, 16, 5, 3)
+    steps(ctx, pool, cache, po, co, [0, 1], [40, 10], torch.float32, rng)
+    x = rng.standard_normal((9, 2, 64)).astype(np.float32)
+    before = contents(cache)
+    pool.extend(ints([0, 2]), ints([0, 9, 9]))     # longer than a row of the table
+    pool.extend(ints([1]), ints([0, 4]))
+    pool.extend(ints([1]), ints([0, 5]))
+    cache.append(dev(x), dev(x), ints([0]), ints([0, 9]))
+    assert ctx.sync_status() == q.EPAGE
+    assert unchanged(before, cache) and pool.refused.tolist() == [1, 0, 1, 0, 0]
+    cache.append(dev(x), dev(x), ints([1]), ints([0, 9]))
+    assert po.extend([1], [4]) and po.extend([1], [5])
+    co.append(x, x, [1], [0, 9])
+    same_pool(pool, po)
+    same_cache(cache, co)
+    for twice in ([1, 1], [1, 5]):
+        pool.extend(ints(twice))
+        assert ctx.sync_status() == q.EPAGE and pool.refused.tolist() == [1, 1, 1, 0, 0]
+    pool.free(ints([0]))
+    po.free([0])
+    src, dst = pool.fork(ints([1]), ints([2]))
+    cache.copy_pages(src, dst)
+    co.copy_pages(*po.fork([1], [2]))
+    assert pool.refused.tolist() == [0, 1, 0, 0, 0]
+    steps(ctx, pool, cache, po, co, [2, 0, 1], [3, 4, 2], torch.float32, rng)
+    ctx.check_sync()
+    assert not pool.refused.any()
+    same_pool(pool, po)
+    same_cache(cache, co)
+    pool._c.refused_dev = None
+    with pytest.raises(q.QcfgError) as e:
+        pool.extend(ints([0]))
+    assert e.value.status == q.EINVAL
