@@ -38,6 +38,12 @@ constexpr int kSetup = 2;           // units
 constexpr int kRun = 32;            // tokens a warp takes at a time
 constexpr int kStreamWarps = 4;
 constexpr int kMinUnits = 2;        // a block takes at least this many
+// ref follows the running maximum only when a score passes it by more than `slack` binary orders, so that sums and accumulators are
+// rescaled a few times in a context and not at every new maximum; a weight stays below 2^15.  fp32 calls take most of fp16's room above 1
+// for the digits of small weights instead: a second half ends at 2^-25, and a weight is held times 2^13, so its 22 bits reach down to 2^-16
+// of the largest and what is lost of smaller ones is 2^-38 of it.  (Held as they are, 40000 tokens of weight 2^-21.5 gave a sum off by 1%.)
+template <bool WIDE> __host__ __device__ constexpr float weight_slack() { return WIDE ? 2.0f : 8.0f; }
+template <bool WIDE> __host__ __device__ constexpr float weight_unit() { return WIDE ? 8192.0f : 1.0f; }
 template <int DP> __host__ __device__ constexpr int stage_bytes() { return 2 * kRun * DP + 32; }             // keys, values, four maxima
 template <int DP, int NR> __host__ __device__ constexpr int stream_blocks() { return DP == 256 ? 1 : DP == 128 ? (NR == 4 ? 2 : 3) : NR == 1 ? 4 : NR == 2 ? 3 : 2; }    // per SM
 template <int DP, int NR> __host__ __device__ constexpr int stream_stages() { return DP == 256 ? 3 : DP == 128 ? (NR == 4 ? 3 : 2) : (NR == 1 ? 3 : 4); }
@@ -467,7 +473,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
         }
       float now = fmaxf(unit, fmaxf(vf[0], vf[1]));
       if (now > 0.0f) now = fmaxf(now, 1.2e-38f);
-      if (__any_sync(0xffffffffu, over > weight_bias<WIDE>() + kWeightSlack || now != unit) || fresh) {
+      if (__any_sync(0xffffffffu, over > weight_bias<WIDE>() + weight_slack<WIDE>() || now != unit) || fresh) {
         inv = now > 0.0f ? __fdiv_rn(1.0f, now) : 0.0f;
         const float change = unit * inv;
         unit = now;
@@ -501,7 +507,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
       uint32_t w_hi[2][NR][2], w_lo[WIDE ? 2 : 1][NR][2];
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const float share = vf[p] * inv;
+        const float share = vf[p] * inv * weight_unit<WIDE>();
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -573,7 +579,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
         for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, merge_top[w][r]);
         float factor = ref[n][z] == -INFINITY ? 0.0f : ex2(ref[n][z] - m);
         if (g == 0) merge_sum[warp][r] = sum[n][z] * factor;
-        factor *= unit;
+        factor *= unit * (1.0f / weight_unit<WIDE>());
         float* to = merged + (warp * ROWS + r) * PITCH;
 #pragma unroll
         for (int t = 0; t < MT; ++t) {

@@ -25,12 +25,10 @@ int launch_prompt(Ctx* ctx, const AttnArgs& a, int dtype, cudaStream_t st);
 
 namespace {
 
-// Weights are 2^(bias + x - ref).  ref follows the running maximum only when a score passes it by more than 2^8: sums and
-// accumulators are rescaled once or twice in a context and not at every new maximum, and a weight stays below 2^15.  The bias leaves
-// 16-bit calls seven more binary orders below the largest weight; fp32 calls hold a weight in two fp16 numbers and take none: an
-// exponent's rounding is relative to its size, which is small then for the weights that count.
+// Weights are 2^(bias + x - ref).  The bias leaves 16-bit calls seven more binary orders below the largest weight; fp32 calls hold a
+// weight in two fp16 numbers and take none: an exponent's rounding is relative to its size, which is small then for the weights that
+// count.
 template <bool WIDE> __host__ __device__ constexpr float weight_bias() { return WIDE ? 0.0f : 7.0f; }
-constexpr float kWeightSlack = 8.0f;
 
 // The tokens the row at position pos sees: [lo, hi), empty as hi <= lo.
 __device__ __forceinline__ void seen_range(const AttnArgs& a, int64_t pos, int len, int& lo, int& hi) {

@@ -158,3 +158,45 @@ def test_room_of_other_calls_and_of_sequences_that_begin_again(ctx):
     with pytest.raises(q.QcfgError) as e:
         pool.extend(ints([0]))
     assert e.value.status == q.EINVAL
+
+
+# ----------------------------------------------------------------------------- digits of the weights
+
+def lone_score(ctx, score, length, rows, heads, dtype, **kw):
+    """`length` tokens with values of 1, whose weights are all the same, next to one with a value of 0 whose score is `score` above theirs.
+    Returns the output and its exact value: errors of the many weights do not cancel."""
+    import paper_2302_01382_b200 as q
+    dim, page = 64, 64
+    pool = q.KvPool(ctx, -(-length // page) + 1, page, 1, -(-length // page) + 1)
+    cache = q.KvCache(pool, heads, dim)
+    k = torch.zeros((length, heads, dim), device="cuda")
+    v = torch.ones((length, heads, dim), device="cuda")
+    at = length // 3
+    k[at, :, 5], v[at] = 1.0, 0.0
+    seqs, st = ints([0]), ints([0, length])
+    pool.extend(seqs, st)
+    cache.append(k, v, seqs, st)
+    x = torch.zeros((rows, heads, dim), device="cuda")
+    x[:, :, 5] = score
+    out = cache.attention(x.to(dtype), seqs, ints([0, rows]), sm_scale=1.0, causal=False, **kw)
+    ctx.check_sync()
+    scale = np.float64(so.scales(np.float32(1))[0]) * 127
+    s = host(x.to(dtype))[0, 0, 5].astype(np.float64) * scale
+    rest = (length - 1) * np.exp(-s)
+    return host(out), scale * rest / (1 + rest), rest, s
+
+
+@pytest.mark.parametrize("score", [6.5, 9.2, 11.0, 12.7, 14.9])
+@pytest.mark.parametrize("rows,heads,max_len", [(1, 2, 0), (12, 2, 0), (1, 2, 512), (12, 2, 512), (300, 26, 0)])
+def test_fp32_weights_keep_their_digits_in_the_tail(ctx, score, rows, heads, max_len):
+    """The score: fp32 queries to 2^-22, three scalings; the exponential and its argument (up to 22 binary orders) 2^-20; a weight 2^-22, and
+    what lies below the fp16 grid 2^-38 of the largest.  Sums of positive numbers, each addition off by U or, in a tensor core, which cuts,
+    2 U.  A few rows stream over parts of up to 320 tokens by four warps: 2 x 5 products, 10 additions of weights and some 20 parts, below
+    100 U; a context that is not cut (the hint says it is short) gives a warp length / 4 tokens, 2 products for each 16 and an addition for
+    each 8.  A block that takes many rows walks the whole context, length / 16 products and length / 128 + 30 additions."""
+    length = 40000
+    out, want, rest, s = lone_score(ctx, score, length, rows, heads, torch.float32, max_new=rows, max_len=max_len)
+    adds = length / 8 + length / 128 + 30 if rows > 32 else 100 + (length / 4 * (4 / 16 + 1 / 8) if max_len else 0)
+    d_score = s * (2.0 ** -22 + 6 * U) + 2.0 ** -20
+    tol = want * (d_score / (1 + rest) + 2.0 ** -22 + adds * U) + length * 2.0 ** -38 / (1 + rest) + U
+    assert (np.abs(out - want) <= tol).all(), (float(np.abs(out - want).max()), tol)
