@@ -4,9 +4,9 @@
 // The codes go to the tensor cores as fp16, which holds them exactly, and never exist as numbers of 16 bits in memory: a page's
 // scale multiplies the finished scores (keys) or the weights (values).  Queries are fp16 after a power of two has brought
 // their row's largest element to 2^12 .. 2^13, so bf16 and fp16 ones lose nothing above 2^-38 of the row; fp32 ones are the sum
-// of two fp16 numbers.  Weights are e = 2^(7 + x - ref) times the page's share of the largest value scale seen, in fp16, with ref
-// at most 8 below the running maximum (fp32 calls: 2^(x - ref), the sum of two): 21 binary orders and more below the largest weight
-// before the fp16 grid coarsens.
+// of two fp16 numbers.  Weights are e = 2^(7 + x - ref) times their page's value scale, against
+// the largest such product the row has seen, in fp16 (fp32 calls: 2^(x - ref), the sum of two), with either reference at most 8 (6) below
+// the running maximum: 21 binary orders and more below the largest product before the fp16 grid coarsens.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -31,8 +31,8 @@ namespace {
 // In the A operand an element of K is (token, dimension), of V^T (dimension, token); the sums run over dimensions and
 // tokens in any order, so both are read 16 bytes at a time as they lie in memory.
 //
-// HBM bounds it, and close behind it the issue slots: 64 entries of one bf16 token over contexts of 8000, 32 heads on 8 of 128, 118 us;
-// one over 131000 tokens 57 us (both 4.7 TB/s, 72% of the measured copy rate, the second kernel's 5 us and the first's start included).
+// HBM bounds it, and close behind it the issue slots: 64 entries of one bf16 token over contexts of 8000, 32 heads on 8 of 128, 114 us;
+// one over 131000 tokens 56 us (4.9 and 4.8 TB/s, 74% of the measured copy rate, the second kernel's 5 us and the first's start included).
 constexpr int kUnit = 64;           // tokens
 constexpr int kSetup = 2;           // units
 constexpr int kRun = 32;            // tokens a warp takes at a time
@@ -40,10 +40,16 @@ constexpr int kStreamWarps = 4;
 constexpr int kMinUnits = 2;        // a block takes at least this many
 // ref follows the running maximum only when a score passes it by more than `slack` binary orders, so that sums and accumulators are
 // rescaled a few times in a context and not at every new maximum; a weight stays below 2^15.  fp32 calls take most of fp16's room above 1
-// for the digits of small weights instead: a second half ends at 2^-25, and a weight is held times 2^13, so its 22 bits reach down to 2^-16
-// of the largest and what is lost of smaller ones is 2^-38 of it.  (Held as they are, 40000 tokens of weight 2^-21.5 gave a sum off by 1%.)
-template <bool WIDE> __host__ __device__ constexpr float weight_slack() { return WIDE ? 2.0f : 8.0f; }
-template <bool WIDE> __host__ __device__ constexpr float weight_unit() { return WIDE ? 8192.0f : 1.0f; }
+// for the digits of small weights instead: a second half ends at 2^-25, and a weight is held times 2^9, so its 22 bits reach down to 2^-12
+// of the largest and what is lost of smaller ones is 2^-34 of it.  (Held as they are, 40000 tokens of weight 2^-21.5 gave a sum off by 1%.
+// 2^13 with 2 orders of slack: 32 entries of 16 tokens over 1000, 16 heads on 8 of 64, 48 -> 54 us, 52 this way: rows move too often.)
+template <bool WIDE> __host__ __device__ constexpr float weight_slack() { return WIDE ? 6.0f : 8.0f; }
+template <bool WIDE> __host__ __device__ constexpr int weight_order() { return WIDE ? 9 : 0; }
+// A row's weights are multiplied with their page's value scale times `low` = 2^(weight_order - d), which follows the row's largest such
+// product as ref follows its largest score: so what a row keeps depends on nothing but the tokens it sees, whatever the values of others
+// in its tile.  (One factor for the tile, the largest scale seen by any of its rows, cost causal rows in front of values 2^20 times
+// as large all their digits.)  In 16-bit calls the
+// product that sets d becomes a power of two, which fp16 holds as it is.
 template <int DP> __host__ __device__ constexpr int stage_bytes() { return 2 * kRun * DP + 32; }             // keys, values, four maxima
 template <int DP, int NR> __host__ __device__ constexpr int stream_blocks() { return DP == 256 ? 1 : DP == 128 ? (NR == 4 ? 2 : 3) : NR == 1 ? 4 : NR == 2 ? 3 : 2; }    // per SM
 template <int DP, int NR> __host__ __device__ constexpr int stream_stages() { return DP == 256 ? 3 : DP == 128 ? (NR == 4 ? 3 : 2) : (NR == 1 ? 3 : 4); }
@@ -151,6 +157,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
   __shared__ int64_t scan[kStreamWarps], found[2];
   __shared__ uint32_t magic_word;
   __shared__ float row_scale[ROWS], merge_top[kStreamWarps][ROWS], merge_sum[kStreamWarps][ROWS];
+  __shared__ __align__(16) float low_of[kStreamWarps][ROWS], d_of[kStreamWarps][ROWS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   const int group = a.q_heads / a.cache.heads, dim = a.cache.dim, page = a.pool.page;
   PartMeta* meta = reinterpret_cast<PartMeta*>(a.work);
@@ -312,7 +319,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
     const int run_hi = min(u1 * (kUnit / kRun), (any_hi + kRun - 1) / kRun);
     const int n_runs = run_hi - run_lo > warp ? (run_hi - run_lo - warp + kStreamWarps - 1) / kStreamWarps : 0;
 
-    float acc[MT][NR][4], ref[NR][2], sum[NR][2], unit = 0.0f, inv = 0.0f;
+    float acc[MT][NR][4], ref[NR][2], sum[NR][2];
+    int least = 0;                     // of the warp's rows: a bound of d
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       ref[n][0] = ref[n][1] = -INFINITY;
@@ -322,6 +330,14 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[m][n][j] = 0.0f;
     }
+    // `low` of the rows: in shared memory, read once a run (in registers they cost the forms of 16 rows and more 4 to 10% in spills)
+    float *low_row = low_of[warp] + 2 * t4, *d_row = d_of[warp] + 2 * t4;
+    if (lane < ROWS) {
+      low_of[warp][lane] = (float)(1 << weight_order<WIDE>());
+      d_of[warp][lane] = 0.0f;
+    }
+    float cap = 0.0f;                  // vf * low stays finite up to here; only tokens that no row sees can have more
+    __syncwarp();
 
     // pages of the next 32 runs: lane l holds those of run l of the window, for its first and second 16 tokens
     int pages[2] = {-1, -1}, window_at = -32;
@@ -429,8 +445,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
           }
         }
       }
-      // scales of the two tiles; a page of zeros must not set the unit, a maximum of -1 marks tokens that are not there
-      float kf[2], vf[2];
+      // scales of the two tiles, the values' with their binary logarithm; a maximum of -1 marks tokens that are not there
+      float kf[2], vf[2], lv[2];
       bool ok[2];
       {
         const uint4 w = lds128(stage + 2 * kRun * DP);
@@ -440,6 +456,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
           ok[p] = !(k_max[p] < 0.0f);
           kf[p] = ok[p] && k_max[p] > 0.0f ? k_max[p] * (1.0f / kQmax8) : 1.0f;      // the scale but for its last bit
           vf[p] = ok[p] ? v_max[p] * (1.0f / kQmax8) : 0.0f;
+          lv[p] = __log2f(fmaxf(vf[p], 1.2e-38f));
         }
       }
       if (tok < all_lo || tok + kRun > all_hi || !ok[0] || !ok[1]) {
@@ -471,25 +488,46 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
             }
           }
         }
-      float now = fmaxf(unit, fmaxf(vf[0], vf[1]));
-      if (now > 0.0f) now = fmaxf(now, 1.2e-38f);
-      if (__any_sync(0xffffffffu, over > weight_bias<WIDE>() + weight_slack<WIDE>() || now != unit) || fresh) {
-        inv = now > 0.0f ? __fdiv_rn(1.0f, now) : 0.0f;
-        const float change = unit * inv;
-        unit = now;
+      const float most = weight_bias<WIDE>() + weight_slack<WIDE>() - fmaxf(fmaxf(lv[0], lv[1]) - (float)least, 0.0f);
+      if (__any_sync(0xffffffffu, over > most) || fresh) {
         fresh = false;
+        least = 127;
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
+        for (int n = 0; n < NR; ++n) {
+          if (NR > 1) {                // eight rows at a time: mostly it is one row that has to move
+            over = ref[n][0] == -INFINITY || ref[n][1] == -INFINITY ? INFINITY : -INFINITY;
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) over = fmaxf(over, s[p][n][j]);
+            if (!__any_sync(0xffffffffu, over > most)) {
+              least = min(least, (int)floorf(fminf(d_row[8 * n], d_row[8 * n + 1])));
+              continue;
+            }
+          }
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
             const float was = ref[n][z] == -INFINITY ? 0.0f : ref[n][z];
-            float m = fmaxf(fmaxf(s[0][n][z], s[0][n][2 + z]), fmaxf(s[1][n][z], s[1][n][2 + z]));
+            const float m0 = fmaxf(s[0][n][z], s[0][n][2 + z]), m1 = fmaxf(s[1][n][z], s[1][n][2 + z]);
+            float m = fmaxf(m0, m1), v = fmaxf(m0 + lv[0], m1 + lv[1]);
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            for (int o = 4; o < 32; o <<= 1) {
+              m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+              v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+            }
             m = fmaxf(m - weight_bias<WIDE>() + was, ref[n][z]);
-            const float base = m == -INFINITY ? 0.0f : m;
-            const float keep = ex2(ref[n][z] - base);
+            v = v - weight_bias<WIDE>() + was;
+            const float base = m == -INFINITY ? 0.0f : m, d_was = d_row[8 * n + z], v_was = ref[n][z] + d_was;
+            float d = m == -INFINITY ? 0.0f : m == ref[n][z] && v <= v_was ? d_was : fminf(fmaxf(fmaxf(v, v_was) - m, -110.0f), 122.0f);
+            if (WIDE) d = ceilf(d);        // a whole number, so that sums and accumulators are rescaled alike to the last bit
+            const float keep = ex2(ref[n][z] - base), keep_values = keep * ex2(fminf(d_was - d, 126.0f));
             ref[n][z] = m;
+            __syncwarp();
+            if (g == 0) {
+              low_row[8 * n + z] = ex2(weight_order<WIDE>() - d);
+              d_row[8 * n + z] = d;
+            }
+            least = min(least, (int)floorf(d));
             fresh |= m == -INFINITY;
             sum[n][z] *= keep;
 #pragma unroll
@@ -498,28 +536,36 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
               for (int j = 0; j < 2; ++j) s[p][n][2 * j + z] += was - base;
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
-              acc[t][n][z] *= keep * change;
-              acc[t][n][2 + z] *= keep * change;
+              acc[t][n][z] *= keep_values;
+              acc[t][n][2 + z] *= keep_values;
             }
           }
+        }
         fresh = __any_sync(0xffffffffu, fresh);
+        least = __reduce_min_sync(0xffffffffu, least);
+        cap = exp2_of(min(126 - weight_order<WIDE>() + least, 127));
+        __syncwarp();
       }
+      float2 low2[NR];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) low2[n] = *reinterpret_cast<const float2*>(low_row + 8 * n);
       uint32_t w_hi[2][NR][2], w_lo[WIDE ? 2 : 1][NR][2];
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const float share = vf[p] * inv * weight_unit<WIDE>();
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
+        for (int n = 0; n < NR; ++n) {
+          const float share0 = fminf(vf[p], cap) * low2[n].x, share1 = fminf(vf[p], cap) * low2[n].y;
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const float e0 = ex2(s[p][n][2 * j]), e1 = ex2(s[p][n][2 * j + 1]);
             sum[n][0] += e0;
             sum[n][1] += e1;
-            const float w0 = e0 * share, w1 = e1 * share;
+            const float w0 = e0 * share0, w1 = e1 * share1;
             const __half2 h = __floats2half2_rn(w0, w1);
             w_hi[p][n][j] = transpose8(h2_bits(h));
             if (WIDE) w_lo[p][n][j] = transpose8(pack_h2(w0 - __low2float(h), w1 - __high2float(h)));
           }
+        }
       }
       // out^T: byte 2 m of a thread's elements is row g of tile m, byte 2 m + 1 row g + 8
 #pragma unroll
@@ -579,7 +625,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
         for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, merge_top[w][r]);
         float factor = ref[n][z] == -INFINITY ? 0.0f : ex2(ref[n][z] - m);
         if (g == 0) merge_sum[warp][r] = sum[n][z] * factor;
-        factor *= unit * (1.0f / weight_unit<WIDE>());
+        factor = __fdiv_rn(factor, low_row[8 * n + z]);
         float* to = merged + (warp * ROWS + r) * PITCH;
 #pragma unroll
         for (int t = 0; t < MT; ++t) {

@@ -14,12 +14,12 @@
 // What bounds it is neither but the chain of one tile: a step takes 4300 cycles, 2450 for a warp's 32 rows of weights (also where it
 // has its scheduler to itself), 350 until the tensor core knows of them, 1500 for the two products and the way back.  A block
 // costs 14000 cycles besides its steps (who it is, the queries, the first codes, the output).  4 entries of up to 2048 bf16 tokens behind up
-// to 4000, 32 heads on 8 of 128: 361 us, 849 TFLOP/s, 52% of the measured bf16 rate; 32 entries of up to 384 fp32 tokens, 12 heads of 64: 71 us.
+// to 4000, 32 heads on 8 of 128: 366 us, 837 TFLOP/s, 52% of the measured bf16 rate; 32 entries of up to 384 fp32 tokens, 12 heads of 64: 72 us.
 // Tried against 370 us then: scores, weights and products in halves of 64 tokens, so that a tile never waits (403: 48 MMAs a step in
 // place of 32, at 54 cycles each whatever their width), weights in halves only (398), a warp that issues for each tile (448: registers),
 // queries fetched before the TMEM is there (383: registers).
 // Numbers as in the streaming kernel: codes are exact in fp16, a page's key scale multiplies the scores' factor, its value scale the
-// weights, here against the largest value scale of the whole range (found before the first step), as a term of the exponent.
+// weights.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -48,7 +48,7 @@ template <int D, bool WIDE> __host__ __device__ constexpr int prompt_smem() {
 
 struct __align__(16) Scales {          // of a step
   float key[kGroups];    // -1: no such tokens
-  float log_share[kGroups], inv_share[kGroups];
+  float value[kGroups], log_value[kGroups], inv_value[kGroups];
 };
 
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -63,10 +63,6 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
                  "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]) : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
@@ -89,13 +85,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
   asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr bool WIDE = sizeof(T) == 4;
   constexpr int HALVES = D / 64, HALF = kTileRows * 128;              // bytes of 64 columns of a tile
+  constexpr int kUnitOrder = WIDE ? 4 : 0;                            // fp32 calls hold weights times 2^4
   constexpr uint32_t kCols = 512, kPart = WIDE ? 16 : 8;             // columns of the weights of 16 tokens (fp32: two fp16 numbers each)
   extern __shared__ uint8_t raw_smem[];
   __shared__ uint64_t bars[15];
   __shared__ uint32_t tmem_at, magic_word;
   __shared__ int abort_word;
   __shared__ struct { int64_t row0; int rows, nth, seq, len, claim; } mine;
-  __shared__ float unit_word, unit_parts[kConvWarps];
   __shared__ Scales scales[kTables];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group = a.q_heads / a.cache.heads, page = a.pool.page, item = blockIdx.x / a.cache.heads, hk = blockIdx.x - item * a.cache.heads;
@@ -237,22 +233,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     load_scales(next);
     load(a.cache.v, vc);
     next = look_up(1);
-    // the largest value scale of the range
-    float unit = 0.0f;
-    for (int64_t tok = tok_lo / page * page + (int64_t)(cw * 32 + lane) * page; tok < seen_hi && tok < len; tok += 32 * kConvWarps * page) {
-      const int p = __ldg(table + tok / page);
-      if (p >= 0 && p < a.pool.n_pages) unit = fmaxf(unit, __ldg(a.cache.v_absmax + (int64_t)p * a.cache.heads + hk));
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, o));
-    if (lane == 0) unit_parts[cw] = unit;
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * kConvWarps) : "memory");
-#pragma unroll
-    for (int w = 0; w < kConvWarps; ++w) unit = fmaxf(unit, unit_parts[w]);
-    unit *= 1.0f / kQmax8;
-    if (unit > 0.0f) unit = fmaxf(unit, 1.2e-38f);
-    if (tid == 32 * kSoftWarps) unit_word = unit;
-    const float inv_unit = unit > 0.0f ? __fdiv_rn(1.0f, unit) : 0.0f;
 
     for (int j = 0; j < steps; ++j) {
       const uint32_t st = j & 1, ph = (j >> 1) & 1;
@@ -263,10 +243,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
         const int g = lane;
         const bool ok = k_max >= 0.0f;
         sc.key[g] = !ok ? -1.0f : k_max > 0.0f ? k_max * (1.0f / kQmax8) : 1.0f;
-        // a page of zeros may have any weight
-        const float share = v_max > 0.0f ? fmaxf(v_max * (1.0f / kQmax8) * inv_unit, 8.7e-19f) : 1.0f;
-        sc.log_share[g] = log2f(share);
-        sc.inv_share[g] = __fdiv_rn(1.0f, share);
+        const float value = ok ? fmaxf(v_max * (1.0f / kQmax8), 1.2e-38f) : 1.2e-38f;       // (a page of zeros may have any)
+        sc.value[g] = value;
+        sc.log_value[g] = log2f(value);
+        sc.inv_value[g] = __fdiv_rn(1.0f, value);
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
@@ -410,6 +390,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t s_row = s_at + 128 * i + lanes, o_row = o_at + D * i + lanes, l_row = l_at + D * i + lanes;
     float ref = -INFINITY, sum = 0.0f;
+    // Weights are multiplied with their page's value scale times `low`, a power of two that follows the row's largest such product as
+    // ref follows its largest score (2^value_ref; low = the weights' unit times 2^(ref - value_ref)): so what a row keeps depends on
+    // nothing but the tokens it sees, whatever the values of others in the block.
+    float value_ref = -INFINITY, low = exp2_of(kUnitOrder);
     bool ok = true, fresh = true;      // fresh: no reference yet
     const int n = i == 0 || two ? steps : 0;
     for (int j = 0; j < n; ++j) {
@@ -418,12 +402,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       if (!mbar_wait_warp(s_full + 8 * i, j & 1, abort_flag, a.err)) { ok = false; break; }
       tc_fence_after();
       const Scales& sc = scales[j % kTables];
-      float f[kGroups], log_share[kGroups], inv_share[kGroups];
+      // fp32 calls multiply weights with their scale; others add its logarithm to the exponent and take it out of the sums of 16: 64
+      // products a step less (4 entries of 2048 tokens behind 4000, 32 heads on 8 of 128: 711 -> 684 us), for digits that 16 bits do not hold
+      float f[kGroups], value[kGroups], inv_value[WIDE ? 1 : kGroups];
 #pragma unroll
       for (int g = 0; g < kGroups; g += 4) {
         *reinterpret_cast<float4*>(f + g) = *reinterpret_cast<const float4*>(sc.key + g);
-        *reinterpret_cast<float4*>(log_share + g) = *reinterpret_cast<const float4*>(sc.log_share + g);
-        *reinterpret_cast<float4*>(inv_share + g) = *reinterpret_cast<const float4*>(sc.inv_share + g);
+        *reinterpret_cast<float4*>(value + g) = *reinterpret_cast<const float4*>((WIDE ? sc.value : sc.log_value) + g);
+        if constexpr (!WIDE) *reinterpret_cast<float4*>(inv_value + g) = *reinterpret_cast<const float4*>(sc.inv_value + g);
       }
       bool some = false;
 #pragma unroll
@@ -444,7 +430,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
       // when a row has none yet or a sum of 16 weights no longer fits fp16: what has been written and summed up is then scaled by a
       // power of two.  So no maximum is taken of most scores.
       constexpr int BLOCK = WIDE ? 1 : 4;
-      float part = 0.0f;             // of the step's unscaled exponentials
+      float part = 0.0f;             // of the step's exponentials
 #pragma unroll
       for (int b = 0; b < 4; b += BLOCK) {
         uint32_t p[2 * BLOCK][8], l[WIDE ? 2 : 1][WIDE ? 8 : 1];
@@ -452,6 +438,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
         bool large;
         auto take = [&]() {
           const float shift = weight_bias<WIDE>() - (ref == -INFINITY ? 0.0f : ref);
+          const float inv_low = __uint_as_float((254u << 23) - __float_as_uint(low)), log_low = shift + (float)((int)(__float_as_uint(low) >> 23) - 127);
           block_part = 0.0f;
           large = false;
           uint32_t v[2][32];
@@ -468,33 +455,42 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
             }
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
-              const float f1 = f[2 * c + z], at1 = shift + log_share[2 * c + z];
-              const float2 fg = make_float2(f1, f1), at = make_float2(at1, at1);
+              const float f1 = f[2 * c + z];
+              float at1 = shift, share1 = 1.0f;
+              if constexpr (WIDE) {
+                share1 = fminf(value[2 * c + z] * low, 8.5e37f);          // (tokens not seen may pass fp32)
+              } else {                       // never below 2^-100, so that the sums keep what the values lose
+                at1 = fmaxf(value[2 * c + z] + log_low, shift - 100.0f);
+                share1 = fminf(inv_value[2 * c + z] * inv_low, 0x1p100f);
+              }
+              const float2 fg = make_float2(f1, f1), at = make_float2(at1, at1), share = make_float2(share1, share1);
               float2 acc[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
               for (int k = 0; k < 8; ++k) {
                 const float2 x = __ffma2_rn(make_float2(__uint_as_float(x32[16 * z + 2 * k]), __uint_as_float(x32[16 * z + 2 * k + 1])), fg, at);
                 const float2 e = make_float2(ex2(x.x), ex2(x.y));
                 acc[k & 1] = __fadd2_rn(acc[k & 1], e);
-                const __half2 h = __floats2half2_rn(e.x, e.y);
+                const float2 w = WIDE ? __fmul2_rn(e, share) : e;
+                const __half2 h = __floats2half2_rn(w.x, w.y);
                 p[2 * (c - b) + z][k] = h2_bits(h);
                 if constexpr (WIDE) {
-                  const float2 rest = __fmul2_rn(__fadd2_rn(e, make_float2(-__low2float(h), -__high2float(h))), make_float2(kRest, kRest));
+                  const float2 rest = __fmul2_rn(__fadd2_rn(w, make_float2(-__low2float(h), -__high2float(h))), make_float2(kRest, kRest));
                   l[z][k] = pack_h2(rest.x, rest.y);
                 }
               }
               acc[0] = __fadd2_rn(acc[0], acc[1]);
               const float of16 = acc[0].x + acc[0].y;
-              large |= !(of16 <= 65504.0f);              // (a NaN counts; it stays one)
-              block_part = fmaf(of16, inv_share[2 * c + z], block_part);
+              large |= !((WIDE ? of16 * share1 : of16) <= 65504.0f);       // (a NaN counts; it stays one)
+              block_part = WIDE ? block_part + of16 : fmaf(of16, share1, block_part);
             }
           }
+          large |= !(block_part <= 0x1p40f);
         };
         bool move = fresh;                 // of the row's reference; written once, so that a step's code stays in the instruction cache and in registers
 #pragma unroll 1
         for (int go = 0; go < 2; ++go) {
           if (__any_sync(0xffffffffu, move)) {
-            float most = -INFINITY;
+            float most = -INFINITY, most_value = -INFINITY;
 #pragma unroll 1
             for (int g = 2 * b; g < 2 * (b + BLOCK); ++g) {
               uint32_t x[16];
@@ -504,27 +500,41 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
               float m = -INFINITY;
 #pragma unroll
               for (int k = 0; k < 16; ++k) m = fmaxf(m, seen & 1u << k ? __uint_as_float(x[k]) : -INFINITY);
-              most = fmaxf(most, m * fmaxf(row_f * sc.key[g], 1.2e-38f));
+              m *= fmaxf(row_f * sc.key[g], 1.2e-38f);
+              most = fmaxf(most, m);
+              most_value = fmaxf(most_value, m + (float)((int)(__float_as_uint(sc.value[g]) >> 23) - 126));      // the order the scale does not reach
             }
-            const float was = ref;
-            if (move) ref = fmaxf(ref, ceilf(most));
+            const float was = ref, value_was = value_ref;
+            if (move) {
+              ref = fmaxf(ref, ceilf(most));
+              value_ref = fmaxf(value_ref, ceilf(most_value));
+            }
             fresh = ref == -INFINITY;
-            const float keep = ex2(was - (fresh ? 0.0f : ref));
-            if (__any_sync(0xffffffffu, keep != 1.0f)) {
+            if (!fresh) {
+              value_ref = fmaxf(value_ref, ref - 110.0f);
+              low = exp2_of(kUnitOrder - (int)(value_ref - ref));
+            }
+            const float keep = ex2(was - (fresh ? 0.0f : ref)), keep_values = ex2(value_was - (fresh ? 0.0f : value_ref));
+            if (__any_sync(0xffffffffu, keep != 1.0f || keep_values != 1.0f)) {
               sum *= keep;
               part *= keep;
-              if (b > 0) tmem_st_wait();       // loads are not ordered behind stores that have not been waited for
+              if constexpr (WIDE) {            // this step's weights so far: both halves as one number, halved anew behind the factor
+                if (b > 0) tmem_st_wait();     // loads are not ordered behind stores that have not been waited for
 #pragma unroll 1
-              for (int h = 0; h < (int)kPart / 8 * 2 * b; ++h) {
-                uint32_t w[8];
-                tmem_ld8(s_row + 8 * h, w);
-                tmem_ld_wait();
+                for (int h = 0; h < 2 * b; ++h) {
+                  uint32_t w[16];
+                  tmem_ld16(s_row + 16 * h, w);
+                  tmem_ld_wait();
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {      // (the factor itself may be too small for fp16)
-                  const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
-                  w[k] = pack_h2(e.x * keep, e.y * keep);
+                  for (int k = 0; k < 8; ++k) {
+                    const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&w[k])), r = __half22float2(*reinterpret_cast<const __half2*>(&w[8 + k]));
+                    const float x = fmaf(r.x, 1.0f / kRest, e.x) * keep_values, y = fmaf(r.y, 1.0f / kRest, e.y) * keep_values;
+                    const __half2 hi = __floats2half2_rn(x, y);
+                    w[k] = h2_bits(hi);
+                    w[8 + k] = pack_h2((x - __low2float(hi)) * kRest, (y - __high2float(hi)) * kRest);
+                  }
+                  tmem_st16(s_row + 16 * h, w);
                 }
-                tmem_st8(s_row + 8 * h, w);
               }
               // the products so far have been completed in front of these scores
 #pragma unroll 1
@@ -534,7 +544,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
                 tmem_ld16(at, w);
                 tmem_ld_wait();
 #pragma unroll
-                for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * keep);
+                for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * keep_values);
                 tmem_st16(at, w);
               }
               tmem_st_wait();
@@ -562,7 +572,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     if (ok && (i == 0 || two)) {
       tc_fence_after();
       float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : (sum == 0.0f ? 0.0f : sum);
-      if (n > 0) inv *= unit_word;
+      inv *= __uint_as_float((254u << 23) - __float_as_uint(low));      // its inverse: a power of two
       // through the tile's queries, which nobody reads any more: a warp's 32 rows of D elements
       const uint32_t stage = q_sm + i * q_tile_bytes<D, WIDE>() + (warp & 3) * 32 * D * (int)sizeof(T);
 #pragma unroll

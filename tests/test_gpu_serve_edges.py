@@ -190,13 +190,74 @@ def lone_score(ctx, score, length, rows, heads, dtype, **kw):
 @pytest.mark.parametrize("rows,heads,max_len", [(1, 2, 0), (12, 2, 0), (1, 2, 512), (12, 2, 512), (300, 26, 0)])
 def test_fp32_weights_keep_their_digits_in_the_tail(ctx, score, rows, heads, max_len):
     """The score: fp32 queries to 2^-22, three scalings; the exponential and its argument (up to 22 binary orders) 2^-20; a weight 2^-22, and
-    what lies below the fp16 grid 2^-38 of the largest.  Sums of positive numbers, each addition off by U or, in a tensor core, which cuts,
-    2 U.  A few rows stream over parts of up to 320 tokens by four warps: 2 x 5 products, 10 additions of weights and some 20 parts, below
-    100 U; a context that is not cut (the hint says it is short) gives a warp length / 4 tokens, 2 products for each 16 and an addition for
-    each 8.  A block that takes many rows walks the whole context, length / 16 products and length / 128 + 30 additions."""
+    what lies below the fp16 grid 2^-34 of the largest.  Sums of positive numbers, each addition off by U or, in a tensor core, which cuts,
+    2 U, and a product of 16 tokens is 16 additions.  A few rows stream over parts of up to 320 tokens by four warps: two halves of 80
+    tokens, 10 additions of weights and some 20 parts, below 400 U; a context that is not cut (the hint says it is short) gives a warp
+    length / 4 tokens, two halves each, and an addition of weights for each 8.  A block that takes many rows walks the whole context, an
+    addition for each token and length / 128 + 30 of weights."""
     length = 40000
     out, want, rest, s = lone_score(ctx, score, length, rows, heads, torch.float32, max_new=rows, max_len=max_len)
-    adds = length / 8 + length / 128 + 30 if rows > 32 else 100 + (length / 4 * (4 / 16 + 1 / 8) if max_len else 0)
+    adds = 2 * length + length / 128 + 30 if rows > 32 else 400 + (length / 4 * (4 + 1 / 8) if max_len else 0)
     d_score = s * (2.0 ** -22 + 6 * U) + 2.0 ** -20
-    tol = want * (d_score / (1 + rest) + 2.0 ** -22 + adds * U) + length * 2.0 ** -38 / (1 + rest) + U
+    tol = want * (d_score / (1 + rest) + 2.0 ** -22 + adds * U) + length * 2.0 ** -34 / (1 + rest) + U
     assert (np.abs(out - want) <= tol).all(), (float(np.abs(out - want).max()), tol)
+
+
+def seen_bound(q, k, v, page, sm_scale, causal, window, dtype):
+    """Oracle and |error| with nothing in it but the tokens a row sees.  As attention_bound, with this for weights below the fp16 grid: a
+    product of weight and page scale is off by 2^-25 where the row's largest is 2^5 or more (in fp32 calls 2^-25 next to 2^8 where all are held
+    times 2^9, 2^-35 next to 2^2 where the second halves are held times 2^10 besides); codes are at most 127 of a page's scale, and the weights of all tokens add up."""
+    rows, q_heads, dim = q.shape
+    length, heads, _ = k.shape
+    out, weight, spread = so.attention(q, k, v, sm_scale, causal, window)
+    mask = so.seen(rows, length, causal, window)
+    pages = np.arange(length) // page
+    tops = np.stack([np.abs(v[pages == j]).max((0, 2)) for j in range(pages[-1] + 1)])[pages]      # [length, heads]: at most the page's maximum
+    tol = np.zeros(q.shape)
+    for h in range(q_heads):
+        kh, top = k[:, h // (q_heads // heads)], tops[:, h // (q_heads // heads)]
+        s = np.where(mask, q[:, h].astype(np.float64) @ kh.T * sm_scale, -np.inf)
+        some = mask.any(1)
+        p = np.where(mask, np.exp(s - np.where(some, s.max(1), 0)[:, None]), 0)
+        p /= np.where(some, p.sum(1), 1)[:, None]
+        largest = (p * top[None, :]).max(1)
+        # the largest element of the keys a row sees, times the query's: what queries of 16 bits in fp16 lose
+        biggest = np.abs(q[:, h]).max(1) * np.where(mask, np.abs(kh).sum(1)[None, :], 0).max(1) * sm_scale
+        score = (dim + 6) * U * spread[:, h] + 2.0 ** -22 * (spread[:, h] + biggest) + 2.0 ** -21
+        rel = 2 * np.expm1(score) + (2.0 ** -11 if dtype != torch.float32 else 2.0 ** -20) + (length + 8) * U
+        tol[:, h] = rel[:, None] * weight[:, h] + (mask.sum(1) * largest * 2.0 ** (-30 if dtype != torch.float32 else -33))[:, None]
+    return out, tol + half_step(dtype) * np.abs(out) + (2.0 ** -25 if dtype == torch.float16 else 1e-38)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 10, 1e6, 1e12, 1e30])
+@pytest.mark.parametrize("page,q_heads,heads,dim", [(16, 4, 2, 64), (32, 8, 1, 128), (16, 3, 3, 80), (64, 26, 26, 64), (16, 32, 8, 128)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_row_does_not_depend_on_values_it_does_not_see(ctx, dtype, page, q_heads, heads, dim, size):
+    """Values far larger than the others come later (causal rows in front of them) and came earlier (a window has left them): to a row that
+    does not see them they are nothing, though it shares tiles with rows that do."""
+    rng = np.random.default_rng(page + dim)
+    pool, cache, po, co = make(ctx, 600 // page + 8, page, 2, 512 // page + 2, heads, dim)
+    one = torch.float32
+    steps(ctx, pool, cache, po, co, [0], [2 * page], one, rng, spread=size)
+    steps(ctx, pool, cache, po, co, [0], [256 - 2 * page], one, rng)
+    steps(ctx, pool, cache, po, co, [0], [11], one, rng, spread=size)
+    # one whose first page is as the others
+    steps(ctx, pool, cache, po, co, [1], [256 - page], one, rng)
+    steps(ctx, pool, cache, po, co, [1], [9], one, rng, spread=size)
+    # the keys stay as they are: their size is not the question here
+    cache.k_absmax.clamp_(max=4.0)
+    co.absmax[0] = np.minimum(co.absmax[0], np.float32(4))
+    ctx.check_sync()
+    for seqs, rows, kw in (([1], [12], {}), ([1], [20], {"max_len": 300}), ([1], [po.lens[1]], {"max_new": po.lens[1]}), ([0], [40], {"window": 100}),
+                           ([0], [po.lens[0]], {"window": 3 * page + 5, "max_new": po.lens[0]}), ([0, 1], [267, 249 - page], {"max_new": 267, "window": 24})):
+        x = dev((rng.standard_normal((sum(rows), q_heads, dim))).astype(np.float32), dtype)
+        got = host(cache.attention(x, ints(seqs), ints(starts_of(rows)), **kw))
+        at = 0
+        for s, c in zip(seqs, rows):
+            k, v = co.values(s)
+            want, tol = seen_bound(host(x)[at:at + c], k, v, page, dim ** -0.5, True, kw.get("window", 0), dtype)
+            ok = np.abs(want) + tol < torch.finfo(dtype).max         # (what the bound lets pass the type's end may be Inf)
+            worst = np.where(ok, np.abs(got[at:at + c] - want) - tol, 0)
+            assert (worst <= 0).all(), (s, c, kw, float(worst.max()), np.argwhere(worst > 0)[:4].tolist(), len(np.argwhere(worst > 0)))
+            at += c
+    ctx.check_sync()
