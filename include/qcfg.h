@@ -303,10 +303,11 @@ typedef struct qcfg_kv_cache {
 /* Which sequences a call is about and which rows of its tensors are theirs.  Entry i stands for
  * sequence seqs_dev[i] (a row of the table; -1: an entry without one, for padded batches) and rows
  * starts_dev[i] .. starts_dev[i+1]-1 of n_rows; starts_dev == NULL: one row each.  Rows behind the last
- * entry's belong to nobody: they are neither read nor written.                                 */
+ * entry's belong to nobody: they are neither read nor written.  An entry whose rows are not among the n_rows is left
+ * out (QCFG_EPAGE).                                                                            */
 typedef struct qcfg_kv_batch {
   const int32_t* seqs_dev;     /* [n]                                                          */
-  const int32_t* starts_dev;   /* [n+1], ascending, or NULL                                    */
+  const int32_t* starts_dev;   /* [n+1], ascending, 0 .. n_rows, or NULL                       */
   int32_t n;
   int64_t n_rows;
 } qcfg_kv_batch;

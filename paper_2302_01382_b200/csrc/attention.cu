@@ -118,7 +118,7 @@ template <int NR>
 __device__ __forceinline__ Entry entry_of(const AttnArgs& a, int i) {
   Entry e;
   int64_t hi;
-  entry_rows(a.batch, i, e.row0, hi);
+  if (!entry_rows(a.batch, i, e.row0, hi)) atomicOr(a.err, ERR_PAGE);
   e.rows = hi - e.row0;
   e.s = a.batch.seqs[i];
   e.len = e.s < 0 || e.s >= a.pool.max_seqs ? 0 : seq_len(a.pool, e.s);

@@ -81,11 +81,10 @@ __global__ void __launch_bounds__(kPlanThreads) kv_extend_kernel(PoolView p, Bat
   __syncthreads();
   for (int i = threadIdx.x; i < b.n; i += kPlanThreads) {
     int64_t lo, hi;
-    entry_rows(b, i, lo, hi);
     const int s = b.seqs[i];
     need[i] = 0;
     grown[i] = -1;
-    if (s >= p.max_seqs) bad = 1;
+    if (!entry_rows(b, i, lo, hi) || s >= p.max_seqs) bad = 1;
     if (s < 0 || s >= p.max_seqs) continue;
     const int old = (int)atomicOr(reinterpret_cast<unsigned*>(p.len) + s, kMark);
     if (old < 0) { bad = 1; continue; }
@@ -331,7 +330,7 @@ __device__ __forceinline__ bool claim_item(const PoolView& p, const BatchView& b
     const int i = i0 + threadIdx.x;
     if (i >= b.n) break;
     int64_t lo, hi;
-    entry_rows(b, i, lo, hi);
+    if (!entry_rows(b, i, lo, hi)) atomicOr(err, ERR_PAGE);
     const int64_t first = b.starts ? (int64_t)b.starts[i] / unit + 2 * (int64_t)i : i;
     const int64_t nth = item - first;
     const int s = b.seqs[i];

@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
     const int i = i0 + tid;
     if (i < a.batch.n) {
       int64_t r0, r1;
-      entry_rows(a.batch, i, r0, r1);
+      if (!entry_rows(a.batch, i, r0, r1)) atomicOr(a.err, ERR_PAGE);
       const int q = entry_seq(a.batch, a.pool, i, a.err), held = q < 0 ? 0 : seq_len(a.pool, q);
       const int64_t nth = item - (a.batch.starts ? (int64_t)a.batch.starts[i] / per_block + i : 2 * (int64_t)i);
       if (nth >= 0 && nth < (r1 - r0 + per_block - 1) / per_block && atomicCAS(&mine.claim, -1, i) == -1) {      // one at most, where starts ascend

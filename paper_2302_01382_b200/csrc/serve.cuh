@@ -116,8 +116,8 @@ __device__ __forceinline__ void load_vec(const T* p, float (&f)[Vec<T>::N]) {
   for (int i = 0; i < Vec<T>::N; ++i) f[i] = to_float<T>(w.t[i]);
 }
 
-// Rows [lo, hi) of entry i, cut to what the tensors have.
-__device__ __forceinline__ void entry_rows(const BatchView& b, int i, int64_t& lo, int64_t& hi) {
+// Rows [lo, hi) of entry i.  False: they are not rows of the tensors, or end before they begin; then there are none.
+__device__ __forceinline__ bool entry_rows(const BatchView& b, int i, int64_t& lo, int64_t& hi) {
   if (b.starts) {
     lo = b.starts[i];
     hi = b.starts[i + 1];
@@ -125,8 +125,9 @@ __device__ __forceinline__ void entry_rows(const BatchView& b, int i, int64_t& l
     lo = i;
     hi = i + 1;
   }
-  lo = lo < 0 ? 0 : (lo > b.rows ? b.rows : lo);
-  hi = hi < lo ? lo : (hi > b.rows ? b.rows : hi);
+  const bool ok = lo >= 0 && lo <= hi && hi <= b.rows;
+  if (!ok) lo = hi = 0;
+  return ok;
 }
 // The table row of entry i, or -1 (none; out of range: reported)
 __device__ __forceinline__ int entry_seq(const BatchView& b, const PoolView& p, int i, unsigned* err) {

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import serve_oracle as so
-from test_gpu_serve import ACTS, DTYPES, U, check_attention, code_weights, ctx, dev, half_step, host, ints, linear_bound, make, same_cache, same_pool, starts_of, steps  # noqa: F401
+from test_gpu_serve import ACTS, DTYPES, U, attention_bound, code_weights, ctx, dev, half_step, host, ints, linear_bound, make, same_cache, same_pool, starts_of, steps  # noqa: F401
 from test_gpu_serve import test_linear as linear_against_oracle
 
 pytestmark = pytest.mark.gpu
@@ -261,3 +261,46 @@ def test_a_row_does_not_depend_on_values_it_does_not_see(ctx, dtype, page, q_hea
             assert (worst <= 0).all(), (s, c, kw, float(worst.max()), np.argwhere(worst > 0)[:4].tolist(), len(np.argwhere(worst > 0)))
             at += c
     ctx.check_sync()
+
+
+# ----------------------------------------------------------------------------- rows out of range
+
+@pytest.mark.parametrize("starts", [[0, 2, 7], [0, 2, 1], [-1, 2, 4], [0, 2, -3]])
+def test_entries_whose_rows_are_not_there_are_left_out(ctx, starts):
+    """Rows behind the tensors' end, before their begin, or that end before they begin: reported, not cut to what is there; the entry
+    beside them is served (but for extend, which is all or nothing)."""
+    import paper_2302_01382_b200 as q
+    rng = np.random.default_rng(43)
+    for dtype, heads, many in ((torch.float32, 2, 1), (torch.bfloat16, 2, 1), (torch.float16, 26, 100)):
+        pool, cache, po, co = make(ctx, 40, 16, 3, 16, heads, 64)
+        steps(ctx, pool, cache, po, co, [0, 1], [20 * many % 240, 37], torch.float32, rng)
+        good, bad = [], []
+        for i in range(2):
+            lo, hi = starts[i], starts[i + 1]
+            (good if 0 <= lo <= hi <= 4 else bad).append(i)
+        assert bad
+        st, n = ints([s * many for s in starts]), 4 * many
+        before = contents(cache)
+        pool.extend(ints([0, 1]), st, rows=n)
+        assert ctx.sync_status() == q.EPAGE
+        same_pool(pool, po)
+        pool.refused.zero_()
+        x = dev(rng.standard_normal((n, heads, 64)).astype(np.float32), dtype)
+        out = torch.full((n, heads, 64), 9.0, dtype=dtype, device="cuda")
+        cache.attention(x, ints([0, 1]), st, out=out, max_new=many * 2)
+        assert ctx.sync_status() == q.EPAGE
+        for i in good:
+            rows = slice(many * starts[i], many * starts[i + 1])
+            want, tol = attention_bound(host(x[rows]), *co.values(i), 64 ** -0.5, True, 0, dtype)
+            assert (np.abs(host(out[rows]) - want) <= tol).all()
+            out[rows] = 9
+        assert (out == 9).all()                        # nobody's rows are not written
+        if many == 1:
+            cache.append(x, x, ints([0, 1]), st)
+            assert ctx.sync_status() == q.EPAGE
+            for i in bad:
+                for a, b in zip(before, contents(cache)):
+                    for page in po.table[i]:
+                        assert torch.equal(a[page], b[page])
+        k, v = cache.read(ints([0, 1]), ints([0, 0]), st, n)
+        assert ctx.sync_status() == q.EPAGE
