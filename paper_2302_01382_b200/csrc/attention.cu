@@ -118,7 +118,7 @@ template <int NR>
 __device__ __forceinline__ Entry entry_of(const AttnArgs& a, int i) {
   Entry e;
   int64_t hi;
-  if (!entry_rows(a.batch, i, e.row0, hi)) atomicOr(a.err, ERR_PAGE);
+  entry_rows(a.batch, i, e.row0, hi);
   e.rows = hi - e.row0;
   e.s = a.batch.seqs[i];
   e.len = e.s < 0 || e.s >= a.pool.max_seqs ? 0 : seq_len(a.pool, e.s);
@@ -167,6 +167,11 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
 
   // ---- this block's share: the sum over all entries, then the entry its first unit lies in
   auto units_of = [&](int i) { return i < a.batch.n ? entry_units(a, entry_of<NR>(a, i)) : (int64_t)0; };
+  if (blockIdx.x == gridDim.x - 1)         // (the others would report the same)
+    for (int i = tid; i < a.batch.n; i += 32 * kStreamWarps) {
+      int64_t lo, hi;
+      if (!entry_rows(a.batch, i, lo, hi)) atomicOr(a.err, ERR_PAGE);
+    }
   // inclusive sums over the block's threads; `sum` gets the total
   auto scan_units = [&](int64_t u, int64_t& sum) {
 #pragma unroll
@@ -320,7 +325,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
     const int n_runs = run_hi - run_lo > warp ? (run_hi - run_lo - warp + kStreamWarps - 1) / kStreamWarps : 0;
 
     float acc[MT][NR][4], ref[NR][2], sum[NR][2];
-    int least = 0;                     // of the warp's rows: a bound of d
+    float least = 0.0f;                // of the warp's rows: a bound of d
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       ref[n][0] = ref[n][1] = -INFINITY;
@@ -330,12 +335,13 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[m][n][j] = 0.0f;
     }
-    // `low` of the rows: in shared memory, read once a run (in registers they cost the forms of 16 rows and more 4 to 10% in spills)
+    // `low` of the rows: in shared memory, read once a run (in registers, where one for 8 rows is, they cost the forms of more rows 4 to 10% in spills)
     float *low_row = low_of[warp] + 2 * t4, *d_row = d_of[warp] + 2 * t4;
     if (lane < ROWS) {
       low_of[warp][lane] = (float)(1 << weight_order<WIDE>());
       d_of[warp][lane] = 0.0f;
     }
+    float2 low_here = make_float2(0.0f, 0.0f);      // (NR = 1)
     float cap = 0.0f;                  // vf * low stays finite up to here; only tokens that no row sees can have more
     __syncwarp();
 
@@ -456,7 +462,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
           ok[p] = !(k_max[p] < 0.0f);
           kf[p] = ok[p] && k_max[p] > 0.0f ? k_max[p] * (1.0f / kQmax8) : 1.0f;      // the scale but for its last bit
           vf[p] = ok[p] ? v_max[p] * (1.0f / kQmax8) : 0.0f;
-          lv[p] = __log2f(fmaxf(vf[p], 1.2e-38f));
+          lv[p] = lg2(fmaxf(vf[p], 1.2e-38f));
         }
       }
       if (tok < all_lo || tok + kRun > all_hi || !ok[0] || !ok[1]) {
@@ -488,10 +494,10 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
             }
           }
         }
-      const float most = weight_bias<WIDE>() + weight_slack<WIDE>() - fmaxf(fmaxf(lv[0], lv[1]) - (float)least, 0.0f);
+      const float most = weight_bias<WIDE>() + weight_slack<WIDE>() - fmaxf(fmaxf(lv[0], lv[1]) - least, 0.0f);
       if (__any_sync(0xffffffffu, over > most) || fresh) {
         fresh = false;
-        least = 127;
+        least = 127.0f;
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
           if (NR > 1) {                // eight rows at a time: mostly it is one row that has to move
@@ -501,7 +507,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
 #pragma unroll
               for (int j = 0; j < 4; ++j) over = fmaxf(over, s[p][n][j]);
             if (!__any_sync(0xffffffffu, over > most)) {
-              least = min(least, (int)floorf(fminf(d_row[8 * n], d_row[8 * n + 1])));
+              least = fminf(least, fminf(d_row[8 * n], d_row[8 * n + 1]));
               continue;
             }
           }
@@ -520,14 +526,15 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
             const float base = m == -INFINITY ? 0.0f : m, d_was = d_row[8 * n + z], v_was = ref[n][z] + d_was;
             float d = m == -INFINITY ? 0.0f : m == ref[n][z] && v <= v_was ? d_was : fminf(fmaxf(fmaxf(v, v_was) - m, -110.0f), 122.0f);
             if (WIDE) d = ceilf(d);        // a whole number, so that sums and accumulators are rescaled alike to the last bit
-            const float keep = ex2(ref[n][z] - base), keep_values = keep * ex2(fminf(d_was - d, 126.0f));
+            const float keep = ex2(ref[n][z] - base), keep_values = keep * ex2(fminf(d_was - d, 126.0f)), low = ex2(weight_order<WIDE>() - d);
             ref[n][z] = m;
             __syncwarp();
             if (g == 0) {
-              low_row[8 * n + z] = ex2(weight_order<WIDE>() - d);
+              low_row[8 * n + z] = low;
               d_row[8 * n + z] = d;
             }
-            least = min(least, (int)floorf(d));
+            if (NR == 1) (z ? low_here.y : low_here.x) = low;
+            least = fminf(least, d);
             fresh |= m == -INFINITY;
             sum[n][z] *= keep;
 #pragma unroll
@@ -542,13 +549,13 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
           }
         }
         fresh = __any_sync(0xffffffffu, fresh);
-        least = __reduce_min_sync(0xffffffffu, least);
-        cap = exp2_of(min(126 - weight_order<WIDE>() + least, 127));
+        least = (float)__reduce_min_sync(0xffffffffu, (int)floorf(least));
+        cap = exp2_of(min(126 - weight_order<WIDE>() + (int)least, 127));
         __syncwarp();
       }
       float2 low2[NR];
 #pragma unroll
-      for (int n = 0; n < NR; ++n) low2[n] = *reinterpret_cast<const float2*>(low_row + 8 * n);
+      for (int n = 0; n < NR; ++n) low2[n] = NR > 1 ? *reinterpret_cast<const float2*>(low_row + 8 * n) : low_here;
       uint32_t w_hi[2][NR][2], w_lo[WIDE ? 2 : 1][NR][2];
 #pragma unroll
       for (int p = 0; p < 2; ++p) {

@@ -43,6 +43,11 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // Two bytes of a word of codes plus 128 as fp16 codes: 0x6400 + b is 1024 + b.  `magic` is 0x64646464, read from shared memory once: a
 // constant the compiler knows it keeps in a uniform register and copies anew in front of almost every permutation, 118 of a run's
 // 870 instructions in the streaming kernel.

@@ -453,15 +453,21 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
 #pragma unroll
               for (int k = 0; k < 32; ++k) x32[k] = seen & 1u << k ? x32[k] : 0xff800000u;
             }
+            float2 both_at, both_share;
+            if constexpr (!WIDE) {
+              both_at = __fadd2_rn(make_float2(value[2 * c], value[2 * c + 1]), make_float2(log_low, log_low));
+              both_share = __fmul2_rn(make_float2(inv_value[2 * c], inv_value[2 * c + 1]), make_float2(inv_low, inv_low));
+            }
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
               const float f1 = f[2 * c + z];
-              float at1 = shift, share1 = 1.0f;
+              float at1, share1;
               if constexpr (WIDE) {
+                at1 = shift;
                 share1 = fminf(value[2 * c + z] * low, 8.5e37f);          // (tokens not seen may pass fp32)
               } else {                       // never below 2^-100, so that the sums keep what the values lose
-                at1 = fmaxf(value[2 * c + z] + log_low, shift - 100.0f);
-                share1 = fminf(inv_value[2 * c + z] * inv_low, 0x1p100f);
+                at1 = fmaxf(z ? both_at.y : both_at.x, shift - 100.0f);
+                share1 = fminf(z ? both_share.y : both_share.x, 0x1p100f);
               }
               const float2 fg = make_float2(f1, f1), at = make_float2(at1, at1), share = make_float2(share1, share1);
               float2 acc[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
