@@ -343,7 +343,8 @@ int qcfg_kv_copy_pages(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_ca
  * where new ones raise it, the codes before them become round_half_even(code * (old / new))
  * (one fp32 division, one product); a page that begins with a new token forgets what it held.
  * NaN and Inf are held as 0, do not count for the maximum and surface as QCFG_ENONFINITE.  k_dev, v_dev: [n_rows] rows of
- * `dtype`, row and head strides in elements, 16-byte aligned pointers and strides (QCFG_EALIGN).
+ * `dtype`, row and head strides in elements, 16-byte aligned pointers and strides (QCFG_EALIGN; strides of a single
+ * row or head do not matter).
  * Pages that several sequences hold are not written, nor is a sequence listed twice or one whose last
  * qcfg_kv_extend was refused (QCFG_EPAGE from qcfg_sync_status).                               */
 int qcfg_kv_append(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* cache, const qcfg_kv_batch* batch, const void* k_dev,
@@ -360,7 +361,7 @@ int qcfg_kv_read(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* c
  * must be 0).  out = softmax(sm_scale * q k^T) v over what it sees; a row that sees nothing (p < 0, an
  * empty sequence, an entry without one) gives zeros.  q_dev, out_dev: [n_rows] rows of
  * `dtype` with q_heads heads of head_dim elements, strides in elements, 16-byte aligned pointers and
- * strides (QCFG_EALIGN); head h reads cache head h / (q_heads / kv_heads).  out_dev must not
+ * strides (QCFG_EALIGN; those of a single row or head do not matter); head h reads cache head h / (q_heads / kv_heads).  out_dev must not
  * overlap q_dev.  A query with a NaN or Inf gives NaN where it sees something.  Sums, maxima and accumulators are fp32.
  * A row depends on nothing but the tokens it sees.  Of these, weights times page scales are held to 11 bits (22 in fp32 calls), and
  * to 2^-30 (2^-34) of the row's largest such product.

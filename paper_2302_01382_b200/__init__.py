@@ -421,7 +421,7 @@ def _output(out, shape, dtype, device, stream):
     if out is None:
         _dtype(dtype)
         return _empty(shape, dtype, device, stream)
-    if tuple(out.shape) != tuple(shape) or out.stride(-1) != 1:
+    if tuple(out.shape) != tuple(shape) or (out.shape[-1] > 1 and out.stride(-1) != 1):
         raise QcfgError(ESHAPE, f"out must be {tuple(shape)} with adjacent columns")
     return out
 
@@ -527,7 +527,7 @@ class KvCache:
         self._heads_of(k, self.kv_heads)
         self._heads_of(v, self.kv_heads)
         strides = k.stride()
-        if k.shape != v.shape or k.dtype != v.dtype or strides != v.stride():
+        if k.shape != v.shape or k.dtype != v.dtype or any(n > 1 and a != b for n, a, b in zip(k.shape, strides, v.stride())):
             raise QcfgError(ESHAPE, "keys and values must agree in shape, type and strides")
         ctx._check(ctx.lib.qcfg_kv_append(ctx.h, self.pool._ref, self._ref, self.pool._batch(seqs, starts, k.shape[0]), k.data_ptr(),
                                           v.data_ptr(), _dtype(k.dtype), strides[0], strides[1], ctx._here(stream)))

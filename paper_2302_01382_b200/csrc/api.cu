@@ -883,6 +883,9 @@ struct DeviceScope {
   ~DeviceScope() { if (back >= 0) (void)cudaSetDevice(back); }
 };
 
+// Whether a stride between `count` things keeps 16-byte loads aligned; of one alone it is never used
+bool stride_ok(int64_t stride, int64_t count, int64_t es) { return count <= 1 || (stride * es) % 16 == 0; }
+
 bool dtype_ok(int t) { return t >= QCFG_FP32 && t <= QCFG_FP16; }
 int dtype_size(int t) { return t == QCFG_FP32 ? 4 : 2; }
 
@@ -1334,7 +1337,7 @@ int qcfg_kv_append(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache*
   if (!dtype_ok(dtype)) return set_error(c, QCFG_EINVAL, "kv_append: bad element type");
   if (batch->n_rows > 0 && batch->n > 0 && (!k_dev || !v_dev)) return set_error(c, QCFG_EINVAL, "kv_append: null pointer");
   const int64_t es = dtype_size(dtype);
-  if ((uintptr_t)k_dev % 16 || (uintptr_t)v_dev % 16 || (row_stride * es) % 16 || (head_stride * es) % 16)
+  if ((uintptr_t)k_dev % 16 || (uintptr_t)v_dev % 16 || !stride_ok(row_stride, batch->n_rows, es) || !stride_ok(head_stride, cache->kv_heads, es))
     return set_error(c, QCFG_EALIGN, "kv_append: pointers and strides must be multiples of 16 bytes");
   DeviceScope dev(c);
   if (!dev.ok) return set_error(c, QCFG_ECUDA, "kv_append: device not available");
@@ -1382,8 +1385,8 @@ int qcfg_kv_attention(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cac
   if (window < 0 || (window > 0 && !causal)) return set_error(c, QCFG_EINVAL, "kv_attention: a window needs causal attention");
   if (max_rows < 0 || max_len < 0) return set_error(c, QCFG_EINVAL, "kv_attention: negative hint");
   const int64_t es = dtype_size(dtype);
-  if ((uintptr_t)q_dev % 16 || (uintptr_t)out_dev % 16 || (q_row_stride * es) % 16 || (q_head_stride * es) % 16 || (out_row_stride * es) % 16 ||
-      (out_head_stride * es) % 16)
+  if ((uintptr_t)q_dev % 16 || (uintptr_t)out_dev % 16 || !stride_ok(q_row_stride, batch->n_rows, es) || !stride_ok(q_head_stride, q_heads, es) ||
+      !stride_ok(out_row_stride, batch->n_rows, es) || !stride_ok(out_head_stride, q_heads, es))
     return set_error(c, QCFG_EALIGN, "kv_attention: pointers and strides must be multiples of 16 bytes");
   const int64_t need = qcfg_kv_attention_work(ctx, cache, batch->n_rows, max_len);
   if (need > 0 && (!work_dev || work_bytes < need)) return set_error(c, QCFG_EINVAL, "kv_attention: %lld bytes of working memory needed", (long long)need);

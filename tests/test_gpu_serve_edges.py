@@ -304,3 +304,31 @@ def test_entries_whose_rows_are_not_there_are_left_out(ctx, starts):
                         assert torch.equal(a[page], b[page])
         k, v = cache.read(ints([0, 1]), ints([0, 0]), st, n)
         assert ctx.sync_status() == q.EPAGE
+
+
+# ----------------------------------------------------------------------------- strides nobody uses
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_strides_of_one_row_or_one_head_do_not_matter(ctx, dtype):
+    """A single row of a matrix of odd width, a single head between others, keys and values that differ in such a stride only."""
+    rng = np.random.default_rng(47)
+    for heads, rows in ((2, 1), (1, 3), (1, 1)):
+        pool, cache, po, co = make(ctx, 8, 16, 2, 4, heads, 64)
+        steps(ctx, pool, cache, po, co, [0], [20], dtype, rng)
+        x = dev(rng.standard_normal((rows, heads, 64)).astype(np.float32), dtype)
+        odd = torch.empty_strided(x.shape, (heads * 64 + 5 if rows == 1 else 72 * heads, 67 if heads == 1 else 64, 1), dtype=dtype, device="cuda")
+        odd.copy_(x)
+        seqs, st = ints([0]), ints([0, rows])
+        pool.extend(seqs, st)
+        assert po.extend([0], [rows])
+        cache.append(odd, odd if rows > 1 else x, seqs, st)
+        co.append(host(x), host(x), [0], [0, rows])
+        same_cache(cache, co)
+        want = cache.attention(x, seqs, st)
+        out = torch.empty_strided(x.shape, odd.stride(), dtype=dtype, device="cuda")
+        assert torch.equal(cache.attention(odd, seqs, st, out=out), want)
+        ctx.check_sync()
+    w, s = code_weights(rng, 1, 64)
+    out = torch.empty_strided((3, 1), (4, 7), dtype=dtype, device="cuda")
+    x = dev(rng.standard_normal((3, 64)).astype(np.float32), dtype)
+    assert torch.equal(ctx.linear_i8(x, w, s, out=out), ctx.linear_i8(x, w, s))
