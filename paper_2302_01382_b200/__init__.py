@@ -343,9 +343,9 @@ class Context:
         return q, scale
 
     def gemm_i8_token(self, qx: torch.Tensor, qw: torch.Tensor, k: int, scale_x: torch.Tensor, scale_w: torch.Tensor,
-                      bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, dtype: torch.dtype = torch.float32,
+                      bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, dtype: Optional[torch.dtype] = None,
                       out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        """act(float(qx qw^T) * (scale_x[m] * scale_w[n]) + bias[n]) as `dtype`."""
+        """act(float(qx qw^T) * (scale_x[m] * scale_w[n]) + bias[n]) as `dtype`: that of `out`, fp32 without one, unless given."""
         self._on_device(qx, qw, scale_x, scale_w, bias, out)
         for t in (qx, qw):
             _rows_of(t, torch.int8)
@@ -355,7 +355,7 @@ class Context:
         _vector(scale_x, m)
         _vector(scale_w, n)
         _vector(bias, n)
-        out = _output(out, (m, n), dtype, qx.device, stream)
+        out = _output(out, (m, n), dtype, torch.float32, qx.device, stream)
         self._check(self.lib.qcfg_gemm_i8_token(self.h, qx.data_ptr(), _ld(qx), qw.data_ptr(), _ld(qw), m, n, k, scale_x.data_ptr(),
                                                 scale_w.data_ptr(), _at(bias), act, out.data_ptr(), _dtype(out.dtype), _ld(out),
                                                 self._here(stream)))
@@ -365,7 +365,7 @@ class Context:
                   act: int = ACT_NONE, bits: int = 8, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
                   stream=None) -> torch.Tensor:
         """A linear layer on x (fp32, bf16 or fp16, quantized row by row) with the weight codes qw [n x ld] that
-        quantize(w, inv, PER_ROW, bits) gives and their scales.  `dtype` of the result: that of x unless given."""
+        quantize(w, inv, PER_ROW, bits) gives and their scales.  `dtype` of the result: that of `out`, or of x, unless given."""
         self._on_device(x, qw, scale_w, bias, out)
         _rows_of(x)
         _rows_of(qw, torch.int8)
@@ -374,7 +374,7 @@ class Context:
             raise QcfgError(ESHAPE, "x has more columns than the weight codes")
         _vector(scale_w, n)
         _vector(bias, n)
-        out = _output(out, (m, n), dtype or x.dtype, x.device, stream)
+        out = _output(out, (m, n), dtype, x.dtype, x.device, stream)
         size = self.lib.qcfg_linear_i8_work(m, k)
         work = _empty(size, torch.uint8, x.device, stream) if size else None
         self._check(self.lib.qcfg_linear_i8(self.h, x.data_ptr(), _dtype(x.dtype), _ld(x), bits, qw.data_ptr(), _ld(qw), m, n, k,
@@ -417,10 +417,13 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _output(out, shape, dtype, device, stream):
+def _output(out, shape, dtype, otherwise, device, stream):
     if out is None:
+        dtype = dtype or otherwise
         _dtype(dtype)
         return _empty(shape, dtype, device, stream)
+    if dtype is not None and out.dtype != dtype:
+        raise QcfgError(EINVAL, f"out is {out.dtype}, {dtype} is asked for")
     if tuple(out.shape) != tuple(shape) or (out.shape[-1] > 1 and out.stride(-1) != 1):
         raise QcfgError(ESHAPE, f"out must be {tuple(shape)} with adjacent columns")
     return out

@@ -332,3 +332,23 @@ def test_strides_of_one_row_or_one_head_do_not_matter(ctx, dtype):
     out = torch.empty_strided((3, 1), (4, 7), dtype=dtype, device="cuda")
     x = dev(rng.standard_normal((3, 64)).astype(np.float32), dtype)
     assert torch.equal(ctx.linear_i8(x, w, s, out=out), ctx.linear_i8(x, w, s))
+
+
+def test_a_type_that_is_not_the_outputs_is_refused(ctx):
+    import paper_2302_01382_b200 as q
+    rng = np.random.default_rng(53)
+    x = dev(rng.standard_normal((5, 64)).astype(np.float32), torch.bfloat16)
+    w, s = code_weights(rng, 32, 64)
+    codes, sx = ctx.quantize_tokens(x)
+    for call in (lambda **kw: ctx.linear_i8(x, w, s, **kw), lambda **kw: ctx.gemm_i8_token(codes, w, 64, sx, s, **kw)):
+        out = torch.zeros((5, 32), dtype=torch.float16, device="cuda")
+        for other in (torch.float32, torch.bfloat16):
+            with pytest.raises(q.QcfgError) as e:
+                call(out=out, dtype=other)
+            assert e.value.status == q.EINVAL
+        assert not out.any()
+        assert call(out=out, dtype=torch.float16) is out and torch.equal(out, call(dtype=torch.float16))
+        call(out=out.zero_())
+        assert torch.equal(out, call(dtype=torch.float16))
+    assert ctx.linear_i8(x, w, s).dtype == torch.bfloat16 and ctx.gemm_i8_token(codes, w, 64, sx, s).dtype == torch.float32
+    ctx.check_sync()
