@@ -359,7 +359,7 @@ int qcfg_kv_read(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* c
  * `rows` rows and len tokens row r stands at position p = len - rows + r.  It sees the tokens 0 .. p
  * (causal), with window > 0 only the last `window` of these, or all len tokens (causal == 0; window
  * must be 0).  out = softmax(sm_scale * q k^T) v over what it sees; a row that sees nothing (p < 0, an
- * empty sequence, an entry without one) gives zeros.  q_dev, out_dev: [n_rows] rows of
+ * empty sequence, an entry without one) gives zeros.  sm_scale: above 0, at most 2^126.  q_dev, out_dev: [n_rows] rows of
  * `dtype` with q_heads heads of head_dim elements, strides in elements, 16-byte aligned pointers and
  * strides (QCFG_EALIGN; those of a single row or head do not matter); head h reads cache head h / (q_heads / kv_heads).  out_dev must not
  * overlap q_dev.  A query with a NaN or Inf gives NaN where it sees something.  Sums, maxima and accumulators are fp32.

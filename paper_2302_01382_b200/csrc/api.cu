@@ -1381,7 +1381,7 @@ int qcfg_kv_attention(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cac
   if (batch->n_rows > 0 && q_dev == out_dev) return set_error(c, QCFG_EINVAL, "kv_attention: out_dev must not overlap q_dev");
   if (q_heads < 1 || q_heads % cache->kv_heads) return set_error(c, QCFG_ESHAPE, "kv_attention: q_heads must be a multiple of kv_heads");
   if (q_heads > 65535) return set_error(c, QCFG_ESHAPE, "kv_attention: too many heads");
-  if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return set_error(c, QCFG_EINVAL, "kv_attention: sm_scale must be positive and finite");
+  if (!(sm_scale > 0.0f) || sm_scale > 0x1p126f) return set_error(c, QCFG_EINVAL, "kv_attention: sm_scale must be positive and at most 2^126");
   if (window < 0 || (window > 0 && !causal)) return set_error(c, QCFG_EINVAL, "kv_attention: a window needs causal attention");
   if (max_rows < 0 || max_len < 0) return set_error(c, QCFG_EINVAL, "kv_attention: negative hint");
   const int64_t es = dtype_size(dtype);
@@ -1464,7 +1464,7 @@ int qcfg_model_set_attention(qcfg_ctx* ctx, qcfg_model* model, int32_t layer, in
   if (page_tokens != 16 && page_tokens != 32 && page_tokens != 64 && page_tokens != 128)
     return set_error(c, QCFG_ESHAPE, "set_attention: page_tokens must be 16, 32, 64 or 128, got %d", page_tokens);
   if (seq_len < 1 || seq_len > 0x7fffffff - 4096) return set_error(c, QCFG_ESHAPE, "set_attention: bad seq_len");
-  if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return set_error(c, QCFG_EINVAL, "set_attention: sm_scale must be positive and finite");
+  if (!(sm_scale > 0.0f) || sm_scale > 0x1p126f) return set_error(c, QCFG_EINVAL, "set_attention: sm_scale must be positive and at most 2^126");
   if (window < 0 || (window > 0 && !causal)) return set_error(c, QCFG_EINVAL, "set_attention: a window needs causal attention");
   AttnInput t;
   t.on = true; t.k = k_layer; t.v = v_layer; t.q_heads = q_heads; t.kv_heads = kv_heads; t.dim = (int32_t)dim; t.seq_len = seq_len;

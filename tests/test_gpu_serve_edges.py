@@ -352,3 +352,20 @@ def test_a_type_that_is_not_the_outputs_is_refused(ctx):
         assert torch.equal(out, call(dtype=torch.float16))
     assert ctx.linear_i8(x, w, s).dtype == torch.bfloat16 and ctx.gemm_i8_token(codes, w, 64, sx, s).dtype == torch.float32
     ctx.check_sync()
+
+
+def test_the_largest_score_scale(ctx):
+    """Scales are multiplied with log2(e) in fp32: one for which that is no number is refused, the largest one works."""
+    import paper_2302_01382_b200 as q
+    rng = np.random.default_rng(59)
+    pool, cache, po, co = make(ctx, 8, 16, 2, 4, 2, 64)
+    steps(ctx, pool, cache, po, co, [0], [20], torch.float32, rng, spread=0.1)
+    x = torch.zeros((1, 2, 64), device="cuda")
+    for scale in (2.0 ** 127, 2.5e38, float("inf"), float("nan"), 0.0, -1.0):
+        with pytest.raises(q.QcfgError) as e:
+            cache.attention(x, ints([0]), sm_scale=scale)
+        assert e.value.status == q.EINVAL
+    out = host(cache.attention(x, ints([0]), sm_scale=2.0 ** 126))
+    want, tol = attention_bound(host(x), *co.values(0), 1.0, True, 0, torch.float32)      # all scores are 0
+    assert (np.abs(out - want) <= tol).all()
+    ctx.check_sync()
