@@ -624,15 +624,19 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
   }
 }
 
+// Blocks of a launch: entry i owns those from starts[i] / per_block + i on, for each head
+int64_t prompt_blocks(const AttnArgs& a) {
+  const int per_block = 2 * (kTileRows / (a.q_heads / a.cache.heads));
+  return (a.batch.starts ? a.batch.rows / per_block + a.batch.n : 2 * (int64_t)a.batch.n) * a.cache.heads;
+}
+
 template <typename T, int D>
 int prompt_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
   constexpr int smem = prompt_smem<D, sizeof(T) == 4>();
   static DeviceOnce once;
   const cudaError_t e = once.smem(device_of(ctx), (const void*)kv_attention_prompt<T, D>, smem);
   if (e != cudaSuccess) return check_cuda(ctx, e, "kv_attention");
-  const int per_block = 2 * (kTileRows / (a.q_heads / a.cache.heads));
-  const int64_t items = a.batch.starts ? a.batch.rows / per_block + a.batch.n : 2 * (int64_t)a.batch.n;
-  launch_pdl(kv_attention_prompt<T, D>, dim3((unsigned)(items * a.cache.heads)), dim3(kPromptThreads), smem, st, a);
+  launch_pdl(kv_attention_prompt<T, D>, dim3((unsigned)prompt_blocks(a)), dim3(kPromptThreads), smem, st, a);
   count_launch(ctx);
   return check_cuda(ctx, cudaGetLastError(), "kv_attention");
 }
@@ -650,6 +654,7 @@ int prompt_as(Ctx* ctx, const AttnArgs& a, cudaStream_t st) {
 bool prompt_pays(Ctx* ctx, const AttnArgs& a, int dtype, int64_t rows) {
   const int group = a.q_heads / a.cache.heads;
   if (group > kTileRows || (a.cache.dim != 64 && a.cache.dim != 128) || (dtype == QCFG_FP32 && a.cache.dim != 64)) return false;
+  if (prompt_blocks(a) > 0x7fffffff) return false;       // (a grid's limit; the streaming kernel's grid does not grow with the batch)
   const int64_t blocks = std::max<int64_t>(a.batch.n, (a.batch.rows * group + 255) / 256) * a.cache.heads;
   return rows * group >= (a.cache.dim == 128 ? 32 : 64) && 3 * blocks >= sm_count(ctx);
 }

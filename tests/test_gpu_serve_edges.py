@@ -369,3 +369,27 @@ def test_the_largest_score_scale(ctx):
     want, tol = attention_bound(host(x), *co.values(0), 1.0, True, 0, torch.float32)      # all scores are 0
     assert (np.abs(out - want) <= tol).all()
     ctx.check_sync()
+
+
+def test_a_batch_of_more_blocks_than_a_grid_has(ctx):
+    """A million entries, mostly empty, of 4096 heads: the kernel for many rows would need more than 2^31 blocks."""
+    rng = np.random.default_rng(61)
+    n, heads, dim, rows = 1 << 20, 4096, 64, 256
+    pool, cache, po, co = make(ctx, 2, 128, 2, 2, 1, dim)      # the oracle holds one head
+    import paper_2302_01382_b200 as q
+    cache = q.KvCache(pool, heads, dim)
+    k, v = (rng.standard_normal((rows, 1, dim)).astype(np.float32) for _ in range(2))
+    seqs, st = ints([1]), ints([0, rows])
+    pool.extend(seqs, st)
+    cache.append(dev(k).expand(-1, heads, -1).contiguous(), dev(v).expand(-1, heads, -1).contiguous(), seqs, st)
+    assert po.extend([1], [rows])
+    co.append(k, v, [1], [0, rows])
+    x = rng.standard_normal((rows, 1, dim)).astype(np.float32)
+    xd = dev(x, torch.float16)
+    many = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    starts = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    many[-1], starts[-1] = 1, rows
+    out = cache.attention(xd.expand(-1, heads, -1).contiguous(), many, starts, max_new=rows)
+    ctx.check_sync()
+    want, tol = attention_bound(host(xd), *co.values(1), dim ** -0.5, True, 0, torch.float16)
+    assert (np.abs(host(out) - want) <= tol).all()             # every head (parts are cut at other places: not the same bits)
