@@ -141,25 +141,6 @@ __device__ __forceinline__ int seq_len(const PoolView& p, int s) {
   const int len = p.len[s];
   return len < 0 ? 0 : (len > most ? (int)most : len);
 }
-// Work item `item` of a launch in which entry i owns items [starts[i] / unit + extra * i, ...): the entry it belongs to.  Every
-// entry has at least rows / unit + extra of them.  Whole block; all threads return the same.
-__device__ __forceinline__ int entry_of_item(const BatchView& b, int64_t item, int unit, int extra, int64_t& first) {
-  if (!b.starts) {
-    const int i = (int)(item / (1 + extra));
-    first = (int64_t)i * (1 + extra);
-    return i;
-  }
-  // base(i) ascends, so the number of entries whose base is not behind the item is the answer; counted by the whole block
-  int count = 0;
-  for (int i0 = 0; i0 < b.n; i0 += blockDim.x) {
-    const int i = i0 + threadIdx.x;
-    count += __syncthreads_count(i < b.n && (int64_t)b.starts[i] / unit + (int64_t)extra * i <= item);
-  }
-  const int i = count - 1;
-  first = i < 0 ? 0 : (int64_t)b.starts[i] / unit + (int64_t)extra * i;
-  return i;
-}
-
 // Exclusive prefix sum over a block of up to 1024 threads; `total` gets the sum.  `buf`: 33 integers of shared memory.
 __device__ __forceinline__ int block_scan(int v, int* buf, int& total) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, nw = (blockDim.x + 31) >> 5;
