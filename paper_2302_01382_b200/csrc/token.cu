@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kTokenThreads, HELD == 2 ? 6 : HELD == 4 ? 5 :
 constexpr int kFewWarps = 16, kAhead = 4, kStep = 2048;
 constexpr int kRingBytes = kFewWarps * kAhead * kStep;
 constexpr int kRawElements = 16384, kRawTokens = 8;      // X_RAW up to this many
-template <int NT> __host__ __device__ constexpr int few_tiles() { return NT <= 2 ? 8 : 4; }      // accumulators: NT x 4 registers each
+template <int NT> __host__ __device__ constexpr int few_tiles() { return NT == 1 ? 8 : 4; }      // accumulators: NT x 4 registers each
 template <int NT> __host__ __device__ constexpr int sum_tiles() { return NT <= 2 ? 4 : 2; }      // tiles added up at a time
 template <int NT> __host__ __device__ constexpr int few_bytes() {      // the ring, and the sums in its place once it is empty
   return kRingBytes > kFewWarps * sum_tiles<NT>() * NT * 512 ? kRingBytes : kFewWarps * sum_tiles<NT>() * NT * 512;
@@ -429,12 +429,14 @@ static int few_raw(Ctx* ctx, const FewArgs& a, cudaStream_t st) {
   return a.t.dtype == QCFG_FP32 ? few_as<TX, float, 1, true>(ctx, a, st) : a.t.dtype == QCFG_BF16 ? few_as<TX, __nv_bfloat16, 1, true>(ctx, a, st)
                                                                                                  : few_as<TX, __half, 1, true>(ctx, a, st);
 }
-// Whether a product goes this way or in the GEMM's tiles of 128 rows.  us, this way / tiles, codes ready, tokens x k x n:
-//   8 x 4096 x 16384 8.7 / 12.2    16 x 4096 x 16384 12.1 / 12.3    24 x 4096 x 16384 18.8 / 12.5    32 x 4096 x 16384 26.1 / 12.9
-//   24 x 768 x 768 2.9 / 4.6    24 x 1024 x 4096 4.7 / 5.8    24 x 4096 x 4096 8.1 / 11.4    24 x 16384 x 4096 20.2 / 33.3
-//   24 x 8192 x 8192 15.4 / 18.7    32 x 16384 x 4096 28.4 / 33.3
-// The GEMM narrows its tiles to 64 columns and fewer for these, and its ring of eight stages then holds too few weights.
-static bool few_pays(Ctx* ctx, int64_t m, int64_t n) { return m <= 16 || (m <= 32 && n <= 64 * (int64_t)sm_count(ctx)); }
+// Whether a product goes this way or in the GEMM's tiles of 128 rows.  us, this way / tiles, codes ready, other weights with each call, so that
+// they come from HBM, tokens x k x n:
+//   1 x 4096 x 16384 13.0 / 15.2    8 x 4096 x 16384 14.2 / 15.3    8 x 4096 x 50257 39.7 / 47.0    8 x 768 x 3072 2.8 / 4.7
+//   16 x 4096 x 16384 16.0 / 15.2   16 x 2048 x 32000 19.5 / 15.7   24 x 4096 x 16384 21.2 / 15.3   32 x 4096 x 16384 29.1 / 15.2
+//   16 x 1024 x 4096 3.9 / 5.5      24 x 768 x 768 3.0 / 4.4        24 x 1024 x 4096 4.6 / 5.5      24 x 4096 x 4096 9.3 / 11.1
+//   24 x 16384 x 4096 22.0 / 33.6   24 x 8192 x 8192 18.2 / 19.9    32 x 16384 x 4096 30.4 / 33.7   17 x 4096 x 9472 12.5 / 12.3
+// The GEMM narrows its tiles to 64 columns and fewer for up to 64 columns a SM, and its ring of eight stages then holds too few weights.
+static bool few_pays(Ctx* ctx, int64_t m, int64_t n) { return m <= 8 || (m <= 32 && n <= 64 * (int64_t)sm_count(ctx)); }
 static int launch_few(Ctx* ctx, const TokenGemm& t, cudaStream_t st) {
   const FewArgs a{t, nullptr, 0, 0.0f, t.early, err_word(ctx)};
   return t.dtype == QCFG_FP32 ? few_codes<float>(ctx, a, st) : t.dtype == QCFG_BF16 ? few_codes<__nv_bfloat16>(ctx, a, st) : few_codes<__half>(ctx, a, st);
