@@ -2480,6 +2480,16 @@ int launch_gemm_group(Ctx* ctx, const GemmArgs* gs_in, int count, cudaStream_t s
     }
     p.bn = bn;
   }
+  // Where no pairs share them, tiles of 128 rows by 256 columns leave room for two stages behind what their epilogue holds, and three are
+  // needed: the width up to 224 whose tiles keep the SMs busy.
+  if (token && !pair && bn == 256 && g0.m > 64) {
+    int64_t best = 0x7fffffffffffffffll;
+    for (int w = 224; w >= 128; w -= 32) {
+      const int64_t cost = ((g0.n + w - 1) / w * row_tiles + sm_count(ctx) - 1) / sm_count(ctx) * w;
+      if (cost < best) { best = cost; bn = w; }
+    }
+    p.bn = bn;
+  }
   const int tile_rows = pair ? 2 * BM : BM;
   p.tiles_m = slab ? (int32_t)(pair ? (row_tiles + 1) / 2 : row_tiles) : (int32_t)((g0.m + tile_rows - 1) / tile_rows);
   const int a_box = token && !pair && g0.m <= 64 ? (g0.m <= 32 ? 32 : 64) : BM;

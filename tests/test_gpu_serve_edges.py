@@ -393,3 +393,21 @@ def test_a_batch_of_more_blocks_than_a_grid_has(ctx):
     ctx.check_sync()
     want, tol = attention_bound(host(xd), *co.values(1), dim ** -0.5, True, 0, torch.float16)
     assert (np.abs(host(out) - want) <= tol).all()             # every head (parts are cut at other places: not the same bits)
+
+
+@pytest.mark.parametrize("m,k,n", [(65, 100, 18945), (68, 817, 21776), (77, 1, 25749), (100, 257, 32001), (128, 1000, 50257)])
+@pytest.mark.parametrize("dtype,act,with_bias", [(torch.float32, "none", False), (torch.float16, "gelu", True)])
+def test_linear_of_one_row_of_tiles_into_many_columns(ctx, m, k, n, dtype, act, with_bias):
+    """65 to 128 tokens into more columns than tiles of 128 cover on 148 SMs."""
+    linear_against_oracle(ctx, m, k, n, dtype, act, with_bias)
+
+
+@pytest.mark.parametrize("m,k,n", [(100, 96, 20000), (300, 100, 700), (1000, 300, 4001), (1500, 64, 6000)])
+def test_linear_without_pairs_of_ctas(m, k, n):
+    import paper_2302_01382_b200 as q
+    c = q.Context(0)
+    try:
+        c.set_pair_tiles(False)
+        linear_against_oracle(c, m, k, n, torch.bfloat16, "relu", True)
+    finally:
+        c.close()
