@@ -971,7 +971,8 @@ __device__ __forceinline__ void epilogue_token(const GroupDesc& G, const CUtenso
     }
     const int left = G.n - col0 - 32 * c;
     if (left <= 0) continue;
-    if (o.tma) {
+    // (a TMA store writes whole pieces of 16 bytes, of which the last may lie behind the last column)
+    if (o.tma && (left >= 32 || (left & (wide ? 3 : 7)) == 0)) {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) tma_store_2d(map, stage, col0 + 32 * c, row0);

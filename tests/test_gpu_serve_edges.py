@@ -411,3 +411,20 @@ def test_linear_without_pairs_of_ctas(m, k, n):
         linear_against_oracle(c, m, k, n, torch.bfloat16, "relu", True)
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("m,k,n", [(1, 64, 51), (24, 2304, 9001), (33, 100, 1), (100, 257, 1557), (211, 141, 20003), (949, 22, 2310), (1756, 1085, 5)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_linear_writes_no_column_behind_the_last(ctx, m, k, n, dtype):
+    """Outputs on 16-byte boundaries, rows too, that end inside 16 bytes: what lies behind belongs to somebody else."""
+    rng = np.random.default_rng(m + n)
+    x = dev(rng.standard_normal((m, k)).astype(np.float32), dtype)
+    w, sw = code_weights(rng, n, (k + 15) // 16 * 16)
+    w[:, k:] = 0
+    room = torch.full((m + 2, (n + 7) // 8 * 8 + 16), 7.0, dtype=dtype, device="cuda")
+    bias = torch.ones(n, device="cuda")
+    ctx.linear_i8(x, w, sw, bias=bias, out=room[1:m + 1, 8:8 + n])
+    assert torch.equal(room[1:m + 1, 8:8 + n], ctx.linear_i8(x, w, sw, bias=bias))
+    room[1:m + 1, 8:8 + n] = 7
+    assert (room == 7).all()
+    ctx.check_sync()
