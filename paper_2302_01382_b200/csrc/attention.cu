@@ -31,8 +31,8 @@ namespace {
 // In the A operand an element of K is (token, dimension), of V^T (dimension, token); the sums run over dimensions and
 // tokens in any order, so both are read 16 bytes at a time as they lie in memory.
 //
-// HBM bounds it, and close behind it the issue slots: 64 entries of one bf16 token over contexts of 8000, 32 heads on 8 of 128, 114 us;
-// one over 131000 tokens 56 us (4.9 and 4.8 TB/s, 74% of the measured copy rate, the second kernel's 5 us and the first's start included).
+// HBM bounds it, and close behind it the issue slots: 64 entries of one bf16 token over contexts of 8000, 32 heads on 8 of 128, 119 us;
+// one over 131000 tokens 57 us (both 4.7 TB/s, 71% of the measured copy rate, the second kernel's 5 us and the first's start included).
 constexpr int kUnit = 64;           // tokens
 constexpr int kSetup = 2;           // units
 constexpr int kRun = 32;            // tokens a warp takes at a time
@@ -42,14 +42,13 @@ constexpr int kMinUnits = 2;        // a block takes at least this many
 // rescaled a few times in a context and not at every new maximum; a weight stays below 2^15.  fp32 calls take most of fp16's room above 1
 // for the digits of small weights instead: a second half ends at 2^-25, and a weight is held times 2^9, so its 22 bits reach down to 2^-12
 // of the largest and what is lost of smaller ones is 2^-34 of it.  (Held as they are, 40000 tokens of weight 2^-21.5 gave a sum off by 1%.
-// 2^13 with 2 orders of slack: 32 entries of 16 tokens over 1000, 16 heads on 8 of 64, 48 -> 54 us, 52 this way: rows move too often.)
+// 2^13 with 2 orders of slack: 32 entries of 16 tokens over 1000, 16 heads on 8 of 64, 48 -> 54 us, 50 this way: rows move too often.)
 template <bool WIDE> __host__ __device__ constexpr float weight_slack() { return WIDE ? 6.0f : 8.0f; }
 template <bool WIDE> __host__ __device__ constexpr int weight_order() { return WIDE ? 9 : 0; }
 // A row's weights are multiplied with their page's value scale times `low` = 2^(weight_order - d), which follows the row's largest such
 // product as ref follows its largest score: so what a row keeps depends on nothing but the tokens it sees, whatever the values of others
-// in its tile.  (One factor for the tile, the largest scale seen by any of its rows, cost causal rows in front of values 2^20 times
-// as large all their digits.)  In 16-bit calls the
-// product that sets d becomes a power of two, which fp16 holds as it is.
+// in its tile.  (One factor for the tile, the largest scale seen by any of its rows, cost causal rows in front of values 2^20 times as
+// large all their digits.)  In 16-bit calls the product that sets d becomes a power of two, which fp16 holds as it is.
 template <int DP> __host__ __device__ constexpr int stage_bytes() { return 2 * kRun * DP + 32; }             // keys, values, four maxima
 template <int DP, int NR> __host__ __device__ constexpr int stream_blocks() { return DP == 256 ? 1 : DP == 128 ? (NR == 4 ? 2 : 3) : NR == 1 ? 4 : NR == 2 ? 3 : 2; }    // per SM
 template <int DP, int NR> __host__ __device__ constexpr int stream_stages() { return DP == 256 ? 3 : DP == 128 ? (NR == 4 ? 3 : 2) : (NR == 1 ? 3 : 4); }

@@ -48,9 +48,8 @@ __device__ __forceinline__ float lg2(float x) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// Two bytes of a word of codes plus 128 as fp16 codes: 0x6400 + b is 1024 + b.  `magic` is 0x64646464, read from shared memory once: a
-// constant the compiler knows it keeps in a uniform register and copies anew in front of almost every permutation, 118 of a run's
-// 870 instructions in the streaming kernel.
+// Two bytes of a word of codes plus 128 as fp16 codes: 0x6400 + b is 1024 + b.  `magic` is 0x64646464, read from shared memory once: as a
+// compile-time constant it cost 118 of the 870 instructions that a run of the streaming kernel took then.
 template <uint32_t SEL>
 __device__ __forceinline__ uint32_t two_codes(uint32_t biased, uint32_t magic) {
   const uint32_t w = __byte_perm(biased, magic, SEL);

@@ -908,7 +908,8 @@ __device__ __forceinline__ void epilogue_rows(const GroupDesc& G, uint32_t tbase
 
 // One warp's 32 rows of a layer with a scale for each row (FL_TOKEN): act(float(acc) * (sx * sw) + bias), the product of the scales
 // first.  sw, bias: the warp's columns; sx: this lane's row.  32 columns at a time, through one staging slot: by TMA (rows of 128
-// bytes, 128B swizzle, or of 64 bytes, 64B swizzle), or, where rows are not 16-byte aligned, row by row with an element per lane.
+// bytes, 128B swizzle, or of 64 bytes, 64B swizzle), or, where rows are not 16-byte aligned or end inside 16 bytes, row by row with an
+// element per lane.
 template <bool PAIR>
 __device__ __forceinline__ void epilogue_token(const GroupDesc& G, const CUtensorMap* map, uint32_t tbase, const float* sw, const float* bias, float sx,
                                                uint32_t stage, int nch, int m, int row0, int col0, int lane, uint32_t tempty_bar) {
@@ -2086,8 +2087,6 @@ bool make_out_map(CUtensorMap* map, const OutDesc& o, int64_t m, int64_t n) {
                    esz == 4 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE);
 }
 
-// Tensor map of the output a fast epilogue body writes: 32-row boxes of 64 int8 columns (64B
-// swizzle), of 64 bf16 or of 32 fp32 columns (128B swizzle).
 // FL_TOKEN: pieces of 32 rows x 32 columns
 bool make_token_map(CUtensorMap* map, const OutDesc& o, int64_t m, int64_t n) {
   const int esz = o.kind == 3 ? 4 : 2;
@@ -2095,6 +2094,8 @@ bool make_token_map(CUtensorMap* map, const OutDesc& o, int64_t m, int64_t n) {
   return encode_2d(map, o.kind == 3 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, o.ptr, (uint64_t)n, (uint64_t)m, (uint64_t)(o.ld * esz),
                    32u, 32u, o.kind == 3 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
+// Tensor map of the output a fast epilogue body writes: 32-row boxes of 64 int8 columns (64B
+// swizzle), of 64 bf16 or of 32 fp32 columns (128B swizzle).
 bool make_fast_map(CUtensorMap* map, const OutDesc& o, int64_t m, int64_t n) {
   const bool codes = o.kind == 1, half = o.kind == 2;
   const int esz = codes ? 1 : half ? 2 : 4;

@@ -9,12 +9,12 @@
 //   warp 11          issues the MMAs: S0, S1, then for each step O0 += P0 V, S0 of the next step, O1 += P1 V, S1 of the next step.
 //                    While one tile's weights are computed, the tensor core works for the other.
 // Each step and tile costs 2 x 128 x 128 x dim products (1024 cycles for both tiles at dim 128, twice) and 128 x 128 exponentials
-// (16 per cycle: 2048 cycles for both tiles): the exponentials and the tensor core are equally long.  40% of the issue slots are used.
+// (16 per cycle: 2048 cycles for both tiles): the exponentials and the tensor core are equally long.  43% of the issue slots are used.
 //
 // What bounds it is neither but the chain of one tile: a step takes 4300 cycles, 2450 for a warp's 32 rows of weights (also where it
 // has its scheduler to itself), 350 until the tensor core knows of them, 1500 for the two products and the way back.  A block
 // costs 14000 cycles besides its steps (who it is, the queries, the first codes, the output).  4 entries of up to 2048 bf16 tokens behind up
-// to 4000, 32 heads on 8 of 128: 366 us, 837 TFLOP/s, 52% of the measured bf16 rate; 32 entries of up to 384 fp32 tokens, 12 heads of 64: 72 us.
+// to 4000, 32 heads on 8 of 128: 367 us, 836 TFLOP/s, 51% of the measured bf16 rate; 32 entries of up to 384 fp32 tokens, 12 heads of 64: 73 us.
 // Tried against 370 us then: scores, weights and products in halves of 64 tokens, so that a tile never waits (403: 48 MMAs a step in
 // place of 32, at 54 cycles each whatever their width), weights in halves only (398), a warp that issues for each tile (448: registers),
 // queries fetched before the TMEM is there (383: registers).
