@@ -341,7 +341,6 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
       d_of[warp][lane] = 0.0f;
     }
     float2 low_here = make_float2(0.0f, 0.0f);      // (NR = 1)
-    float cap = 0.0f;                  // vf * low stays finite up to here; only tokens that no row sees can have more
     __syncwarp();
 
     // pages of the next 32 runs: lane l holds those of run l of the window, for its first and second 16 tokens
@@ -549,7 +548,6 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
         }
         fresh = __any_sync(0xffffffffu, fresh);
         least = (float)__reduce_min_sync(0xffffffffu, (int)floorf(least));
-        cap = exp2_of(min(126 - weight_order<WIDE>() + (int)least, 127));
         __syncwarp();
       }
       float2 low2[NR];
@@ -560,7 +558,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
       for (int p = 0; p < 2; ++p) {
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-          const float share0 = fminf(vf[p], cap) * low2[n].x, share1 = fminf(vf[p], cap) * low2[n].y;
+          // (kept finite: tokens a row does not see have weights of 0)
+          const float share0 = fminf(vf[p] * low2[n].x, 8.5e37f), share1 = fminf(vf[p] * low2[n].y, 8.5e37f);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const float e0 = ex2(s[p][n][2 * j]), e1 = ex2(s[p][n][2 * j + 1]);

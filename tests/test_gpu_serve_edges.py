@@ -263,6 +263,32 @@ def test_a_row_does_not_depend_on_values_it_does_not_see(ctx, dtype, page, q_hea
     ctx.check_sync()
 
 
+@pytest.mark.parametrize("small,large", [(1e-25, 1e20), (1e-4, 1e35), (1e-36, 1.0)])
+@pytest.mark.parametrize("page,q_heads,heads,dim", [(16, 4, 2, 64), (32, 8, 1, 128), (16, 3, 3, 80), (64, 26, 26, 64), (16, 32, 8, 128)])
+@pytest.mark.parametrize("dtype", DTYPES[:2])
+def test_rows_of_a_tile_that_see_values_of_any_size(ctx, dtype, page, q_heads, heads, dim, small, large):
+    """Rows that see small values only share tiles with rows that see large ones, up to 2^150 apart, further than the factors of one row's
+    may be from another's in fp32.  A weight below 2^-125 of the largest may be 0."""
+    rng = np.random.default_rng(page + dim)
+    pool, cache, po, co = make(ctx, 300 // page + 8, page, 1, 300 // page + 2, heads, dim)
+    for n, size in ((100 // page * page + page, small), (9, large), (13, small)):
+        steps(ctx, pool, cache, po, co, [0], [n], torch.float32, rng, spread=size)
+    cache.k_absmax.fill_(4.0)                      # keys of ordinary size
+    co.absmax[0][:] = 4
+    length = po.lens[0]
+    k, v = co.values(0)
+    for rows, kw in ((30, {}), (30, {"window": 20}), (30, {"max_len": 200}), (length, {"max_new": 400}), (length, {"max_new": 400, "window": 20})):
+        x = dev(rng.standard_normal((rows, q_heads, dim)).astype(np.float32), dtype)
+        got = host(cache.attention(x, ints([0]), ints([0, rows]), **kw))
+        want, tol = seen_bound(host(x), k, v, page, dim ** -0.5, True, kw.get("window", 0), dtype)
+        mask = so.seen(rows, length, True, kw.get("window", 0))
+        for h in range(q_heads):
+            tol[:, h] += 2.0 ** -125 * np.where(mask, np.abs(v[:, h // (q_heads // heads)]).max(1)[None, :], 0).sum(1)[:, None]
+        worst = np.abs(got - want) - tol
+        assert (worst <= 0).all(), (rows, kw, float(worst.max()), np.argwhere(worst > 0)[:4].tolist(), len(np.argwhere(worst > 0)))
+    ctx.check_sync()
+
+
 # ----------------------------------------------------------------------------- rows out of range
 
 @pytest.mark.parametrize("starts", [[0, 2, 7], [0, 2, 1], [-1, 2, 4], [0, 2, -3]])
