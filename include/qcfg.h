@@ -365,7 +365,7 @@ int qcfg_kv_read(qcfg_ctx* ctx, const qcfg_kv_pool* pool, const qcfg_kv_cache* c
  * strides (QCFG_EALIGN; those of a single row or head do not matter); head h reads cache head h / (q_heads / kv_heads).  out_dev must not
  * overlap q_dev.  A query with a NaN or Inf gives NaN where it sees something.  Sums, maxima and accumulators are fp32.
  * A row depends on nothing but the tokens it sees.  Of these, weights times page scales are held to 11 bits (22 in fp32 calls), and
- * to 2^-30 (2^-34) of the row's largest such product; a weight below 2^-125 of the row's largest may be 0.
+ * to 2^-30 (2^-34) of the row's largest such product; a weight below 2^-110 of the row's largest may be lost.
  * max_rows, max_len: the longest entry's rows and the longest sequence's tokens as far as the caller
  * knows them (0: unknown).  They only choose how the work is spread; the results hold for any value.
  * work_dev: qcfg_kv_attention_work bytes (of the same n_rows and max_len; 0: may be NULL) on a 256-byte

@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(32 * kStreamWarps, stream_blocks<DP, NR>()) kv
       for (int p = 0; p < 2; ++p) {
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-          // (kept finite: tokens a row does not see have weights of 0)
+          // (kept finite: tokens a row does not see have weights of 0; one of 2^-110 and less may lose by it)
           const float share0 = fminf(vf[p] * low2[n].x, 8.5e37f), share1 = fminf(vf[p] * low2[n].y, 8.5e37f);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {

@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt(const A
               float at1, share1;
               if constexpr (WIDE) {
                 at1 = shift;
-                share1 = fminf(value[2 * c + z] * low, 8.5e37f);          // (tokens not seen may pass fp32)
+                share1 = fminf(value[2 * c + z] * low, 8.5e37f);          // (kept finite for tokens not seen; a weight of 2^-110 and less may lose)
               } else {                       // never below 2^-100, so that the sums keep what the values lose
                 at1 = fmaxf(z ? both_at.y : both_at.x, shift - 100.0f);
                 share1 = fminf(z ? both_share.y : both_share.x, 0x1p100f);
